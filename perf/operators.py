@@ -299,7 +299,7 @@ def work(case):
     if kind == "append":
         M, P, Hq, Hkv, D = (case[n] for n in ("M", "P", "Hq", "Hkv", "D"))
         heads, cached = Hq + 2 * Hkv, 2 * M * Hkv
-            bytes_ = 2 * M * heads * D + 4 * M + 4 * M * D + 2 * M * Hq * D + (4 * D if case["norm"] else 0)
+        bytes_ = 2 * M * heads * D + 4 * M + 4 * M * D + 2 * M * Hq * D + (4 * D if case["norm"] else 0)
         bytes_ += 2 * cached * D if case["fmt"] == "fp16" else cached * (D + 2) + 2 * cached * D    # codes and scales, and the values read back
         return {"bytes": bytes_, "flops": M * (Hq + Hkv) * D * (3.0 + (4.0 if case["norm"] else 0.0)) + (4.0 * cached * D if case["fmt"] != "fp16" else 0.0)}
     if kind == "read":
