@@ -167,7 +167,7 @@ def prepare(case, seed):
         if kind == "attn":
             s["ws"] = B.new_workspace(B.tree_verify_attn_kv8_workspace_bytes(M, P, Hq, Hkv, D_ATTN))
         elif kind == "sample":
-            s["ws"] = B.new_workspace(B.sample_workspace_bytes(M, V))
+            s["ws"] = B.new_workspace(B.lm_head_sample_workspace_bytes(M, V))
     return s
 
 
@@ -270,21 +270,21 @@ def run(s):
 def _run_own(s, case, kind):
     from paper_2505_22179_amd import binding as B
     if kind == "sample":
-        B.sample_tokens(s["logits"], case["M"], case["V"], s["temperature"], s["top_k"], s["top_p"], s["min_p"], s["u"], s["token"], s["prob"], s["ws"])
+        B.lm_head_sample(s["logits"], case["M"], case["V"], s["temperature"], s["top_k"], s["top_p"], s["min_p"], s["u"], s["token"], s["prob"], s["ws"])
         return s["token"], s["prob"]
     if kind == "append" and case["fmt"] == "fp16":
         M, P, Hq, Hkv, D = (case[n] for n in ("M", "P", "Hq", "Hkv", "D"))
-        B.qk_norm_rope_append(s["qkv"], s["gq"], s["gk"], EPS, s["pos"], s["cos"], s["sin"], P + M, s["q"], s["k"], s["v"], M, P, Hq, Hkv, D)
+        B.rope_append_qk_norm(s["qkv"], s["gq"], s["gk"], EPS, s["pos"], s["cos"], s["sin"], P + M, s["q"], s["k"], s["v"], M, P, Hq, Hkv, D)
         return s["q"], s["k"], s["v"]
     fmt = B.KV8_INT8 if case["fmt"] == "int8" else B.KV8_E4M3
     if kind == "append":
         M, P, Hq, Hkv, D = (case[n] for n in ("M", "P", "Hq", "Hkv", "D"))
-        B.kv8_append(s["qkv"], s["gq"], s["gk"], EPS, s["pos"], s["cos"], s["sin"], P + M, s["q"], s["k"], s["v"], s["ks"], s["vs"], fmt,
+        B.rope_append_kv8(s["qkv"], s["gq"], s["gk"], EPS, s["pos"], s["cos"], s["sin"], P + M, s["q"], s["k"], s["v"], s["ks"], s["vs"], fmt,
                      M, P, Hq, Hkv, D)
-        B.kv8_read(s["k"], s["v"], s["ks"], s["vs"], fmt, P, M, Hkv, D, s["k_out"], s["v_out"])   # the values that the codes stand for
+        B.w4a16_kv8_read(s["k"], s["v"], s["ks"], s["vs"], fmt, P, M, Hkv, D, s["k_out"], s["v_out"])   # the values that the codes stand for
         return s["q"], s["k_out"], s["v_out"]
     if kind == "read":
-        B.kv8_read(s["k"], s["v"], s["ks"], s["vs"], fmt, case["first"], case["rows"], case["Hkv"], case["D"], s["k_out"], s["v_out"])
+        B.w4a16_kv8_read(s["k"], s["v"], s["ks"], s["vs"], fmt, case["first"], case["rows"], case["Hkv"], case["D"], s["k_out"], s["v_out"])
         return s["k_out"], s["v_out"]
     B.tree_verify_attn_kv8(s["q"], s["k"], s["v"], s["ks"], s["vs"], fmt, s["mask"], s["out"], case["M"], case["P"], case["Hq"], case["Hkv"],
                            D_ATTN, D_ATTN ** -0.5, s["ws"])
