@@ -269,6 +269,59 @@ int w4a16_decoder_layer(const w4a16_layer_weights *w, void *h, int M, int P, con
                         const float *cos_table, const float *sin_table, int n_pos, const uint8_t *mask,
                         void *k_cache, void *v_cache, const w4a16_layer_scratch *s, void *stream);
 
+/* rope_append with a root-mean-square norm of every query and key head ahead of the rotation, in the same pass (target models
+ * that norm queries and keys per head):
+ *   x[d] <- x[d] * gamma[d] / sqrt(mean_d(x^2) + eps) for each query head (q_gamma) and key head (k_gamma), then rope_append's
+ *   rotation; values are appended as they are.  fp32 arithmetic, one rounding to fp16, after the rotation.
+ * q_gamma, k_gamma fp16 [D], eps >= 0; all else as rope_append, except that D % 8 == 0, D <= 512 and 16-byte-aligned tables
+ * are required.  A row whose position lies outside [0, n_pos) gets its values appended but its q and k rows are left untouched. */
+int rope_append_qk_norm(const void *qkv, const void *q_gamma, const void *k_gamma, float eps, const int32_t *pos, const float *cos_table,
+                        const float *sin_table, int n_pos, void *q, void *k_cache, void *v_cache, int M, int P, int Hq, int Hkv, int D,
+                        void *stream);
+
+/* An attention cache of 8 bits per value: half the bytes that a long prefix costs every decode step (paper section 2.1: decoding
+ * is bound by memory).  It consists of
+ *   k, v              codes, 8 bits each, [rows, Hkv, D]
+ *   k_scale, v_scale  fp16 [rows, Hkv]: one scale per cached row and head
+ * in one of two formats, chosen by the caller and passed to every call:
+ *   W4A16_KV8_INT8  code a signed integer within +-127; scale = max|x| / 127 rounded up to four significant bits (a multiple of
+ *                   2^-24, at least that, at most 512); code = x / scale rounded to the nearest (ties to even), saturating
+ *   W4A16_KV8_E4M3  code an e4m3 number (four exponent bits, three mantissa bits, bias 7, no infinities); scale = max|x| / 448 rounded
+ *                   up to a power of two, at least 2^-15; code = x / scale rounded to the nearest (ties to even), saturating at
+ *                   +-448, at +-240 where the scale is 256
+ * Code times scale always is an fp16 number, the value the cache stands for.  A head with an infinity or a NaN in it gets codes 0 and
+ * scale NaN: all its values are NaN. */
+#define W4A16_KV8_INT8 1
+#define W4A16_KV8_E4M3 2
+
+/* rope_append (q_gamma and k_gamma NULL) or rope_append_qk_norm into an 8-bit cache: rows P..P+M-1 receive the codes and scales of
+ * the rotated keys -- rounded to fp16 first, so they are what rope_append would have appended -- and of the values.  q is the q of those
+ * calls, bit for bit.  All pointers 16-byte aligned but pos (4); D % 8 == 0, D <= 512.  Rows whose position lies outside [0, n_pos) as there. */
+int rope_append_kv8(const void *qkv, const void *q_gamma, const void *k_gamma, float eps, const int32_t *pos, const float *cos_table,
+               const float *sin_table, int n_pos, void *q, void *k, void *v, void *k_scale, void *v_scale, int format, int M, int P, int Hq,
+               int Hkv, int D, void *stream);
+
+/* The values of rows first .. first + rows - 1 of an 8-bit cache: k_out, v_out fp16 [rows, Hkv, D].  Exact.  rows == 0 does nothing.
+ * D % 8 == 0, D <= 512. */
+int w4a16_kv8_read(const void *k, const void *v, const void *k_scale, const void *v_scale, int format, int first, int rows, int Hkv, int D, void *k_out,
+             void *v_out, void *stream);
+
+/* Scratch needed by tree_verify_attn_kv8 for these sizes; the size for the largest M and P serves every smaller call of the same heads. */
+size_t tree_verify_attn_kv8_workspace_bytes(int M, int P, int Hq, int Hkv, int D);
+
+/* tree_verify_attn over an 8-bit cache of P + M rows: the attention over the values that w4a16_kv8_read returns.  Probabilities are rounded
+ * to fp16 for the product with the values; softmax, sums and accumulation are fp32.  A row whose mask row is empty and P == 0, or
+ * that sees no key for any other reason, gets zeros.  What a mask hides may be anything, NaN scales and codes included; a row that sees
+ * a key or value of scale NaN is NaN.  P <= 2^30; otherwise arguments, sizes and errors as tree_verify_attn, and `workspace` must
+ * hold tree_verify_attn_kv8_workspace_bytes and have been initialised with w4a16_workspace_init (W4A16_EWORKSPACE otherwise). */
+int tree_verify_attn_kv8(const void *q, const void *k, const void *v, const void *k_scale, const void *v_scale, int format, const uint8_t *mask,
+                         void *out, int M, int P, int Hq, int Hkv, int D, float scale, void *workspace, size_t workspace_bytes, void *stream);
+
+/* tree_accept on an 8-bit cache: the same walk, path and result; cache row P + j receives codes and scales of row P + path[j].  The cache
+ * must be given; D % 8 == 0, D <= 512.  Works for either format. */
+int tree_accept_kv8(const int32_t *parent, const int32_t *token, const int32_t *target, int M, int32_t *path, int32_t *result, void *k, void *v,
+                    void *k_scale, void *v_scale, int P, int Hkv, int D, void *stream);
+
 /* Size in bytes of the packed LM-head weight for a V-token vocabulary and hidden size K (the
  * vocabulary is padded to a multiple of 16 inside the buffer).  0 if the shape is not supported. */
 size_t lm_head_packed_bytes(int V, int K);

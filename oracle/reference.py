@@ -308,3 +308,104 @@ def lm_head_topk(x, W, top_k: int):
         idx[m] = order[:top_k]
     lp = np.take_along_axis(logits, idx, axis=1) - lse[:, None]
     return logits, idx, lp
+
+
+# ---------------------------------------------------------------------------------------------
+# head norms ahead of the rotation, and the 8-bit attention cache
+
+
+def rope_append_qk_norm(qkv, q_gamma, k_gamma, eps: float, pos, cos, sin, k_cache, v_cache, P: int, Hq: int, Hkv: int, D: int):
+    """rope_append with every query and key head x replaced by x * gamma / sqrt(mean(x^2) + eps) first.  fp64; returns
+    (q, k_cache, v_cache) like rope_append, unrounded (float64 arrays)."""
+    x = np.array(qkv, dtype=np.float64).reshape(len(pos), Hq + 2 * Hkv, D)
+    for first, last, gamma in ((0, Hq, q_gamma), (Hq, Hq + Hkv, k_gamma)):
+        part = x[:, first:last]
+        x[:, first:last] = part / np.sqrt((part * part).mean(-1, keepdims=True) + eps) * np.asarray(gamma, dtype=np.float64)
+    half = D // 2
+    c, s = (np.asarray(t, dtype=np.float64)[np.asarray(pos)][:, None, :] for t in (cos, sin))
+    a, b = x[:, :Hq + Hkv, :half].copy(), x[:, :Hq + Hkv, half:].copy()
+    x[:, :Hq + Hkv, :half] = a * c - b * s
+    x[:, :Hq + Hkv, half:] = b * c + a * s
+    k2, v2 = np.array(k_cache, dtype=np.float64), np.array(v_cache, dtype=np.float64)
+    k2[P:P + len(pos)] = x[:, Hq:Hq + Hkv]
+    v2[P:P + len(pos)] = x[:, Hq + Hkv:]
+    return x[:, :Hq], k2, v2
+
+
+INT8, E4M3 = 1, 2
+
+
+def e4m3_table():
+    """the numbers of the 256 e4m3 codes (sign, four exponent bits of bias 7, three mantissa bits; 0x7F and 0xFF are NaN)"""
+    out = np.empty(256)
+    for code in range(256):
+        e, m = (code >> 3) & 15, code & 7
+        mag = np.nan if code & 0x7F == 0x7F else (8 + m) * 2.0 ** (e - 10) if e else m * 2.0 ** -9
+        out[code] = -mag if code & 0x80 else mag
+    return out
+
+
+def _nearest_e4m3(y):
+    """codes of the e4m3 numbers nearest to y (|y| <= 448), ties to the even mantissa; zeros keep their sign"""
+    grid = e4m3_table()[:0x7F]                       # 0 .. 448, increasing
+    mag = np.abs(y)
+    hi = np.clip(np.searchsorted(grid, mag, side="left"), 1, 0x7E)
+    lo = hi - 1
+    below, above = mag - grid[lo], grid[hi] - mag     # exact: the operands are short
+    code = np.where(below < above, lo, np.where(above < below, hi, np.where(lo % 2 == 0, lo, hi)))
+    return (code | np.where(np.signbit(y), 0x80, 0)).astype(np.uint8)
+
+
+def kv8_quantise(x, fmt: int):
+    """codes uint8 [..., D] (int8 codes as their bytes) and scales fp16 [...] of fp16 x [..., D], by the definition of the format.
+    The scale is found in whole numbers of 2^-24, of which every fp16 number is one."""
+    x = np.asarray(x, dtype=np.float16)
+    codes, scales = np.zeros(x.shape, dtype=np.uint8), np.full(x.shape[:-1], np.nan, dtype=np.float16)
+    for at in np.ndindex(*x.shape[:-1]):
+        row = x[at].astype(np.float64)
+        if not np.isfinite(row).all():
+            continue                                  # codes 0, scale NaN
+        units = int(np.abs(row).max() * 2.0 ** 24)
+        if fmt == INT8:
+            want = -(-units // 127)                   # ceil
+            shift = max(0, want.bit_length() - 4)
+            want = -(-units // (127 << shift)) << shift
+            if want.bit_length() > shift + 4:         # 15.x rounded up to 16: one bit more
+                want = -(-units // (127 << (shift + 1))) << (shift + 1)
+            s = min(max(want, 1) * 2.0 ** -24, 512.0)
+            codes[at] = np.clip(np.rint(row / s), -127, 127).astype(np.int8).view(np.uint8)
+        else:
+            s = 2.0 ** -15
+            while s * 448 < units * 2.0 ** -24:
+                s *= 2
+            most = 240.0 if s == 256 else 448.0
+            codes[at] = _nearest_e4m3(np.clip(row / s, -most, most))
+        scales[at] = s
+    return codes, scales
+
+
+def kv8_values(codes, scales, fmt: int):
+    """float64 values of codes and scales"""
+    numbers = np.asarray(codes).view(np.int8).astype(np.float64) if fmt == INT8 else e4m3_table()[np.asarray(codes)]
+    return numbers * np.asarray(scales, dtype=np.float64)[..., None]
+
+
+def tree_verify_attn_seen(q, k, v, mask, scale: float):
+    """tree_verify_attn for masks that may leave a row nothing to see (zeros) and caches whose hidden rows may hold anything.
+    Returns (out, spread) in float64, spread = sum_j p_j |v_j| (what the rounding of the probabilities acts on)."""
+    q, k, v = (np.asarray(t, dtype=np.float64) for t in (q, k, v))
+    M, Hq, D = q.shape
+    T, Hkv, _ = k.shape
+    P = T - M
+    out, spread = np.zeros((M, Hq, D)), np.zeros((M, Hq, D))
+    for i in range(M):
+        seen = np.flatnonzero(np.concatenate([np.ones(P, dtype=bool), np.asarray(mask)[i] != 0]))
+        for g in range(Hkv if len(seen) else 0):
+            heads = slice(g * (Hq // Hkv), (g + 1) * (Hq // Hkv))
+            with np.errstate(invalid="ignore"):
+                logits = scale * (q[i, heads] @ k[seen, g].T)
+                p = np.exp(logits - logits.max(-1, keepdims=True))
+                p /= p.sum(-1, keepdims=True)
+                out[i, heads] = p @ v[seen, g]
+                spread[i, heads] = p @ np.abs(v[seen, g])
+    return out, spread

@@ -18,11 +18,13 @@ EXPORTS = (
     "w4a16_gemm", "w4a16_gemm_fused", "w4a16_gemm_rope", "w4a16_pack_heads", "w4a16_pack_gate_up", "w4a16_read_probe", "tree_verify_attn_workspace_bytes",
     "tree_verify_attn", "tree_accept", "rms_norm", "rope_append", "lm_head_workspace_bytes", "lm_head_topk",
     "lm_head_packed_bytes", "lm_head_pack", "w4a16_decoder_layer", "w4a16_plan_describe", "w4a16_gemm_static", "w4a16_weight_is_symmetric",
-    "tree_verify_attn_plan_describe", "lm_head_plan_describe",
+    "tree_verify_attn_plan_describe", "lm_head_plan_describe", "rope_append_qk_norm", "rope_append_kv8", "w4a16_kv8_read", "tree_accept_kv8",
+    "tree_verify_attn_kv8", "tree_verify_attn_kv8_workspace_bytes",
 )
 
 EPI_NONE, EPI_RESIDUAL, EPI_SILU_MUL = 0, 1, 2
 SYMMETRIC = 0x100   # OR-ed into an epilogue code: every zero-point of the weight is 8
+KV8_INT8, KV8_E4M3 = 1, 2   # formats of an 8-bit attention cache
 
 _lib = None
 
@@ -86,6 +88,13 @@ def load() -> ctypes.CDLL:
     L.w4a16_gemm_rope.argtypes = [vp, vp, i, i, i, vp, vp, vp, i, vp, vp, vp, i, i, i, i, vp, sz, vp]
     L.rms_norm.argtypes = [vp, vp, vp, i, i, ctypes.c_float, vp]
     L.rope_append.argtypes = [vp, vp, vp, vp, i, vp, vp, vp, i, i, i, i, i, vp]
+    L.rope_append_qk_norm.argtypes = [vp, vp, vp, ctypes.c_float, vp, vp, vp, i, vp, vp, vp, i, i, i, i, i, vp]
+    L.rope_append_kv8.argtypes = [vp, vp, vp, ctypes.c_float, vp, vp, vp, i, vp, vp, vp, vp, vp, i, i, i, i, i, i, vp]
+    L.w4a16_kv8_read.argtypes = [vp, vp, vp, vp, i, i, i, i, i, vp, vp, vp]
+    L.tree_verify_attn_kv8_workspace_bytes.restype = sz
+    L.tree_verify_attn_kv8_workspace_bytes.argtypes = [i, i, i, i, i]
+    L.tree_verify_attn_kv8.argtypes = [vp, vp, vp, vp, vp, i, vp, vp, i, i, i, i, i, ctypes.c_float, vp, sz, vp]
+    L.tree_accept_kv8.argtypes = [vp, vp, vp, i, vp, vp, vp, vp, vp, vp, i, i, i, vp]
     L.w4a16_decoder_layer.argtypes = [ctypes.POINTER(LayerWeights), vp, i, i, vp, vp, vp, i, vp, vp, vp,
                                       ctypes.POINTER(LayerScratch), vp]
     L.lm_head_packed_bytes.restype = sz
@@ -319,6 +328,62 @@ def tree_verify_attn(q, k, v, mask, out, M: int, P: int, Hq: int, Hkv: int, D: i
 def tree_accept(parent, token, target, M: int, path, result, k=None, v=None, P: int = 0, Hkv: int = 0, D: int = 0) -> None:
     _check(load().tree_accept(_ptr(parent), _ptr(token), _ptr(target), M, _ptr(path), _ptr(result), _ptr(k), _ptr(v),
                               P, Hkv, D, _stream()), "tree_accept")
+
+
+def rope_append_qk_norm(qkv, q_gamma, k_gamma, eps: float, pos, cos_table, sin_table, n_pos: int, q, k_cache, v_cache, M: int, P: int,
+                        Hq: int, Hkv: int, D: int) -> None:
+    _init_cuda()
+    rc = (_lib or load()).rope_append_qk_norm(
+        0 if qkv is None else qkv.data_ptr(), 0 if q_gamma is None else q_gamma.data_ptr(), 0 if k_gamma is None else k_gamma.data_ptr(), eps,
+        0 if pos is None else pos.data_ptr(), 0 if cos_table is None else cos_table.data_ptr(), 0 if sin_table is None else sin_table.data_ptr(),
+        n_pos, 0 if q is None else q.data_ptr(), 0 if k_cache is None else k_cache.data_ptr(), 0 if v_cache is None else v_cache.data_ptr(),
+        M, P, Hq, Hkv, D, _raw_stream(_current_device()))
+    if rc:
+        _check(rc, "rope_append_qk_norm")
+
+
+def rope_append_kv8(qkv, q_gamma, k_gamma, eps: float, pos, cos_table, sin_table, n_pos: int, q, k, v, k_scale, v_scale, fmt: int, M: int, P: int,
+               Hq: int, Hkv: int, D: int) -> None:
+    _init_cuda()
+    rc = (_lib or load()).rope_append_kv8(
+        0 if qkv is None else qkv.data_ptr(), 0 if q_gamma is None else q_gamma.data_ptr(), 0 if k_gamma is None else k_gamma.data_ptr(), eps,
+        0 if pos is None else pos.data_ptr(), 0 if cos_table is None else cos_table.data_ptr(), 0 if sin_table is None else sin_table.data_ptr(),
+        n_pos, 0 if q is None else q.data_ptr(), 0 if k is None else k.data_ptr(), 0 if v is None else v.data_ptr(),
+        0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr(), fmt, M, P, Hq, Hkv, D,
+        _raw_stream(_current_device()))
+    if rc:
+        _check(rc, "rope_append_kv8")
+
+
+def w4a16_kv8_read(k, v, k_scale, v_scale, fmt: int, first: int, rows: int, Hkv: int, D: int, k_out, v_out) -> None:
+    _init_cuda()
+    rc = (_lib or load()).w4a16_kv8_read(
+        0 if k is None else k.data_ptr(), 0 if v is None else v.data_ptr(), 0 if k_scale is None else k_scale.data_ptr(),
+        0 if v_scale is None else v_scale.data_ptr(), fmt, first, rows, Hkv, D, 0 if k_out is None else k_out.data_ptr(),
+        0 if v_out is None else v_out.data_ptr(), _raw_stream(_current_device()))
+    if rc:
+        _check(rc, "w4a16_kv8_read")
+
+
+def tree_verify_attn_kv8_workspace_bytes(M: int, P: int, Hq: int, Hkv: int, D: int) -> int:
+    return load().tree_verify_attn_kv8_workspace_bytes(M, P, Hq, Hkv, D)
+
+
+def tree_verify_attn_kv8(q, k, v, k_scale, v_scale, fmt: int, mask, out, M: int, P: int, Hq: int, Hkv: int, D: int, scale: float,
+                         workspace) -> None:
+    _init_cuda()
+    rc = (_lib or load()).tree_verify_attn_kv8(
+        0 if q is None else q.data_ptr(), 0 if k is None else k.data_ptr(), 0 if v is None else v.data_ptr(),
+        0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr(), fmt, 0 if mask is None else mask.data_ptr(),
+        0 if out is None else out.data_ptr(), M, P, Hq, Hkv, D, float(scale), 0 if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _raw_stream(_current_device()))
+    if rc:
+        _check(rc, "tree_verify_attn_kv8")
+
+
+def tree_accept_kv8(parent, token, target, M: int, path, result, k, v, k_scale, v_scale, P: int, Hkv: int, D: int) -> None:
+    _check(load().tree_accept_kv8(_ptr(parent), _ptr(token), _ptr(target), M, _ptr(path), _ptr(result), _ptr(k), _ptr(v), _ptr(k_scale),
+                                  _ptr(v_scale), P, Hkv, D, _stream()), "tree_accept_kv8")
 
 
 # ---- conveniences for tests and the benchmark (still marshalling only) ----

@@ -1,0 +1,235 @@
+"""GPU: tree_verify_attn_kv8 through the C ABI against the fp64 oracle over the values of the cache.
+
+Tolerance per output, derived: probabilities are rounded to fp16 (2^-11 of each, 2^-25 below 2^-14; 128-row sums of products in fp32 stay far below
+that), a score errs by the fp32 sum of 128 products, at most 128 2^-24 sum |q k| times the scale, which moves each weight by that
+share, and twice so with the normalisation; the output is rounded once (2^-11 of it)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import reference as R
+from paper_2505_22179_amd import binding as B
+from paper_2505_22179_amd import inputs as I
+
+pytestmark = pytest.mark.gpu
+DEV, D = "cuda", 128
+dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+FORMATS = [B.KV8_INT8, B.KV8_E4M3]
+
+
+class Call:
+    def __init__(self, seed, M, P, Hq, Hkv, fmt, tree="random", q_std=1.0, v_std=1.0, scale=None):
+        rng = np.random.default_rng(seed)
+        self.M, self.P, self.Hq, self.Hkv, self.fmt = M, P, Hq, Hkv, fmt
+        self.scale = scale or D ** -0.5
+        self.q = (rng.standard_normal((M, Hq, D)) * q_std).astype(np.float16)
+        T = P + M
+        if fmt == B.KV8_INT8:
+            codes = lambda: np.clip(np.rint(rng.standard_normal((T, Hkv, D)) * 40), -127, 127).astype(np.int8).view(np.uint8)
+            scales = lambda std: (rng.integers(8, 16, (T, Hkv)) * 2.0 ** (-9 + rng.integers(0, 3, (T, Hkv))) * std).astype(np.float16)
+        else:
+            codes = lambda: R._nearest_e4m3(np.clip(rng.standard_normal((T, Hkv, D)) * 100, -448, 448))
+            scales = lambda std: (2.0 ** (-8 + rng.integers(0, 3, (T, Hkv))) * std).astype(np.float16)
+        self.k, self.ks, self.v, self.vs = codes(), scales(1.0), codes(), scales(v_std)
+        if tree == "random" and M > 1:
+            self.mask = I.make_tree(seed + 1, M, min(6, M - 1), 4)[2]
+        else:
+            self.mask = I.chain_tree(M)[2] if tree == "chain" or M == 1 else np.eye(M, dtype=np.uint8)
+
+    def tensors(self):
+        return [dev(t) for t in (self.q, self.k, self.v, self.ks, self.vs)] + [self.fmt, dev(self.mask)]
+
+    def sizes(self):
+        return self.M, self.P, self.Hq, self.Hkv, D, self.scale
+
+    def workspace(self):
+        return B.new_workspace(B.tree_verify_attn_kv8_workspace_bytes(self.M, self.P, self.Hq, self.Hkv, D))
+
+    def run(self, ws=None):
+        out = torch.full((self.M + 1, self.Hq, D), 77.0, dtype=torch.float16, device=DEV)
+        B.tree_verify_attn_kv8(*self.tensors(), out, *self.sizes(), self.workspace() if ws is None else ws)
+        torch.cuda.synchronize()
+        o = out.cpu().numpy()
+        assert (o[self.M:] == 77).all()
+        return o[:self.M]
+
+    def check(self, out16):
+        k, v = R.kv8_values(self.k, self.ks, self.fmt), R.kv8_values(self.v, self.vs, self.fmt)
+        want, spread = R.tree_verify_attn_seen(self.q, k, v, self.mask, self.scale)
+        np.testing.assert_array_equal(np.isnan(out16), np.isnan(want))
+        rep = self.Hq // self.Hkv
+        with np.errstate(invalid="ignore"):
+            qk = np.nanmax(np.abs(self.q.astype(np.float64)).sum(-1)) * np.nanmax(np.abs(k)) * self.scale   # above every sum |q k| scale
+            score = 2 * 128 * 2.0 ** -24 * min(qk, 64.0 * 8)
+            vmax = np.nanmax(np.abs(v), axis=(0, 2)).repeat(rep)[None, :, None]
+            tol = spread * (2.0 ** -11 * 1.01 + score) + np.abs(want) * 2.0 ** -11 + 2.0 ** -25 + (self.P + self.M) * 2.0 ** -25 * vmax / max(1.0, (self.P + self.M) ** 0.5)
+            err = np.abs(out16.astype(np.float64) - want)
+        worst = np.nanmax(err / tol)
+        assert worst <= 1, f"worst error {worst:.3g} of the tolerance"
+        fine = ~np.isnan(want)
+        rel = np.linalg.norm((out16 - want)[fine]) / max(np.linalg.norm(want[fine]), 1e-30)
+        assert rel <= 2.0 ** -10, rel
+        return rel
+
+
+CASES = [
+    # M, P, Hq, Hkv, tree
+    (1, 2048, 64, 8, "chain"),       # plain decoding
+    (1, 0, 8, 1, "chain"),           # a single key
+    (1, 30, 8, 8, "chain"),          # 31 keys: one short of a step
+    (1, 31, 8, 8, "chain"),          # exactly one step
+    (1, 32, 7, 1, "chain"),
+    (7, 2048, 32, 8, "chain"),       # sequence verification
+    (60, 2048, 64, 8, "random"),     # tree verification
+    (64, 100, 8, 8, "random"),
+    (64, 64, 64, 8, "random"),       # 512 rows per KV head
+    (17, 0, 16, 4, "random"),        # no prefix
+    (33, 31, 8, 2, "identity"),
+    (48, 5, 4, 1, "random"),
+    (3, 2, 12, 2, "chain"),          # fewer keys than one step
+    (12, 300, 32, 4, "random"),
+    (37, 1333, 28, 4, "random"),     # groups of seven
+    (5, 70, 40, 8, "random"),        # groups of five
+    (8, 10001, 16, 2, "random"),     # many steps per range, ragged end
+    (40, 5000, 8, 1, "random"),      # one KV head: 320 rows over a long prefix
+]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,P,Hq,Hkv,tree", CASES)
+def test_parity(M, P, Hq, Hkv, tree, fmt):
+    print(f"attn_kv8 parity M={M} P={P} Hq={Hq} Hkv={Hkv} {tree} fmt={fmt}", flush=True)
+    c = Call(3000 + M + P + Hq, M, P, Hq, Hkv, fmt, tree)
+    out = c.run()
+    c.check(out)
+    np.testing.assert_array_equal(c.run().view(np.uint16), out.view(np.uint16))   # the same bits again
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("v_std", [2.0 ** -6, 16.0])
+def test_values_of_any_size(fmt, v_std):
+    """scales near both ends: codes times scale stay fp16 numbers, nothing under- or overflows on the way"""
+    c = Call(11, 9, 700, 16, 4, fmt, v_std=v_std)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_sharp_softmax(fmt):
+    """large scores: a few keys carry everything, running maxima move from step to step"""
+    c = Call(12, 20, 3000, 16, 4, fmt, q_std=6.0)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,P,Hq,Hkv", [(9, 0, 16, 4), (37, 250, 28, 4), (64, 33, 64, 8), (60, 0, 8, 1)])
+def test_rows_that_see_nothing_and_hidden_rows_that_hold_anything(M, P, Hq, Hkv, fmt):
+    """a tree padded to a fixed size: the last rows are no nodes -- with no prefix they see nothing -- and their cache rows were never written"""
+    print(f"attn_kv8 padded M={M} P={P} Hq={Hq} Hkv={Hkv} fmt={fmt}", flush=True)
+    c = Call(50 + M, M, P, Hq, Hkv, fmt)
+    n = M - M // 3
+    c.mask[n:], c.mask[:, n:] = 0, 0
+    clean = c.run()
+    c.check(clean)
+    assert P or (clean[n:] == 0).all()
+    rng = np.random.default_rng(M)
+    for codes, scales in ((c.k, c.ks), (c.v, c.vs)):
+        codes[P + n:] = rng.choice(np.array([0x7F, 0xFF, 0x80, 0x7E], dtype=np.uint8), codes[P + n:].shape)
+        scales[P + n:] = rng.choice(np.array([np.nan, np.inf, -np.inf, 65504.0, 1.0], dtype=np.float16), scales[P + n:].shape)
+    np.testing.assert_array_equal(c.run().view(np.uint16), clean.view(np.uint16))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("at", [3, 70, 100])
+def test_a_nan_key_or_value_reaches_the_rows_that_see_it_and_no_others(at, fmt):
+    """NaN scales: at a committed row all query rows see it; at a draft row only its descendants"""
+    M, P = 12, 96
+    for which in ("ks", "vs"):
+        c = Call(60 + at, M, P, 8, 2, fmt, tree="random")
+        getattr(c, which)[at, 1] = np.nan
+        getattr(c, which[0])[at, 1] = 0     # as rope_append_kv8 writes it
+        out = c.run()
+        c.check(out)
+        assert not np.isnan(out[:, :4]).any() and np.isnan(out[:, 4:]).any()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_infinite_and_nan_queries_stay_in_their_rows(fmt):
+    c = Call(61, 10, 200, 8, 2, fmt)
+    clean = c.run()
+    c.q[4, 3, 7], c.q[6, 5, 0] = np.nan, np.inf
+    out = c.run()
+    assert np.isnan(out[4, 3]).all() and np.isnan(out[6, 5]).all()
+    out[4, 3], out[6, 5] = clean[4, 3], clean[6, 5]
+    np.testing.assert_array_equal(out.view(np.uint16), clean.view(np.uint16))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_equal_to_the_fp16_attention_over_the_cache_read_back(fmt):
+    c = Call(62, 24, 1500, 32, 8, fmt)
+    q, k, v, ks, vs, _, mask = c.tensors()
+    k16, v16 = torch.empty(c.P + c.M, 8, D, dtype=torch.float16, device=DEV), torch.empty(c.P + c.M, 8, D, dtype=torch.float16, device=DEV)
+    B.w4a16_kv8_read(k, v, ks, vs, fmt, 0, c.P + c.M, 8, D, k16, v16)
+    want = torch.empty_like(q)
+    B.tree_verify_attn(q, k16, v16, mask, want, *c.sizes(), B.new_workspace(B.tree_verify_attn_workspace_bytes(c.M, c.P, 32, 8, D)))
+    torch.cuda.synchronize()
+    got, want = c.run().astype(np.float64), want.cpu().numpy().astype(np.float64)
+    assert np.linalg.norm(got - want) <= 2.0 ** -10 * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_workspace_shared_by_calls_in_a_row_and_another_stream(fmt):
+    """one workspace, calls of several sizes one after another, tickets back at zero; and the same on a stream that is not the default one"""
+    calls = [Call(70 + i, M, P, Hq, 8, fmt) for i, (M, P, Hq) in enumerate(((60, 900, 64), (1, 4000, 64), (24, 333, 32), (1, 5, 64)))]
+    want = [c.run() for c in calls]
+    ws = B.new_workspace(max(B.tree_verify_attn_kv8_workspace_bytes(c.M, c.P, c.Hq, 8, D) for c in calls))
+    for c, w in zip(calls, want):
+        np.testing.assert_array_equal(c.run(ws).view(np.uint16), w.view(np.uint16))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for c, w in zip(calls, want):
+            np.testing.assert_array_equal(c.run(ws).view(np.uint16), w.view(np.uint16))
+
+
+def test_graph_replays_equal_the_eager_calls():
+    """append, attention and acceptance of one step captured together, replayed with other work in between"""
+    M, P, Hq, Hkv, fmt = 24, 500, 32, 8, B.KV8_INT8
+    rng = np.random.default_rng(5)
+    qkv = dev(rng.standard_normal((M, (Hq + 2 * Hkv) * D)).astype(np.float16))
+    gq, gk = dev(I.make_gamma(1, D)), dev(I.make_gamma(2, D))
+    parent, _, mask = I.make_tree(3, M, 5, 3)
+    token, target = I.make_verify(4, parent, p_accept=0.9)
+    i32 = lambda a: dev(np.asarray(a, dtype=np.int32))
+    ids = [i32(parent), i32(token), i32(target)]
+    pos, maskd = dev(I.tree_positions(parent, P)), dev(mask)
+    cos, sin = (dev(t) for t in I.make_rope_tables(P + 16, D))
+    k0, v0 = (dev(rng.integers(0, 100, (P + M, Hkv, D), dtype=np.uint8)) for _ in range(2))
+    s0 = dev((2.0 ** rng.integers(-8, -4, (P + M, Hkv))).astype(np.float16))
+    k, v, ks, vs = k0.clone(), v0.clone(), s0.clone(), s0.clone()
+    q, out = torch.empty(M, Hq, D, dtype=torch.float16, device=DEV), torch.empty(M, Hq, D, dtype=torch.float16, device=DEV)
+    path, result = torch.empty(M, dtype=torch.int32, device=DEV), torch.empty(2, dtype=torch.int32, device=DEV)
+    ws = B.new_workspace(B.tree_verify_attn_kv8_workspace_bytes(64, 4000, 64, 8, D))
+
+    def reset():
+        k.copy_(k0), v.copy_(v0), ks.copy_(s0), vs.copy_(s0)
+
+    def step():
+        B.rope_append_kv8(qkv, gq, gk, 1e-6, pos, cos, sin, P + 16, q, k, v, ks, vs, fmt, M, P, Hq, Hkv, D)
+        B.tree_verify_attn_kv8(q, k, v, ks, vs, fmt, maskd, out, M, P, Hq, Hkv, D, D ** -0.5, ws)
+        B.tree_accept_kv8(*ids, M, path, result, k, v, ks, vs, P, Hkv, D)
+
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (q, out, path, result, k, v, ks, vs)]
+    graph = torch.cuda.CUDAGraph()
+    reset()
+    with torch.cuda.graph(graph):
+        step()
+    other = Call(90, 60, 2000, 64, 8, B.KV8_E4M3)
+    for replay in range(4):
+        reset(), q.zero_(), out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, w in zip((q, out, path, result, k, v, ks, vs), want):
+            assert torch.equal(got, w), replay
+        other.run(ws)
