@@ -354,6 +354,30 @@ size_t lm_head_workspace_bytes(int M, int V, int K, int top_k);
 int lm_head_topk(const void *x, const void *packed, int M, int V, int K, int top_k, float *logits, int32_t *top_idx,
                  float *top_logprob, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Scratch of lm_head_sample for these sizes; the size for the largest M and V serves every smaller call. */
+size_t lm_head_sample_workspace_bytes(int M, int V);
+
+/* One token per row from the logits that lm_head_topk wrote (or any others) and given uniform numbers: drafting and verifying with
+ * a temperature, where tree_accept's tokens are greedy.  Row m: tokens in the order of falling logits, equal logits by token index;
+ *   weight    w = exp((logit - largest logit) / temperature[m])
+ *   top_k     the first top_k[m] tokens stay
+ *   top_p     of those, a token stays while the weight before it is below top_p[m] times the weight of them all
+ *   min_p     of those, a token stays if w >= min_p[m], i.e. its probability is min_p of the largest one's
+ * The first token always stays.  Of the tokens that stay, in the order of their indices, token[m] is the first whose cumulative weight exceeds
+ * uniform[m] times their sum, and prob[m] its share of that sum.
+ *   logits       fp32 [M, V], 16-byte aligned; 1 <= M <= 64, 1 <= V <= 262144
+ *   temperature  fp32 [M]; not above 0, or NaN: the largest logit's first token, prob 1.  NULL: 1
+ *   top_k        int32 [M]; below 1 or above V: no limit.  NULL: none
+ *   top_p        fp32 [M]; 1 and above, or NaN: no limit; 0 and below: the first token only.  NULL: none
+ *   min_p        fp32 [M]; 0 and below, or NaN: no limit; above 1: the first token only.  NULL: none
+ *   uniform      fp32 [M], in [0, 1); what lies below (or is NaN) counts as 0, what lies above as the largest number below 1
+ *   token int32 [M], prob fp32 [M]: out; all [M] arrays 4-byte aligned
+ * Weights and sums are fp64 or exact whole numbers of 2^-44, so a token depends on nothing but its row; tokens more than e^31 below the row's
+ * largest weigh nothing.  A logit of -inf or NaN is no token; +inf shares the row with its equals; a row with no token at all gives token
+ * 0x7FFFFFFF and prob 0.  `workspace` holds lm_head_sample_workspace_bytes(M, V) bytes and has been initialised with w4a16_workspace_init. */
+int lm_head_sample(const float *logits, int M, int V, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                   const float *uniform, int32_t *token, float *prob, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------------------------------------------
  * Measurement and ablation aids.  Not part of the method's interface: nothing above needs them, a
  * deployment never calls them.  They exist so that the benchmark and the tests can force a kernel

@@ -30,6 +30,7 @@ by the paper and this oracle is the definition.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import numpy as np
@@ -409,3 +410,45 @@ def tree_verify_attn_seen(q, k, v, mask, scale: float):
                 out[i, heads] = p @ v[seen, g]
                 spread[i, heads] = p @ np.abs(v[seen, g])
     return out, spread
+
+
+# ---------------------------------------------------------------------------------------------
+# sampling from the logits of a language-model head
+
+
+def sample(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, u=0.0):
+    """One row.  Returns (token, probability, margin): the token and its share of the kept weight, by the definition in include/w4a16.h, and
+    how near a border decided -- the smallest distance, as a share of the row's weight, between u or top_p and a cumulative weight next to it, or
+    between min_p and a weight.  Plain Python over the tokens in order."""
+    x = [float(v) for v in logits]
+    order = sorted((v for v in range(len(x)) if x[v] > -math.inf), key=lambda v: (-x[v], v))   # NaN compares false
+    if not order:
+        return 0x7FFFFFFF, 0.0, 1.0
+    top = x[order[0]]
+    if not temperature > 0 or top_p <= 0 or min_p > 1:
+        return order[0], 1.0, 1.0
+    weight = lambda v: 1.0 if x[v] == top else 0.0 if math.isinf(top) else math.exp((x[v] - top) / temperature)
+    if 0 < top_k < len(order):
+        order = order[:top_k]
+    w = {v: weight(v) for v in order}
+    margin, total = 1.0, math.fsum(w.values())
+    if top_p < 1:
+        kept, before = [], 0.0
+        for v in order:
+            if kept and w[v] > 0:
+                margin = min(margin, abs(before / total - top_p))
+            if kept and not before < top_p * total:
+                break
+            kept.append(v)
+            before += w[v]
+        order = kept
+    if min_p > 0:
+        margin = min([margin] + [abs(w[v] - min_p) for v in order[1:]])
+        order = order[:1] + [v for v in order[1:] if w[v] >= min_p]
+    order = sorted(v for v in order if w[v] > 0)
+    total, upto = math.fsum(w[v] for v in order), 0.0
+    for v in order:
+        upto += w[v]
+        margin = min(margin, abs(upto / total - u)) if v != order[-1] else margin
+        if upto > u * total or v == order[-1]:
+            return v, w[v] / total, margin

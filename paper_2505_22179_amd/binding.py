@@ -19,7 +19,7 @@ EXPORTS = (
     "tree_verify_attn", "tree_accept", "rms_norm", "rope_append", "lm_head_workspace_bytes", "lm_head_topk",
     "lm_head_packed_bytes", "lm_head_pack", "w4a16_decoder_layer", "w4a16_plan_describe", "w4a16_gemm_static", "w4a16_weight_is_symmetric",
     "tree_verify_attn_plan_describe", "lm_head_plan_describe", "rope_append_qk_norm", "rope_append_kv8", "w4a16_kv8_read", "tree_accept_kv8",
-    "tree_verify_attn_kv8", "tree_verify_attn_kv8_workspace_bytes",
+    "tree_verify_attn_kv8", "tree_verify_attn_kv8_workspace_bytes", "lm_head_sample", "lm_head_sample_workspace_bytes",
 )
 
 EPI_NONE, EPI_RESIDUAL, EPI_SILU_MUL = 0, 1, 2
@@ -103,6 +103,9 @@ def load() -> ctypes.CDLL:
     L.lm_head_workspace_bytes.restype = sz
     L.lm_head_workspace_bytes.argtypes = [i, i, i, i]
     L.lm_head_plan_describe.argtypes = [i, i, i, ctypes.POINTER(ctypes.c_int)]
+    L.lm_head_sample_workspace_bytes.restype = sz
+    L.lm_head_sample_workspace_bytes.argtypes = [i, i]
+    L.lm_head_sample.argtypes = [vp, i, i, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.lm_head_topk.argtypes = [vp, vp, i, i, i, i, vp, vp, vp, vp, sz, vp]
     _lib = L
     return L
@@ -288,6 +291,22 @@ def lm_head_plan_describe(M: int, V: int, K: int) -> tuple:
     out = (ctypes.c_int * 3)()
     _check(load().lm_head_plan_describe(M, V, K, out), "lm_head_plan_describe")
     return tuple(out)
+
+
+def lm_head_sample_workspace_bytes(M: int, V: int) -> int:
+    return load().lm_head_sample_workspace_bytes(M, V)
+
+
+def lm_head_sample(logits, M: int, V: int, temperature, top_k, top_p, min_p, uniform, token, prob, workspace) -> None:
+    _init_cuda()
+    rc = (_lib or load()).lm_head_sample(
+        0 if logits is None else logits.data_ptr(), M, V, 0 if temperature is None else temperature.data_ptr(),
+        0 if top_k is None else top_k.data_ptr(), 0 if top_p is None else top_p.data_ptr(), 0 if min_p is None else min_p.data_ptr(),
+        0 if uniform is None else uniform.data_ptr(), 0 if token is None else token.data_ptr(), 0 if prob is None else prob.data_ptr(),
+        0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _raw_stream(_current_device()))
+    if rc:
+        _check(rc, "lm_head_sample")
 
 
 def w4a16_read_probe(buf, nbytes: int, sink) -> None:

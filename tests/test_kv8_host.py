@@ -89,3 +89,18 @@ def test_workspace_serves_every_smaller_call(Hq, Hkv):
     for M, P in sizes:
         assert 0 < B.tree_verify_attn_kv8_workspace_bytes(M, P, Hq, Hkv, 128) <= most
     assert B.tree_verify_attn_kv8_workspace_bytes(65, 10, Hq, Hkv, 128) == 0
+
+
+def test_lm_head_sample_refuses():
+    call = caller("lm_head_sample", logits=A, M=4, V=1000, temperature=A, top_k=A, top_p=A, min_p=A, uniform=A, token=A, prob=A, ws=A, bytes=1 << 30)
+    refusals(call, {
+        EINVAL: [dict(M=0), dict(V=0), dict(V=-1)],
+        EUNSUP: [dict(M=65), dict(V=262145)],
+        ENULL: [{n: None} for n in ("logits", "uniform", "token", "prob")],
+        EALIGN: [dict(logits=A + 4), dict(ws=A + 128)] + [{n: A + 2} for n in ("temperature", "top_k", "top_p", "min_p", "uniform", "token", "prob")],
+        EWS: [dict(ws=None), dict(bytes=B.lm_head_sample_workspace_bytes(4, 1000) - 1)],
+    })
+    assert B.lm_head_sample_workspace_bytes(65, 1000) == 0 and B.lm_head_sample_workspace_bytes(1, 262145) == 0
+    for M in (1, 7, 64):
+        for V in (1, 1000, 128256, 262144):
+            assert 0 < B.lm_head_sample_workspace_bytes(M, V) <= B.lm_head_sample_workspace_bytes(64, 262144)
