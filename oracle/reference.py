@@ -392,7 +392,8 @@ def kv8_values(codes, scales, fmt: int):
 
 
 def tree_verify_attn_seen(q, k, v, mask, scale: float):
-    """tree_verify_attn for masks that may leave a row nothing to see (zeros) and caches whose hidden rows may hold anything.
+    """tree_verify_attn for trees padded to a fixed size and caches whose hidden rows may hold anything: a row whose mask row is empty is
+    padding, sees nothing, committed keys included, and gets zeros.
     Returns (out, spread) in float64, spread = sum_j p_j |v_j| (what the rounding of the probabilities acts on)."""
     q, k, v = (np.asarray(t, dtype=np.float64) for t in (q, k, v))
     M, Hq, D = q.shape
@@ -400,8 +401,9 @@ def tree_verify_attn_seen(q, k, v, mask, scale: float):
     P = T - M
     out, spread = np.zeros((M, Hq, D)), np.zeros((M, Hq, D))
     for i in range(M):
-        seen = np.flatnonzero(np.concatenate([np.ones(P, dtype=bool), np.asarray(mask)[i] != 0]))
-        for g in range(Hkv if len(seen) else 0):
+        draft = np.asarray(mask)[i] != 0
+        seen = np.flatnonzero(np.concatenate([np.ones(P, dtype=bool), draft]))
+        for g in range(Hkv if draft.any() else 0):
             heads = slice(g * (Hq // Hkv), (g + 1) * (Hq // Hkv))
             with np.errstate(invalid="ignore"):
                 logits = scale * (q[i, heads] @ k[seen, g].T)

@@ -695,15 +695,6 @@ constexpr int kWaveEnd = kWaveWeights + kWaveRows * kSharedWaves * 8;
 constexpr int kWaveLds = kWaveQ + kWaveRows * kHeadDim * 2 > kWaveEnd ? kWaveQ + kWaveRows * kHeadDim * 2 : kWaveEnd;
 typedef float float2v __attribute__((ext_vector_type(2)));
 
-// the transposing read of four key rows at lds_addr + OFFSET and the four that lie eight rows further on
-template <int OFFSET>
-__device__ __forceinline__ void read_transposed_rows(short4v &lo, short4v &hi, uint32_t lds_addr)
-{
-    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\tds_read_b64_tr_b16 %1, %2 offset:%4"
-                 : "=&v"(lo), "=&v"(hi)
-                 : "v"(lds_addr), "n"(OFFSET), "n"(OFFSET + 8 * 256));
-}
-
 __global__ __launch_bounds__(64 * kSharedWaves) void tree_attn_wave_kernel(
     uint32_t by_tiles, uint32_t by_ranges, const _Float16 *__restrict__ q, const _Float16 *__restrict__ k, const _Float16 *__restrict__ v,
     const uint8_t *__restrict__ mask, _Float16 *__restrict__ out, float *__restrict__ part_o,

@@ -126,8 +126,8 @@ static uint32_t divider(int d) { return (uint32_t)(((1u << 31) + (unsigned)d - 1
 
 // Merge of the key ranges of one tile by the workgroup that finished last (fused mode): NS = compiled
 // upper bound of the number of ranges, IT = items a thread handles at once (all their loads are issued
-// together).  Loads are device-scope: other workgroups, on other XCDs, wrote the partials in this kernel.
-template <int NS, int IT>
+// together), PAD = rows that the partials of a range take.  Loads are device-scope: other workgroups, on other XCDs, wrote the partials in this kernel.
+template <int NS, int IT, int PAD>
 __device__ __forceinline__ void merge_ranges(PartialBuffer unit_o, PartialBuffer unit_ml, _Float16 *__restrict__ out,
                                              int tid, int threads, const RowTile &tile, int nsplit)
 {
@@ -146,9 +146,9 @@ __device__ __forceinline__ void merge_ranges(PartialBuffer unit_o, PartialBuffer
                 ls[it][s] = 0.f;
                 os[it][s] = (float4v){0.f, 0.f, 0.f, 0.f};
                 if (s < nsplit && idx < items) {
-                    ms[it][s] = load_partial_f32(unit_ml, (s * kRowsPad + trow) * 2);
-                    ls[it][s] = load_partial_f32(unit_ml, (s * kRowsPad + trow) * 2 + 1);
-                    os[it][s] = load_partial(unit_o, (s * kRowsPad + trow) * (kHeadDim / 4) + d4);
+                    ms[it][s] = load_partial_f32(unit_ml, (s * PAD + trow) * 2);
+                    ls[it][s] = load_partial_f32(unit_ml, (s * PAD + trow) * 2 + 1);
+                    os[it][s] = load_partial(unit_o, (s * PAD + trow) * (kHeadDim / 4) + d4);
                 }
             }
         }
@@ -178,13 +178,14 @@ __device__ __forceinline__ void merge_ranges(PartialBuffer unit_o, PartialBuffer
     }
 }
 
+template <int PAD = kRowsPad>
 __device__ __forceinline__ void merge_tile(PartialBuffer unit_o, PartialBuffer unit_ml, _Float16 *__restrict__ out, int tid,
                                            int threads, const RowTile &tile, int nsplit)
 {
-    if (nsplit <= 4) merge_ranges<4, 4>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
-    else if (nsplit <= 8) merge_ranges<8, 2>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
-    else if (nsplit <= 16) merge_ranges<16, 1>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
-    else merge_ranges<kMaxRanges, 1>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
+    if (nsplit <= 4) merge_ranges<4, 4, PAD>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
+    else if (nsplit <= 8) merge_ranges<8, 2, PAD>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
+    else if (nsplit <= 16) merge_ranges<16, 1, PAD>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
+    else merge_ranges<kMaxRanges, 1, PAD>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
 }
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -215,6 +216,15 @@ static void even_tiles(int pairs, int most, int &tile_rows, int &tiles_per_kv)
     const int n = (pairs + most - 1) / most;
     tile_rows = (pairs + n - 1) / n;
     tiles_per_kv = (pairs + tile_rows - 1) / tile_rows;
+}
+
+// the transposing read of four key rows at lds_addr + OFFSET and the four that lie eight rows further on
+template <int OFFSET>
+__device__ __forceinline__ void read_transposed_rows(short4v &lo, short4v &hi, uint32_t lds_addr)
+{
+    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\tds_read_b64_tr_b16 %1, %2 offset:%4"
+                 : "=&v"(lo), "=&v"(hi)
+                 : "v"(lds_addr), "n"(OFFSET), "n"(OFFSET + 8 * 256));
 }
 
 // the merge by a second kernel (attn.hip)

@@ -73,7 +73,7 @@ __device__ __forceinline__ void kv8_numbers(uint32_t w, half2v &lo, half2v &hi)
     }
 }
 
-// the values of four codes of one head; scale a finite scale of that head
+// the values of four codes of one head; NaN for a NaN scale
 template <int FMT>
 __device__ __forceinline__ void kv8_values(uint32_t w, _Float16 scale, half2v &lo, half2v &hi)
 {

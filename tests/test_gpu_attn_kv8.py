@@ -233,3 +233,76 @@ def test_graph_replays_equal_the_eager_calls():
         for got, w in zip((q, out, path, result, k, v, ks, vs), want):
             assert torch.equal(got, w), replay
         other.run(ws)
+
+
+# many rows over a long prefix: taller row tiles, whose codes become fp16 numbers once for 128 rows
+TALL = [
+    (60, 8192, 64, 8),      # 480 rows per KV head
+    (64, 8191, 64, 8),      # draft keys from the last key of a step to the third step on
+    (64, 6002, 64, 8),      # the last step holds two keys
+    (37, 24000, 28, 4),     # 259 rows: tiles of 87
+    (12, 33000, 64, 8),     # 96 rows, one tile, 31 ranges
+]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,P,Hq,Hkv", TALL)
+def test_many_rows_over_a_long_prefix(M, P, Hq, Hkv, fmt):
+    print(f"attn_kv8 tall M={M} P={P} Hq={Hq} Hkv={Hkv} fmt={fmt}", flush=True)
+    c = Call(100 + M, M, P, Hq, Hkv, fmt, tree="random", q_std=3.0)
+    out = c.run()
+    c.check(out)
+    np.testing.assert_array_equal(c.run().view(np.uint16), out.view(np.uint16))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("at", [5, 8190, 8230])
+def test_nan_keys_and_values_under_many_rows(at, fmt):
+    """as above: a NaN scale reaches the rows that see its key, and only the heads of its KV head"""
+    c = Call(110 + at, 60, 8190, 64, 8, fmt, tree="random")
+    c.ks[at, 3], c.k[at, 3] = np.nan, 0
+    c.vs[at, 5], c.v[at, 5] = np.nan, 0
+    out = c.run()
+    c.check(out)
+    lost = np.isnan(out).any(axis=(0, 2))
+    assert lost[24:32].all() and lost[40:48].all() and lost.sum() == 16
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_hidden_rows_that_hold_anything_under_many_rows(fmt):
+    M, P = 64, 9001
+    c = Call(120, M, P, 64, 8, fmt)
+    n = 41
+    c.mask[n:], c.mask[:, n:] = 0, 0
+    clean = c.run()
+    c.check(clean)
+    rng = np.random.default_rng(M)
+    for codes, scales in ((c.k, c.ks), (c.v, c.vs)):
+        codes[P + n:] = rng.choice(np.array([0x7F, 0xFF, 0x80, 0x7E], dtype=np.uint8), codes[P + n:].shape)
+        scales[P + n:] = rng.choice(np.array([np.nan, np.inf, -np.inf, 65504.0, 1.0], dtype=np.float16), scales[P + n:].shape)
+    np.testing.assert_array_equal(c.run().view(np.uint16), clean.view(np.uint16))
+
+
+def test_workspace_shared_by_calls_of_every_kind():
+    """few and many rows, short and long prefixes, one workspace, one after another, twice"""
+    calls = [Call(130 + i, *c) for i, c in enumerate(((60, 8192, 64, 8, 1), (1, 2048, 64, 8, 2), (7, 40000, 32, 8, 1), (60, 700, 64, 8, 2), (12, 33000, 64, 8, 1)))]
+    want = [c.run() for c in calls]
+    ws = B.new_workspace(max(B.tree_verify_attn_kv8_workspace_bytes(c.M, c.P, c.Hq, c.Hkv, D) for c in calls))
+    for _ in range(2):
+        for c, w in zip(calls, want):
+            np.testing.assert_array_equal(c.run(ws).view(np.uint16), w.view(np.uint16))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,P,Hq,Hkv", [(5, 40, 8, 2), (37, 3333, 28, 4), (60, 8190, 64, 8)])
+def test_rows_of_padding_are_zero_whatever_the_prefix_holds(M, P, Hq, Hkv, fmt):
+    """an empty mask row sees no committed key either: neither a NaN key there nor a NaN or an infinity in the row's own query shows"""
+    c = Call(140 + M, M, P, Hq, Hkv, fmt)
+    c.mask[M - 2:], c.mask[:, M - 2:] = 0, 0
+    c.mask[1] = 0     # and one inside the tree
+    out = c.run()
+    c.check(out)
+    c.ks[3, 1], c.k[3, 1] = np.nan, 0
+    c.q[1, 0], c.q[M - 1, 0, 5], c.q[M - 2, 0, 5] = np.inf, np.nan, -np.inf
+    out = c.run()
+    assert (out[[1, M - 2, M - 1]] == 0).all() and np.isnan(out[0]).any()
