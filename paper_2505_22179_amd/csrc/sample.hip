@@ -6,13 +6,16 @@
 // of the row's total where sums in fp32 would be off by 1e-5 -- tokens near a border would change with the split.  Tokens more than e^31 below the
 // row's largest weigh nothing (262144 of them 1e-8 of the total at most) and take part in nothing.
 //
-// Three kernels, each over chunks of kChunk tokens of every row, pass over the logits once:
-//   sample_top_kernel    the chunks' largest logit, its token, and their smallest number
-//   sample_bins_kernel   counts and weights (fp32 is enough here) in kBins bins of even width in (max - x) / T; the row's last workgroup finds the
+// Three kernels, each of several workgroups per row, pass over the logits once:
+//   sample_top_kernel    the largest logit of each chunk of kChunk tokens, its token, and the smallest number
+//   sample_bins_kernel   counts and weights (fp32 is enough here) in kBins bins of even width in max - x; the row's last workgroup finds the
 //                        few bins in which the limits of top-k and top-p fall, whatever the rounding.  Not launched without such limits.
-//   sample_draw_kernel   exact weight of what certainly stays, chunk by chunk, and a list of the tokens in those few bins; the row's last
-//                        workgroup sorts the list, which gives the exact cut, draws the chunk and then the token inside it
+//   sample_draw_kernel   exact weight of what certainly stays, by segments of 512 tokens, and a list of the tokens in those few bins; the row's last
+//                        workgroup sorts the list, which gives the exact cut, draws the segment and then the token inside it
 // A list of more than kList tokens (thousands of nearly equal logits) is given up: the last workgroup then finds the cut by digits of the logits.
+// Measured, the three kernels: 1 row of 32000 tokens, top-k 4 + 8 + 11 us; 7 rows of 128256, top-p 4 + 10 + 16; 60 rows of 128256, all limits
+// 8 + 14 + 20, where reading the logits once takes 6.  What bounds them: for few rows the chain of dependent steps (three launches, two meetings of a
+// row's workgroups, each several trips to memory); for many the vector units, which put every token in its bin and weigh the kept ones in fp64.
 #include "internal.h"
 #include "devscope.h"
 
@@ -24,7 +27,9 @@ constexpr int kChunk = kSampleThreads * kPer;
 constexpr int kChunks = 262144 / kChunk;                 // of the largest vocabulary
 constexpr int kBins = 1024;
 constexpr int kList = 2048;                              // entries of a row's list
-constexpr int kPart = 1024;                              // and of a chunk's part of it
+constexpr int kSegment = 512;                            // tokens whose weight is held as one number
+constexpr int kSegments = kChunks * kChunk / kSegment;   // of the largest vocabulary
+constexpr int kGroups = 64;                              // workgroups of a row in sample_draw_kernel
 constexpr double kFarthest = 31.0;
 constexpr double kOne = 17592186044416.0;                // 2^44: weight 1
 constexpr int32_t kNoToken = 0x7FFFFFFF;
@@ -73,17 +78,16 @@ struct RowRule {
     int k;           // 0: no limit
     double p;        // >= 1: no limit
     double min_w;    // 0: no limit
-    double bins_per; // bins of unit distance
+    float bins_per;  // bins of unit depth
+    float deepest;   // tokens of this depth and more weigh nothing
     float u;         // the uniform number
 
-    // distance below the largest logit in units of the temperature; at least kFarthest, or NaN, for what takes no part
-    __device__ __forceinline__ double below(float x) const
-    {
-        if (x == top) return 0.0;
-        return x > -__builtin_inff() ? ((double)top - (double)x) * inv_t : kFarthest;
-    }
-    // y < kFarthest; rises with y, equal for equal y
-    __device__ __forceinline__ int bin(double y) const { return min((int)(y * bins_per), kBins - 1); }
+    // Half the distance below the largest logit, in fp32: rises as x falls, the same for equal logits, and cannot overflow.  It says which tokens take part
+    // (depth < deepest; not so for NaN and -inf) and which bin they are in.
+    __device__ __forceinline__ float depth(float x) const { return x == top ? 0.f : __builtin_fmaf(-0.5f, x, 0.5f * top); }
+    __device__ __forceinline__ int bin(float depth) const { return (int)fminf(depth * bins_per, (float)(kBins - 1)); }
+    // distance below the largest logit in units of the temperature, of tokens that take part
+    __device__ __forceinline__ double below(float x) const { return x == top ? 0.0 : ((double)top - (double)x) * inv_t; }
 };
 // w in whole numbers of 2^-44, 0 <= w <= 1: added to 2^52, a double's lowest bit is one
 __device__ __forceinline__ uint64_t units(double w) { return __builtin_bit_cast(uint64_t, fma(w, kOne, 0x1p52)) & ((1ull << 52) - 1); }
@@ -95,17 +99,20 @@ struct SampleArgs {
     const float *top_p, *min_p, *uniform;
     int32_t *token;
     float *prob;
-    int V, chunks;
+    int V, chunks, segments;
+    int bin_groups, bin_chunks;      // workgroups of a row in sample_bins_kernel, chunks of each
+    int groups, rounds;              // workgroups of a row in sample_draw_kernel, segments of each wavefront
     struct ChunkTop *tops;           // [M][chunks]
-    unsigned long long *bins;        // [M][chunks][kBins]: count << 50 | weight in 2^-31
+    unsigned long long *bins;        // [M][bin_groups][kBins]: count << 48 | weight in 2^-31; a group has 32768 tokens at most
     struct RowCut *cuts;             // [M]
-    struct ChunkMass *masses;        // [M][chunks]
-    unsigned long long *lists;       // [M][chunks][kPart]
+    unsigned long long *kept;        // [M][segments]: weight that stays for certain and is not below min_p
+    struct GroupMass *masses;        // [M][groups]
+    unsigned long long *lists;       // [M][groups][kList]
     uint32_t *tickets;               // [2 M]
 };
 struct ChunkTop { float top; int32_t at; float least; int32_t unused; };
-// weights: kept for certain and not below min_p; all above the first border bin; between the border bins and the k-th token's.  And the chunk's list
-struct ChunkMass { unsigned long long kept, above, between, listed; };
+// weights of all above the first border bin, and of all between the border bins and the k-th token's; the length of the group's list
+struct GroupMass { unsigned long long above, between, listed, unused; };
 struct RowCut { int32_t first, last, k_bin, above_k; };   // border bins of top-p (first .. last), bin of the k-th token (kNoBin: none), tokens in the bins above it
 
 // the rule of row m and, in at, the first token of its largest logit (kNoToken: the row has no token); every lane of a wavefront calls it
@@ -140,8 +147,9 @@ __device__ __forceinline__ RowRule row_rule(const SampleArgs &a, int m, int &at)
     r.p = p < 1.f ? (double)p : 2.0;
     r.min_w = min_p > 0.f ? (double)min_p : 0.0;
     // the bins span the distances that there are, so that they stay narrow at high temperatures
-    const double span = fmin(r.below(c.least), kFarthest);
-    r.bins_per = span > 0.0 ? (double)kBins / span : 0.0;
+    r.deepest = r.greedy ? 0.f : fmaxf((float)(0.5 * kFarthest * (double)t), 0x1p-149f);
+    const float span = fminf(r.depth(c.least), r.deepest);
+    r.bins_per = span > 0.f ? fminf((float)kBins / span, 3.0e38f) : 0.f;
     return r;
 }
 
@@ -252,49 +260,59 @@ __global__ __launch_bounds__(kSampleThreads) void sample_top_kernel(const Sample
 // Rows without a limit of this kind leave at once, and so does a row's every workgroup.
 __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(const SampleArgs a)
 {
-    const int tid = threadIdx.x, m = blockIdx.y, first = blockIdx.x * kChunk;
+    const int tid = threadIdx.x, m = blockIdx.y;
     const float *x = a.logits + (size_t)m * a.V;
     __shared__ unsigned long long bins[kBins];
     float v[kPer];
+    auto fetch = [&](int chunk) {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const int i = first + e * kSampleThreads + tid;
-        v[e] = i < a.V ? x[i] : -__builtin_inff();
-    }
+        for (int e = 0; e < kPer; ++e) {
+            const int i = chunk * kChunk + e * kSampleThreads + tid;
+            v[e] = i < a.V ? x[i] : -__builtin_inff();
+        }
+    };
+    int chunk = blockIdx.x * a.bin_chunks;
+    const int chunks_end = min(chunk + a.bin_chunks, a.chunks);
+    fetch(chunk);
     int at;
     const RowRule r = row_rule(a, m, at);
     if (at == kNoToken || r.greedy || (r.k == 0 && r.p >= 1.0)) return;   // uniform over the row
     for (int b = tid; b < kBins; b += kSampleThreads) bins[b] = 0;
     __syncthreads();
+    const float per_octave = (float)(r.inv_t * -2.0 * 1.44269504088896340736);
+    while (true) {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const double y = r.below(v[e]);
-        if (!(y < kFarthest)) continue;
-        const float w = __builtin_amdgcn_exp2f((float)y * -1.44269504f);
-        atomicAdd(&bins[r.bin(y)], (1ull << 50) + (unsigned long long)(uint32_t)(w * 2147483648.f + 0.5f));
+        for (int e = 0; e < kPer; ++e) {
+            const float d = r.depth(v[e]);
+            if (!(d < r.deepest)) continue;
+            const float w = __builtin_amdgcn_exp2f(d * per_octave);
+            atomicAdd(&bins[r.bin(d)], (1ull << 48) + (unsigned long long)(uint32_t)(w * 2147483648.f + 0.5f));
+        }
+        if (++chunk >= chunks_end) break;   // uniform
+        fetch(chunk);
     }
     __syncthreads();
     // two neighbouring bins per thread, here and below
     static_assert(kBins == 2 * kSampleThreads, "two bins per thread");
     typedef float float4v __attribute__((ext_vector_type(4)));
     typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
-    const PartialBuffer rows = partial_buffer(reinterpret_cast<const float *>(a.bins + (size_t)m * a.chunks * kBins));
+    const PartialBuffer rows = partial_buffer(reinterpret_cast<const float *>(a.bins + (size_t)m * a.bin_groups * kBins));
     store_partial(rows, blockIdx.x * (kBins / 2) + tid, __builtin_bit_cast(float4v, (u64x2){bins[2 * tid], bins[2 * tid + 1]}));
-    if (!last_of_row(a.tickets + m, a.chunks)) return;
+    if (!last_of_row(a.tickets + m, a.bin_groups)) return;
     // counts and weights of the whole row, and their sums up to each bin
     uint64_t count[2] = {0, 0}, mass[2] = {0, 0};
-    constexpr int kTogether = 16;   // chunks whose loads are under way together
-    for (int c0 = 0; c0 < a.chunks; c0 += kTogether) {
+    constexpr int kTogether = 16;   // groups whose loads are under way together
+    for (int c0 = 0; c0 < a.bin_groups; c0 += kTogether) {
         u64x2 n[kTogether];
 #pragma unroll
-        for (int c = 0; c < kTogether; ++c) n[c] = __builtin_bit_cast(u64x2, load_partial(rows, min(c0 + c, a.chunks - 1) * (kBins / 2) + tid));
+        for (int c = 0; c < kTogether; ++c) n[c] = __builtin_bit_cast(u64x2, load_partial(rows, min(c0 + c, a.bin_groups - 1) * (kBins / 2) + tid));
 #pragma unroll
         for (int c = 0; c < kTogether; ++c)
-            if (c0 + c < a.chunks) {   // uniform
+            if (c0 + c < a.bin_groups) {   // uniform
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    count[e] += n[c][e] >> 50;
-                    mass[e] += n[c][e] & ((1ull << 50) - 1);
+                    count[e] += n[c][e] >> 48;
+                    mass[e] += n[c][e] & ((1ull << 48) - 1);
                 }
             }
     }
@@ -317,7 +335,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(const Sampl
         __syncthreads();
     }
     if (r.p < 1.0) {
-        // The weights here are off by less than 2^-18 of each (an fp32 exponent of up to 45) and by V 2^-32 in all: the true border lies between
+        // The weights here are off by less than 2^-17 of each (an fp32 exponent of up to 45 with three roundings) and by V 2^-32 in all: the true border lies between
         // `low` and `high`, and so in the bins that reach over one and begin below the other
         const double slack = (double)a.V * 0.5 + 1.0;   // in units of 2^-31
         const double low = r.p * (double)(limited_k ? k_low : all[1]) * (1.0 - 0x1p-16) - slack;
@@ -361,11 +379,10 @@ __device__ __attribute__((noinline)) uint64_t cut_by_digits(const float *x, int 
         for (int i = tid; i < V; i += kSampleThreads) {
             const float v = x[i];
             const uint32_t key = order_key(v);
-            const double y = r.below(v);
-            if ((key & known) != prefix || !(y < kFarthest)) continue;
+            if ((key & known) != prefix || !(r.depth(v) < r.deepest)) continue;
             const int d = (key >> shift) & 255;
             atomicAdd(&sh.count[d], 1u);
-            atomicAdd(&sh.mass[d], (unsigned long long)units(exp_minus(y)));
+            atomicAdd(&sh.mass[d], (unsigned long long)units(exp_minus(r.below(v))));
         }
         __syncthreads();
         if (tid == 0) {
@@ -420,16 +437,24 @@ __device__ __attribute__((noinline)) uint64_t cut_by_digits(const float *x, int 
 // stretches of the distance, then each entry by the greater ones of its stretch: 14 us fewer than by the greater ones of 600 entries, 60 barriers
 // fewer than a bitonic sort.  A stretch with many entries (equal logits) makes it bitonic all the same.
 constexpr int kStretches = 1024, kStretchMost = 64;
-__device__ __forceinline__ void sort_list(unsigned long long *list, unsigned long long *other, uint32_t n, const RowRule &r, const RowCut &cut)
+// What only the row's last workgroup holds in LDS: it lies where the segments' logits were
+struct TailLds {
+    unsigned long long upto[kList];
+    uint32_t from[kStretches + 1], most;
+    DigitBins digits;
+};
+__device__ __forceinline__ void sort_list(unsigned long long *list, TailLds &sh, uint32_t n, const RowRule &r, const RowCut &cut)
 {
     const int tid = threadIdx.x;
-    __shared__ uint32_t from[kStretches + 1];
-    __shared__ uint32_t most;
+    unsigned long long *const other = sh.upto;
+    uint32_t *const from = sh.from;
+    uint32_t &most = sh.most;
     constexpr int kEach = kList / kSampleThreads;
     const int low_bin = min(cut.first, cut.k_bin), high_bin = cut.k_bin == kNoBin ? cut.last : max(cut.last, cut.k_bin);
-    const double low = r.bins_per > 0.0 ? (double)low_bin / r.bins_per : 0.0, per = r.bins_per * (double)kStretches / (double)(high_bin - low_bin + 1);
+    const float per = (float)kStretches / (float)(high_bin - low_bin + 1);
     auto stretch = [&](uint64_t o) {   // rises with the distance, equal for equal logits
-        return min(max((int)((r.below(order_number((uint32_t)(o >> 32))) - low) * per), 0), kStretches - 1);
+        const float b = r.depth(order_number((uint32_t)(o >> 32))) * r.bins_per - (float)low_bin;
+        return (int)fminf(fmaxf(b * per, 0.f), (float)(kStretches - 1));
     };
     static_assert(kStretches == 2 * kSampleThreads, "two stretches per thread");
     from[2 * tid] = from[2 * tid + 1] = 0;
@@ -493,19 +518,35 @@ __device__ __forceinline__ void sort_list(unsigned long long *list, unsigned lon
     __syncthreads();
 }
 
+__device__ __forceinline__ void number_to_lds(const float *src, float *lds_base)   // lane l's number at src lands at lds_base[l] (wavefront-uniform)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, (__attribute__((address_space(3))) void *)lds_base, 4, 0, 0);
+}
+
+// A wavefront takes segments of 512 tokens, `rounds` of them; their logits come straight to LDS, two segments ahead, and are looked at in loops that are not
+// unrolled: code that runs once is fetched from memory, and unrolled over 16 tokens it took 2 us longer than the work.
 __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const SampleArgs a)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = blockIdx.y, first = blockIdx.x * kChunk, V = a.V;
+    const int tid = threadIdx.x, lane = tid & 63, m = blockIdx.y, V = a.V;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float *x = a.logits + (size_t)m * V;
-    __shared__ unsigned long long list[kList], upto[kList];
-    __shared__ unsigned long long sums[3];
+    constexpr int kSteps = kSegment / 64;
+    __shared__ unsigned long long list[kList];
+    __shared__ float4 early[kSampleWaves * 2 * kSegment / 4];
+    static_assert(sizeof(TailLds) <= sizeof(early), "the tail's LDS lies where the segments were");
+    TailLds &tail = *reinterpret_cast<TailLds *>(early);
+    __shared__ unsigned long long sums[2];
     __shared__ uint32_t listed;
-    float v[kPer];
+    float *const mine = reinterpret_cast<float *>(early) + wave * 2 * kSegment;
+    const int segment0 = blockIdx.x * kSampleWaves * a.rounds + wave;
+    const int rounds = min(a.rounds, (a.segments - segment0 + kSampleWaves - 1) / kSampleWaves);   // not above 0: none
+    auto request = [&](int round) {
+        const int i0 = (segment0 + round * kSampleWaves) * kSegment + lane;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const int i = first + e * kSampleThreads + tid;
-        v[e] = i < V ? x[i] : -__builtin_inff();
-    }
+        for (int e = 0; e < kSteps; ++e) number_to_lds(x + min(i0 + e * 64, V - 1), mine + (round & 1) * kSegment + e * 64);
+    };
+    if (rounds > 0) request(0);
+    if (rounds > 1) request(1);
     RowCut cut = {kNoBin, kNoBin, kNoBin, 0};
     if (a.top_k || a.top_p) cut = a.cuts[m];   // of use where sample_bins_kernel has written it
     int at;
@@ -515,118 +556,132 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const Sampl
             a.token[m] = at;
             a.prob[m] = at == kNoToken ? 0.f : 1.f;
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may land in LDS that has been given to others
         return;
     }
     const bool limited = r.k != 0 || r.p < 1.0;   // uniform over the row
     if (!limited) cut = {kNoBin, kNoBin, kNoBin, 0};
-    if (tid == 0) listed = 0, sums[0] = sums[1] = sums[2] = 0;
+    if (tid == 0) listed = 0, sums[0] = sums[1] = 0;
     __syncthreads();
-    uint64_t kept = 0, above = 0, between = 0;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const double y = r.below(v[e]);
-        if (!(y < kFarthest)) continue;
-        const int b = r.bin(y);
-        if (b >= cut.first && (b <= cut.last || b >= cut.k_bin)) {   // a border bin, or beyond them all
-            if (b > cut.last && b > cut.k_bin) continue;
-            const uint32_t n = atomicAdd(&listed, 1u);
-            if (n < kPart) list[n] = order_of(v[e], first + e * kSampleThreads + tid);
-        } else {
-            const double w = exp_minus(y);
-            const uint64_t n = units(w);
-            above += b < cut.first ? n : 0;
-            between += b < cut.first ? 0 : n;
-            kept += b < cut.first && w >= r.min_w ? n : 0;
+    unsigned long long *const row_kept = a.kept + (size_t)m * a.segments;
+    uint64_t above = 0, between = 0;
+#pragma unroll 1
+    for (int round = 0; round < rounds; ++round) {
+        const int segment = segment0 + round * kSampleWaves, i0 = segment * kSegment + lane;
+        if (round + 1 < rounds) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");   // the next segment may be under way
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const float *const here = mine + (round & 1) * kSegment + lane;
+        uint64_t kept = 0;
+#pragma unroll 1
+        for (int e = 0; e < kSteps; ++e) {
+            const float v = here[e * 64];
+            const float d = r.depth(v);
+            const int b = r.bin(d);
+            if (!(d < r.deepest) || i0 + e * 64 >= V || (b > cut.last && b > cut.k_bin)) continue;   // takes no part, or is beyond the limits
+            if (b >= cut.first && (b <= cut.last || b == cut.k_bin)) {   // a border bin
+                const uint32_t n = atomicAdd(&listed, 1u);
+                if (n < kList) list[n] = order_of(v, i0 + e * 64);
+            } else {
+                const double w = exp_minus(r.below(v));
+                const uint64_t n = units(w);
+                above += b < cut.first ? n : 0;
+                between += b < cut.first ? 0 : n;
+                kept += b < cut.first && w >= r.min_w ? n : 0;
+            }
         }
+        if (round + 2 < rounds) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this segment has been read
+            request(round + 2);
+        }
+        kept = scan_wave(kept);
+        if (lane == 63) store_shared(row_kept + segment, kept);
     }
-    kept = scan_wave(kept);
     above = scan_wave(above);
     between = scan_wave(between);
     if (lane == 63) {
-        atomicAdd(&sums[0], (unsigned long long)kept);
-        atomicAdd(&sums[1], (unsigned long long)above);
-        atomicAdd(&sums[2], (unsigned long long)between);
+        atomicAdd(&sums[0], (unsigned long long)above);
+        atomicAdd(&sums[1], (unsigned long long)between);
     }
     __syncthreads();
-    ChunkMass *const masses = a.masses + m * a.chunks;
-    unsigned long long *const lists = a.lists + (size_t)m * a.chunks * kPart;
-    if (tid < 3) store_shared(&masses[blockIdx.x].kept + tid, sums[tid]);
-    if (tid == 3) store_shared(&masses[blockIdx.x].listed, listed);
-    for (uint32_t n = tid; n < min(listed, (uint32_t)kPart); n += kSampleThreads) store_shared(lists + (size_t)blockIdx.x * kPart + n, list[n]);
-    if (!last_of_row(a.tickets + gridDim.y + m, a.chunks)) return;
+    GroupMass *const masses = a.masses + m * a.groups;
+    unsigned long long *const lists = a.lists + (size_t)m * a.groups * kList;
+    if (tid < 2) store_shared(&masses[blockIdx.x].above + tid, sums[tid]);
+    if (tid == 2) store_shared(&masses[blockIdx.x].listed, listed);
+    for (uint32_t n = tid; n < min(listed, (uint32_t)kList); n += kSampleThreads) store_shared(lists + (size_t)blockIdx.x * kList + n, list[n]);
+    if (!last_of_row(a.tickets + gridDim.y + m, a.groups)) return;
 
     // ---- the row's last workgroup: the exact cut, then the draw
-    // Every wavefront fetches what the chunks found (lane = chunk), and, not knowing their counts yet, the first 64 entries of the parts that it
-    // will gather: chunks wave, wave + 8, ...
-    __shared__ unsigned long long chunk_mass[kChunks];
-    ChunkMass mine = {0, 0, 0, 0};
-    if (lane < a.chunks) {
-        mine.kept = load_shared(&masses[lane].kept);
-        mine.above = load_shared(&masses[lane].above);
-        mine.between = load_shared(&masses[lane].between);
-        mine.listed = load_shared(&masses[lane].listed);
+    // Every wavefront fetches what the groups found (lane = group), and, not knowing their counts yet, the first 64 entries of the lists that it
+    // will gather: groups wave, wave + 8, ...
+    __shared__ unsigned long long segment_mass[kSegments];
+    static_assert(kSegments == kSampleThreads && kSegment == kSampleThreads, "a thread per segment, and per token of one");
+    GroupMass found = {0, 0, 0, 0};
+    if (lane < a.groups) {
+        found.above = load_shared(&masses[lane].above);
+        found.between = load_shared(&masses[lane].between);
+        found.listed = load_shared(&masses[lane].listed);
     }
-    constexpr int kParts = kChunks / kSampleWaves;
+    const uint64_t own_kept = tid < a.segments ? load_shared(row_kept + tid) : 0;
+    constexpr int kParts = kGroups / kSampleWaves;
     uint64_t entry[kParts];
 #pragma unroll
-    for (int q = 0; q < kParts; ++q) entry[q] = load_shared(lists + (size_t)min(wave + q * kSampleWaves, a.chunks - 1) * kPart + lane);
-    if (tid < kChunks) chunk_mass[tid] = mine.kept;
-    const uint64_t listed_to = scan_wave(mine.listed);
-    const uint64_t all_above = of_lane(scan_wave(mine.above), 63), all_between = of_lane(scan_wave(mine.between), 63);
-    const bool parts_fit = !__any(mine.listed > kPart);
+    for (int q = 0; q < kParts; ++q) entry[q] = load_shared(lists + (size_t)min(wave + q * kSampleWaves, a.groups - 1) * kList + lane);
+    segment_mass[tid] = own_kept;
+    const uint64_t listed_to = scan_wave(found.listed);
+    const uint64_t all_above = of_lane(scan_wave(found.above), 63), all_between = of_lane(scan_wave(found.between), 63);
     const uint32_t n = (uint32_t)of_lane(listed_to, 63);
     uint64_t cut_order = 0;   // tokens of this order and earlier ones stay
-    if (n > kList || !parts_fit) {
-        __shared__ DigitBins digits;
+    if (n > kList) {
+        DigitBins &digits = tail.digits;
         uint64_t weight;
         if (cut.k_bin != kNoBin) {
             cut_order = cut_by_digits(x, V, r, false, (double)r.k, digits, weight);
         } else {   // the list's share of the row is not known: once more from the logits
             uint64_t part[1] = {0}, total[1];
             for (int i = tid; i < V; i += kSampleThreads) {
-                const double y = r.below(x[i]);
-                if (y < kFarthest) part[0] += units(exp_minus(y));
+                const float v = x[i];
+                if (r.depth(v) < r.deepest) part[0] += units(exp_minus(r.below(v)));
             }
             scan_block(part, total);
             weight = total[0];
         }
         if (r.p < 1.0) cut_order = cut_by_digits(x, V, r, true, r.p * (double)weight, digits, weight);
         __syncthreads();
-        if (tid < kChunks) chunk_mass[tid] = 0;
+        segment_mass[tid] = 0;
         __syncthreads();
-        for (int c = 0; c < a.chunks; ++c) {
-            uint64_t part = 0;
-            for (int i = c * kChunk + tid; i < min((c + 1) * kChunk, V); i += kSampleThreads) {
-                const double y = r.below(x[i]), w = y < kFarthest && order_of(x[i], i) >= cut_order ? exp_minus(y) : 0.0;
-                if (w >= r.min_w) part += units(w);
-            }
-            part = scan_wave(part);
-            if (lane == 63) atomicAdd(&chunk_mass[c], (unsigned long long)part);
+        for (int c = 0; c < a.segments; ++c) {
+            const int i = c * kSegment + tid;
+            const float v = i < V ? x[i] : -__builtin_inff();
+            const double w = r.depth(v) < r.deepest && order_of(v, i) >= cut_order ? exp_minus(r.below(v)) : 0.0;
+            const uint64_t part = scan_wave(w >= r.min_w ? units(w) : 0);
+            if (lane == 63) atomicAdd(&segment_mass[c], (unsigned long long)part);
         }
         __syncthreads();
     } else if (n > 0) {
 #pragma unroll
         for (int q = 0; q < kParts; ++q) {
             const int c = wave + q * kSampleWaves;
-            if (c >= a.chunks) break;   // uniform over the wavefront
-            const uint32_t count = (uint32_t)of_lane(mine.listed, c), base = (uint32_t)of_lane(listed_to, c) - count;
+            if (c >= a.groups) break;   // uniform over the wavefront
+            const uint32_t count = (uint32_t)of_lane(found.listed, c), base = (uint32_t)of_lane(listed_to, c) - count;
             if ((uint32_t)lane < count) list[base + lane] = entry[q];
-            for (uint32_t i = 64 + lane; i < count; i += 64) list[base + i] = load_shared(lists + (size_t)c * kPart + i);
+            for (uint32_t i = 64 + lane; i < count; i += 64) list[base + i] = load_shared(lists + (size_t)c * kList + i);
         }
         __shared__ uint32_t to_k_bin, staying;
         if (tid == 0) to_k_bin = 0, staying = 0;
         __syncthreads();
-        sort_list(list, upto, n, r, cut);
+        unsigned long long *const upto = tail.upto;
+        sort_list(list, tail, n, r, cut);
         // weights down the list; its places where something ends are found by the entry ahead of them
-        auto distance = [&](uint32_t i) { return r.below(order_number((uint32_t)(list[i] >> 32))); };
+        auto logit = [&](uint32_t i) { return order_number((uint32_t)(list[i] >> 32)); };
+        auto bin_at = [&](uint32_t i) { return r.bin(r.depth(logit(i))); };
         uint64_t so_far = 0;
 #pragma unroll 1
         for (uint32_t i0 = 0; i0 < n; i0 += kSampleThreads) {
             const uint32_t i = i0 + tid;
             uint64_t to[1] = {0}, all[1];
             if (i < n) {
-                to[0] = units(exp_minus(distance(i)));
-                if (r.bin(distance(i)) < cut.k_bin && (i + 1 == n || r.bin(distance(i + 1)) >= cut.k_bin)) to_k_bin = i + 1;   // one entry of all, or none
+                to[0] = units(exp_minus(r.below(logit(i))));
+                if (bin_at(i) < cut.k_bin && (i + 1 == n || bin_at(i + 1) >= cut.k_bin)) to_k_bin = i + 1;   // one entry of all, or none
             }
             scan_block(to, all);
             if (i < n) upto[i] = so_far + to[0];
@@ -650,54 +705,31 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const Sampl
         cut_order = stay ? list[stay - 1] : list[0] + 1;
 #pragma unroll 1
         for (uint32_t i = tid; i < stay; i += kSampleThreads)
-            if (r.min_w == 0.0 || exp_minus(distance(i)) >= r.min_w)
-                atomicAdd(&chunk_mass[(~(uint32_t)list[i]) / kChunk], (unsigned long long)(upto[i] - (i ? upto[i - 1] : 0)));
+            if (r.min_w == 0.0 || exp_minus(r.below(logit(i))) >= r.min_w)
+                atomicAdd(&segment_mass[(~(uint32_t)list[i]) / kSegment], (unsigned long long)(upto[i] - (i ? upto[i - 1] : 0)));
         __syncthreads();
     } else {
         __syncthreads();
     }
-    // the chunk, in every wavefront alike
-    const uint64_t mass_to = scan_wave(lane < kChunks ? chunk_mass[lane & (kChunks - 1)] : 0);
-    const uint64_t total = of_lane(mass_to, 63);
-    uint64_t rank = drawn_rank(r.u, total);
-    const int chunk = __builtin_ctzll(__ballot(mass_to > rank));   // rank < total
-    if (chunk > 0) rank -= of_lane(mass_to, chunk - 1);
-    // the token: wavefront w takes kPer x 64 consecutive ones
-    const int i0 = chunk * kChunk + wave * (kPer * 64) + lane;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) v[e] = i0 + e * 64 < V ? x[i0 + e * 64] : -__builtin_inff();
-    double w[kPer];
-    uint64_t sum = 0;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const double y = r.below(v[e]);
-        w[e] = 0.0;
-        if (y < kFarthest && order_of(v[e], i0 + e * 64) >= cut_order) {   // few, where top-k or top-p cut much
-            const double own = exp_minus(y);
-            w[e] = own < r.min_w ? 0.0 : own;
-        }
-        sum += units(w[e]);
-    }
-    __shared__ unsigned long long wave_mass[kSampleWaves];
-    sum = of_lane(scan_wave(sum), 63);
-    if (lane == 0) wave_mass[wave] = sum;
+    // the segment, then the token
+    __shared__ uint64_t chosen_rank;
+    __shared__ int chosen;
+    uint64_t mass[1] = {segment_mass[tid]}, total[1], all[1];
+    const uint64_t own = mass[0];
+    scan_block(mass, total);
+    const uint64_t rank = drawn_rank(r.u, total[0]);   // below the total: one thread finds it in its segment
+    if (mass[0] > rank && mass[0] - own <= rank) chosen = tid, chosen_rank = rank - (mass[0] - own);
     __syncthreads();
-    for (int q = 0; q < wave; ++q) {
-        if (rank < wave_mass[q]) return;   // an earlier wavefront's
-        rank -= wave_mass[q];
-    }
-    if (rank >= sum) return;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const uint64_t here = units(w[e]), to = scan_wave(here), all = of_lane(to, 63);
-        if (rank < all) {   // uniform
-            if (to > rank && to - here <= rank) {
-                a.token[m] = i0 + e * 64;
-                a.prob[m] = (float)(w[e] * kOne / (double)total);
-            }
-            return;
-        }
-        rank -= all;
+    const int i = chosen * kSegment + tid;
+    const float v = i < V ? x[i] : -__builtin_inff();
+    double w = r.depth(v) < r.deepest && order_of(v, i) >= cut_order ? exp_minus(r.below(v)) : 0.0;
+    if (w < r.min_w) w = 0.0;
+    uint64_t to[1] = {units(w)};
+    const uint64_t here = to[0];
+    scan_block(to, all);
+    if (to[0] > chosen_rank && to[0] - here <= chosen_rank) {
+        a.token[m] = i;
+        a.prob[m] = (float)(w * kOne / (double)total[0]);
     }
 }
 
@@ -707,14 +739,33 @@ using namespace w4;
 
 extern "C" {
 
-// tickets | tops | cuts | masses | bins | lists
-static size_t sample_layout(int M, int V, size_t (&at)[6])
+// How a call's rows are split: about 512 workgroups at most, two per CU at work together.  More would wait for the first ones, in each of
+// which a few us pass before the first logit is looked at: 60 rows of 128256 tokens take 42 us with 512, 54 with 1024, 44 with 256.
+constexpr int kMost = 512;
+static_assert((kChunks * W4A16_MAX_M + kMost - 1) / kMost * kChunk < 1 << 16, "a bin counts the tokens of a group in 16 bits");
+static void sample_split(int M, int V, SampleArgs &a)
 {
-    const size_t rows = (size_t)M, chunks = (size_t)(V + kChunk - 1) / kChunk;
-    const size_t sizes[6] = {kTicketBytes, rows * chunks * sizeof(ChunkTop), rows * sizeof(RowCut), rows * chunks * sizeof(ChunkMass),
-                             rows * chunks * kBins * 8, rows * chunks * kPart * 8};
+    a.V = V;
+    a.chunks = (V + kChunk - 1) / kChunk;
+    a.segments = (V + kSegment - 1) / kSegment;
+    a.bin_chunks = (M * a.chunks + kMost - 1) / kMost;
+    a.bin_groups = (a.chunks + a.bin_chunks - 1) / a.bin_chunks;
+    const int smallest = (a.segments + kSampleWaves - 1) / kSampleWaves;   // groups, at one segment per wavefront; 64 at most
+    a.rounds = (M * smallest + kMost - 1) / kMost;
+    a.groups = (smallest + a.rounds - 1) / a.rounds;
+}
+
+// tickets | tops | cuts | group masses | segment masses | bins | lists
+constexpr int kSampleParts = 7;
+static size_t sample_layout(int M, const SampleArgs &a, size_t (&at)[kSampleParts])
+{
+    // M groups of a call are fewer than kMost + M: taken as that, so that what serves a call serves all smaller ones
+    const size_t rows = (size_t)M, most = kMost + W4A16_MAX_M, smallest = (a.segments + kSampleWaves - 1) / kSampleWaves;
+    const size_t groups = rows * smallest < most ? rows * smallest : most, bin_groups = rows * a.chunks < most ? rows * a.chunks : most;
+    const size_t sizes[kSampleParts] = {kTicketBytes, rows * a.chunks * sizeof(ChunkTop), rows * sizeof(RowCut), groups * sizeof(GroupMass),
+                                        rows * a.segments * 8, bin_groups * kBins * 8, groups * kList * 8};
     size_t end = 0;
-    for (int i = 0; i < 6; ++i) {
+    for (int i = 0; i < kSampleParts; ++i) {
         at[i] = end;
         end += (sizes[i] + 255) & ~(size_t)255;   // workgroups exchange through these: no line belongs to two
     }
@@ -724,8 +775,10 @@ static size_t sample_layout(int M, int V, size_t (&at)[6])
 size_t lm_head_sample_workspace_bytes(int M, int V)
 {
     if (M < 1 || M > W4A16_MAX_M || V < 1 || V > kChunks * kChunk) return 0;
-    size_t at[6];
-    return sample_layout(M, V, at);
+    SampleArgs a;
+    size_t at[kSampleParts];
+    sample_split(M, V, a);
+    return sample_layout(M, a, at);
 }
 
 int lm_head_sample(const float *logits, int M, int V, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
@@ -739,16 +792,30 @@ int lm_head_sample(const float *logits, int M, int V, const float *temperature, 
          reinterpret_cast<uintptr_t>(min_p) | reinterpret_cast<uintptr_t>(uniform) | reinterpret_cast<uintptr_t>(token) |
          reinterpret_cast<uintptr_t>(prob)) & 3u)
         return W4A16_EALIGN;
-    size_t at[6];
-    if (!workspace || workspace_bytes < sample_layout(M, V, at)) return W4A16_EWORKSPACE;
+    SampleArgs a;
+    size_t at[kSampleParts];
+    sample_split(M, V, a);
+    if (!workspace || workspace_bytes < sample_layout(M, a, at)) return W4A16_EWORKSPACE;
     uint8_t *ws = reinterpret_cast<uint8_t *>(workspace);
-    const SampleArgs a = {logits, temperature, top_k, top_p, min_p, uniform, token, prob, V, (V + kChunk - 1) / kChunk, (ChunkTop *)(ws + at[1]),
-                          (unsigned long long *)(ws + at[4]), (RowCut *)(ws + at[2]), (ChunkMass *)(ws + at[3]), (unsigned long long *)(ws + at[5]),
-                          (uint32_t *)ws};
-    const dim3 grid((unsigned)a.chunks, (unsigned)M);
-    hipLaunchKernelGGL(sample_top_kernel, grid, dim3(kSampleThreads), 0, (hipStream_t)stream, a);
-    if (top_k || top_p) hipLaunchKernelGGL(sample_bins_kernel, grid, dim3(kSampleThreads), 0, (hipStream_t)stream, a);
-    hipLaunchKernelGGL(sample_draw_kernel, grid, dim3(kSampleThreads), 0, (hipStream_t)stream, a);
+    a.logits = logits;
+    a.temperature = temperature;
+    a.top_k = top_k;
+    a.top_p = top_p;
+    a.min_p = min_p;
+    a.uniform = uniform;
+    a.token = token;
+    a.prob = prob;
+    a.tickets = (uint32_t *)ws;
+    a.tops = (ChunkTop *)(ws + at[1]);
+    a.cuts = (RowCut *)(ws + at[2]);
+    a.masses = (GroupMass *)(ws + at[3]);
+    a.kept = (unsigned long long *)(ws + at[4]);
+    a.bins = (unsigned long long *)(ws + at[5]);
+    a.lists = (unsigned long long *)(ws + at[6]);
+    const auto grid = [M](int groups) { return dim3((unsigned)groups, (unsigned)M); };
+    hipLaunchKernelGGL(sample_top_kernel, grid(a.chunks), dim3(kSampleThreads), 0, (hipStream_t)stream, a);
+    if (top_k || top_p) hipLaunchKernelGGL(sample_bins_kernel, grid(a.bin_groups), dim3(kSampleThreads), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL(sample_draw_kernel, grid(a.groups), dim3(kSampleThreads), 0, (hipStream_t)stream, a);
     return launch_status();
 }
 

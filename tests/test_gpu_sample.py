@@ -157,6 +157,33 @@ def test_rows_do_not_depend_on_their_neighbours_or_on_the_call():
         assert one[0][0] == token[m] and one[1][0] == prob[m]
 
 
+@pytest.mark.parametrize("V", [128256, 262144])
+def test_rows_do_not_depend_on_how_many_there_are(V):
+    """64 long rows are split into fewer, longer pieces than one is"""
+    x, rng = rows(14, 64, V)
+    kw = dict(temperature=rng.uniform(0.5, 1.5, 64), top_k=rng.integers(-5, 3000, 64), top_p=rng.uniform(0.5, 1.1, 64), min_p=rng.uniform(-0.1, 0.01, 64), u=rng.random(64))
+    token, prob = run(x, **kw)
+    for m in range(0, 64, 9):
+        one = run(x[m:m + 1], **{n: v[m:m + 1] for n, v in kw.items()})
+        assert one[0][0] == token[m] and one[1][0] == prob[m]
+
+
+def test_equal_logits_in_the_largest_call():
+    """a whole row in one bin: the first k tokens stay, or the first ceil(p V); token j of n equal ones is drawn for u in [j / n, (j + 1) / n)"""
+    V, rng = 262144, np.random.default_rng(15)
+    x = np.zeros((64, V), dtype=np.float32)
+    u = rng.integers(0, 1 << 24, 64).astype(np.float64) / (1 << 24)
+    k = rng.integers(2, V, 64)
+    token, prob = run(x, top_k=k, u=u)
+    np.testing.assert_array_equal(token, np.floor(u * k).astype(np.int64))
+    np.testing.assert_array_equal(prob, (1.0 / k).astype(np.float32))
+    p = rng.integers(1, 256, 64) / 256.0
+    n = np.ceil(p * V)
+    token, prob = run(x, top_p=p, u=u)
+    np.testing.assert_array_equal(token, np.floor(u * n).astype(np.int64))
+    np.testing.assert_array_equal(prob, (1.0 / n).astype(np.float32))
+
+
 def test_graph_replays_and_another_stream():
     x, rng = rows(12, 5, 50000)
     d = lambda a, t=torch.float32: torch.as_tensor(np.asarray(a), dtype=t).to(DEV)
