@@ -126,8 +126,10 @@ static uint32_t divider(int d) { return (uint32_t)(((1u << 31) + (unsigned)d - 1
 
 // Merge of the key ranges of one tile by the workgroup that finished last (fused mode): NS = compiled
 // upper bound of the number of ranges, IT = items a thread handles at once (all their loads are issued
-// together), PAD = rows that the partials of a range take.  Loads are device-scope: other workgroups, on other XCDs, wrote the partials in this kernel.
-template <int NS, int IT, int PAD>
+// together), PAD = rows that the partials of a range take, MARKS = a range's sum may be kPaddingMark.  Loads are device-scope: other
+// workgroups, on other XCDs, wrote the partials in this kernel.
+constexpr float kPaddingMark = -1.f;   // the row gets zeros, whatever the ranges hold
+template <int NS, int IT, int PAD, bool MARKS>
 __device__ __forceinline__ void merge_ranges(PartialBuffer unit_o, PartialBuffer unit_ml, _Float16 *__restrict__ out,
                                              int tid, int threads, const RowTile &tile, int nsplit)
 {
@@ -162,13 +164,16 @@ __device__ __forceinline__ void merge_ranges(PartialBuffer unit_o, PartialBuffer
             for (int s = 0; s < NS; ++s) m_all = fmaxf(m_all, ms[it][s]);
             float den = 0.f;
             float4v num = {0.f, 0.f, 0.f, 0.f};
+            bool padding = false;
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
+                if constexpr (MARKS) padding |= ls[it][s] < 0.f;
                 float wgt = (ms[it][s] == NEG_INF) ? 0.f : __builtin_amdgcn_exp2f(ms[it][s] - m_all);
                 den += wgt * ls[it][s];
                 num += wgt * os[it][s];
             }
-            const float inv = den == 0.f ? 0.f : 1.f / den;   // a row that sees no key (the 8-bit form allows it): zeros
+            const float inv = padding || den == 0.f ? 0.f : 1.f / den;
+            if (padding) num = (float4v){0.f, 0.f, 0.f, 0.f};
             int qrow, h;
             tile.locate(trow, qrow, h);
             typedef _Float16 half4v __attribute__((ext_vector_type(4)));
@@ -178,14 +183,14 @@ __device__ __forceinline__ void merge_ranges(PartialBuffer unit_o, PartialBuffer
     }
 }
 
-template <int PAD = kRowsPad>
+template <int PAD = kRowsPad, bool MARKS = false>
 __device__ __forceinline__ void merge_tile(PartialBuffer unit_o, PartialBuffer unit_ml, _Float16 *__restrict__ out, int tid,
                                            int threads, const RowTile &tile, int nsplit)
 {
-    if (nsplit <= 4) merge_ranges<4, 4, PAD>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
-    else if (nsplit <= 8) merge_ranges<8, 2, PAD>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
-    else if (nsplit <= 16) merge_ranges<16, 1, PAD>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
-    else merge_ranges<kMaxRanges, 1, PAD>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
+    if (nsplit <= 4) merge_ranges<4, 4, PAD, MARKS>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
+    else if (nsplit <= 8) merge_ranges<8, 2, PAD, MARKS>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
+    else if (nsplit <= 16) merge_ranges<16, 1, PAD, MARKS>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
+    else merge_ranges<kMaxRanges, 1, PAD, MARKS>(unit_o, unit_ml, out, tid, threads, tile, nsplit);
 }
 
 typedef __attribute__((address_space(3))) void lds_void;

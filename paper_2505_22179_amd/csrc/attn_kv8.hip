@@ -43,8 +43,8 @@ __device__ __forceinline__ void clear_codes(uint8_t *tile, uint32_t keys, int la
 
 // ---- row tiles of at most 32 rows: wavefronts with K and V tiles of their own -------------------------------
 // As tree_attn_wave_kernel: eight wavefronts carry the same 32 rows, wavefront w takes key steps w, w + 8, ... of the workgroup's range and
-// meets the others only at the end.  A step is 32 keys: 4 KB of K codes, 4 KB of V codes and 64 scales, brought straight to LDS up to two
-// steps ahead of their use (two buffers per wavefront).
+// meets the others only at the end.  A step is 32 keys: 4 KB of K codes, 4 KB of V codes and 64 scales, brought straight to LDS one step
+// ahead of their use (two buffers per wavefront; two steps ahead was no faster over long prefixes and 0.3 us slower over short ones).
 // What bounds it: with few rows over a long prefix, memory (7 rows of 32/8 heads over 131072 keys: 268 MB of codes in 53 us, 5.0 TB/s); over a short
 // one, its own length (1 row of 64/8 heads over 2049 keys: 8 us, of which the walk takes 3.5, arguments, mask and Q 2, the merges 2.5); with many rows
 // the turning of codes into numbers, which every 32 rows do again.
@@ -63,7 +63,11 @@ constexpr int kWaveWeights = kWaveState + kWaveRows * kWaves * 8;
 constexpr int kWaveEnd = kWaveWeights + kWaveRows * kWaves * 8;
 constexpr int kWaveLds = kWaveTiles > kWaveEnd ? kWaveTiles : kWaveEnd;
 typedef float float2v __attribute__((ext_vector_type(2)));
-constexpr float kBehind = 8.f;   // binary orders of magnitude
+// Running maxima are left behind the true ones by up to this many binary orders of magnitude: probabilities reach 2^8 then, which fp16 and the sums hold
+// as well as 1, and sums and outputs are rescaled a few times in all, not in most steps.
+constexpr float kBehind = 8.f;
+// A row whose mask row is empty is padding and sees nothing, committed keys included.  Only ranges with draft keys read the mask (in the others it would cost
+// up to 1.2 us of 15): they give such rows this sum, and whoever joins the ranges writes zeros.
 
 struct Kv8Args {
     uint32_t by_tiles, by_ranges;   // divider() of tiles_per_kv and nsplit
@@ -85,8 +89,6 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
 {
     extern __shared__ float4v smem4[];
     uint8_t *lds = reinterpret_cast<uint8_t *>(smem4);
-    fetch_arguments_together(a.by_tiles, a.by_ranges, a.q, a.k, a.v, a.k_scale, a.v_scale, a.mask, a.out, a.part_o, a.part_ml, a.tickets, a.M, a.P, a.Hq, a.Hkv,
-                             a.group, a.scale_log2e, a.nsplit, a.bq, a.brem, a.tile_rows, a.tiles_per_kv, a.fused);
     const int M = a.M, P = a.P, T = P + M;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -96,7 +98,25 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
     const RowTile tile(kvh, share.tile, M, a.Hq, a.group, a.tile_rows);
     const int b0 = sp * a.bq + (sp < a.brem ? sp : a.brem), b1 = b0 + a.bq + (sp < a.brem ? 1 : 0);
     const size_t kv_row_bytes = (size_t)a.Hkv * kHeadDim;
+    int my_row, my_head;
+    tile.locate(c, my_row, my_head);
 
+    // tree mask of the draft keys, one 64-bit word per query row: bytes requested first, words made of them behind the transfers
+    __shared__ uint64_t row_bits[kRowsPad];
+    const bool reaches_draft = b1 * kKeyBlock > P;   // uniform over the workgroup
+    uint32_t mask_byte[8] = {};
+    if (reaches_draft) {
+        const int mcol = min(lane, M - 1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mask_byte[i] = a.mask[(size_t)min(wave * 8 + i, M - 1) * M + mcol];
+    }
+    // Q fragments (second operand of S^T): steps 2 j and 2 j + 1 take the halves of chunk 2 j + h of the row
+    half8v qf[8];
+    {
+        const _Float16 *row = a.q + ((size_t)my_row * a.Hq + my_head) * kHeadDim + 16 * h;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) qf[j] = *reinterpret_cast<const half8v *>(row + 32 * (j >> 1) + 8 * (j & 1));
+    }
     // transfers: lane l of transfer i fills 16 l .. of 1 KB: chunk position l % 8 of key 8 i + l / 8
     uint8_t *const mine = lds + wave * 2 * kWaveBuf;
     const uint8_t *const k_src = a.k + (size_t)kvh * kHeadDim, *const v_src = a.v + (size_t)kvh * kHeadDim;
@@ -105,57 +125,38 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
     uint32_t lane_src[2];   // the chunk permutation depends on the transfer's parity only
 #pragma unroll
     for (int par = 0; par < 2; ++par) lane_src[par] = (uint32_t)trow * (uint32_t)kv_row_bytes + (uint32_t)((tchunk ^ ((4 * par + (trow >> 1)) & 7)) << 4);
-    auto request_rows = [&](const uint8_t *src, int step, uint8_t *dst) {   // four transfers
+    auto request = [&](int step, int buf) {
         const int key0 = step * kKeyBlock;
+        uint8_t *dst = mine + buf * kWaveBuf;
+        half_to_lds(s_src + (size_t)min(key0 + c, T - 1) * a.Hkv, dst + 2 * kWaveTile);
         if (key0 + kKeyBlock <= T) {   // uniform
-            const uint8_t *from = src + (size_t)key0 * kv_row_bytes;
+            const size_t at = (size_t)key0 * kv_row_bytes;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) row_to_lds(from + (size_t)(8 * i) * kv_row_bytes + lane_src[i & 1], dst + i * 1024);
+            for (int i = 0; i < 4; ++i) row_to_lds(k_src + at + (size_t)(8 * i) * kv_row_bytes + lane_src[i & 1], dst + i * 1024);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) row_to_lds(v_src + at + (size_t)(8 * i) * kv_row_bytes + lane_src[i & 1], dst + kWaveTile + i * 1024);
         } else {   // the last step of all: rows beyond the last key repeat it (they are hidden below)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                row_to_lds(src + (size_t)min(key0 + 8 * i + trow, T - 1) * kv_row_bytes + ((tchunk ^ ((4 * i + (trow >> 1)) & 7)) << 4), dst + i * 1024);
+            for (int i = 0; i < 4; ++i) {
+                const size_t at = (size_t)min(key0 + 8 * i + trow, T - 1) * kv_row_bytes + ((tchunk ^ ((4 * i + (trow >> 1)) & 7)) << 4);
+                row_to_lds(k_src + at, dst + i * 1024);
+                row_to_lds(v_src + at, dst + kWaveTile + i * 1024);
+            }
         }
     };
-    auto request_k = [&](int step, int buf) {   // the step's scales and K codes: five transfers
-        half_to_lds(s_src + (size_t)min(step * kKeyBlock + c, T - 1) * a.Hkv, mine + buf * kWaveBuf + 2 * kWaveTile);
-        request_rows(k_src, step, mine + buf * kWaveBuf);
-    };
-    auto request_v = [&](int step, int buf) { request_rows(v_src, step, mine + buf * kWaveBuf + kWaveTile); };
-    // Two steps are under way: a step's K follows into the buffer of the step two before as soon as that one's scores are done, its V behind that
-    // one's products.
     int step = b0 + wave;
-    if (step < b1) request_k(step, 0);
-
-    int my_row, my_head;
-    tile.locate(c, my_row, my_head);
-    half8v qf[8];   // Q fragments (second operand of S^T): steps 2 j and 2 j + 1 take the halves of chunk 2 j + h of the row
-    {
-        const _Float16 *row = a.q + ((size_t)my_row * a.Hq + my_head) * kHeadDim + 16 * h;
+    if (step < b1) request(step, 0);
+    uint64_t mbits = 0;
+    if (reaches_draft) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) qf[j] = *reinterpret_cast<const half8v *>(row + 32 * (j >> 1) + 8 * (j & 1));
+        for (int i = 0; i < 8; ++i) {
+            asm volatile("" : "+v"(mask_byte[i]));
+            const uint64_t bits = __ballot(mask_byte[i] != 0 && wave * 8 + i < M && lane < M);
+            if (lane == i) row_bits[wave * 8 + i] = bits;
+        }
+        __syncthreads();
+        mbits = row_bits[my_row];
     }
-    // tree mask of the draft keys, one 64-bit word per query row: bytes requested here, words made of them behind the other requests.  Ranges
-    // that end before the draft need it too: a row whose word is zero is padding and sees nothing at all.
-    __shared__ uint64_t row_bits[kRowsPad];
-    uint32_t mask_byte[8];
-    const int mcol = min(lane, M - 1);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) mask_byte[i] = a.mask[(size_t)min(wave * 8 + i, M - 1) * M + mcol];
-    __builtin_amdgcn_sched_barrier(0);
-    if (step < b1) request_v(step, 0);
-    if (step + kWaves < b1) {
-        request_k(step + kWaves, 1);
-        request_v(step + kWaves, 1);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        asm volatile("" : "+v"(mask_byte[i]));
-        const uint64_t bits = __ballot(mask_byte[i] != 0 && wave * 8 + i < M && lane < M);
-        if (lane == i) row_bits[wave * 8 + i] = bits;
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const uint64_t mbits = row_bits[my_row];
     const uint32_t kfrag = (uint32_t)(c * kHeadDim + ((h ^ ((c >> 1) & 7)) << 4));   // chunk 2 j + h: ^ (j << 5)
     // V: in 16-lane block b, lane s points at key 4 (b / 2) + r (r = s / 2 < 4) or 4 further on, chunk 2 dt + b % 2, bytes 8 (s % 2) ..
     const int vr = (lane & 15) >> 1, vkey = 4 * h + (vr < 4 ? vr : vr + 4);
@@ -169,11 +170,14 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
 
     int buf = 0;
     while (step < b1) {   // uniform over the wavefront; no barrier inside
-        const int key0 = step * kKeyBlock;
-        const bool next = step + kWaves < b1, next2 = step + 2 * kWaves < b1;   // uniform
-        // this step's K and scales have landed; newer: its V (4), the next step (9)
-        if (next) asm volatile("s_waitcnt vmcnt(13)" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+        const int next = step + kWaves, key0 = step * kKeyBlock;
+        asm volatile("" ::: "memory");
+        if (next < b1) {
+            request(next, buf ^ 1);
+            asm volatile("s_waitcnt vmcnt(9)" ::: "memory");   // this step's tiles; the next step's nine transfers are newer
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
         const uint8_t *const tiles = mine + buf * kWaveBuf;
         const uint32_t *const scales = reinterpret_cast<const uint32_t *>(tiles + 2 * kWaveTile);
         // A scale that is no number marks a head that held an infinity or a NaN.  Such keys take no part in the products (a hidden one must
@@ -183,21 +187,6 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
         uint32_t ks = scales[c];
         if ((ks & 0x7FFFu) >= kHalfInf) ks = 0;
         const _Float16 k_scale = __builtin_bit_cast(_Float16, (uint16_t)ks);
-        // V scales in the order of the contraction: slots 8 h + p of product u are keys 16 u + 4 h + p, and 8 further on for p >= 4
-        half8v vs[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            u32x4 s0 = *reinterpret_cast<const u32x4 *>(scales + 32 + 16 * u + 4 * h), s1 = *reinterpret_cast<const u32x4 *>(scales + 40 + 16 * u + 4 * h);
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                if (__builtin_expect(bad, 0)) {
-                    if ((s0[p] & 0x7FFFu) >= kHalfInf) s0[p] = 0;
-                    if ((s1[p] & 0x7FFFu) >= kHalfInf) s1[p] = 0;
-                }
-                vs[u][p] = __builtin_bit_cast(_Float16, (uint16_t)s0[p]);
-                vs[u][4 + p] = __builtin_bit_cast(_Float16, (uint16_t)s1[p]);
-            }
-        }
         float16v sc;
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[i] = 0.f;
@@ -213,33 +202,46 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
                 sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, qf[2 * j + e], sc, 0, 0, 0);
             }
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(vs[0]), "+v"(vs[1]) : : "memory");   // K tile and scales have been read
-        if (next2) request_k(step + 2 * kWaves, buf);
-        settled(sc);   // element i: key 8 (i / 4) + 4 h + i % 4 of the step
-        if (__builtin_expect(key0 + kKeyBlock > P || bad, 0)) {   // uniform: the step has draft keys, or keys that are no numbers
-            const int first = key0 - P;   // its first key as a draft key; negative: it begins with committed keys
-            const uint32_t seen = first <= -kKeyBlock ? ~0u : (uint32_t)(first >= 0 ? mbits >> first : (mbits << -first) | ((1ull << -first) - 1));
-            const uint32_t vis = seen >> (4 * h), hit = (seen & bad) >> (4 * h);
+        // V scales in the order of the contraction: slots 8 h + p of product u are keys 16 u + 4 h + p, and 8 further on for p >= 4
+        half8v vs[2];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int bit = 8 * (i >> 2) + (i & 3);
-                sc[i] = (vis >> bit) & 1u ? ((hit >> bit) & 1u ? __builtin_nanf("") : sc[i]) : -__builtin_inff();
+        for (int u = 0; u < 2; ++u) {
+            u32x4 s0 = *reinterpret_cast<const u32x4 *>(scales + 32 + 16 * u + 4 * h), s1 = *reinterpret_cast<const u32x4 *>(scales + 40 + 16 * u + 4 * h);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                if (bad) {
+                    if ((s0[p] & 0x7FFFu) >= kHalfInf) s0[p] = 0;
+                    if ((s1[p] & 0x7FFFu) >= kHalfInf) s1[p] = 0;
+                }
+                vs[u][p] = __builtin_bit_cast(_Float16, (uint16_t)s0[p]);
+                vs[u][4 + p] = __builtin_bit_cast(_Float16, (uint16_t)s1[p]);
             }
+        }
+        settled(sc);
+        float s[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = sc[i];   // key 8 (i / 4) + 4 h + i % 4 of the step
+        uint32_t seen = ~0u;
+        if (key0 + kKeyBlock > P) {   // uniform: the step has draft keys; its first key is draft key `first` (negative: begins with committed keys)
+            const int first = key0 - P;
+            seen = (uint32_t)(first >= 0 ? mbits >> first : (mbits << -first) | ((1ull << -first) - 1));
+            const uint32_t vis = seen >> (4 * h);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = ((vis >> (8 * (i >> 2) + (i & 3))) & 1u) ? s[i] : -__builtin_inff();
             uint32_t by_any = seen;
 #pragma unroll
             for (int off = 1; off < kWaveRows; off <<= 1) by_any |= (uint32_t)__shfl_xor((int)by_any, off, 64);
-            // V of this step; newer: the next step (9) and the K of the one after (5)
-            if (next2) asm volatile("s_waitcnt vmcnt(14)" ::: "memory");
-            else if (next) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
-            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             clear_codes(mine + buf * kWaveBuf + kWaveTile, ~by_any, lane);
         }
+        if (bad) {   // uniform, rare
+            const uint32_t hit = (seen & bad) >> (4 * h);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = ((hit >> (8 * (i >> 2) + (i & 3))) & 1u) ? __builtin_nanf("") : s[i];
+        }
         // the scale is positive (checked by the host): the largest raw score is the largest scaled one
-        const float m_a = max_of_three(max_of_three(sc[0], sc[1], sc[2]), max_of_three(sc[3], sc[4], sc[5]), max_of_three(sc[6], sc[7], sc[8]));
-        const float m_b = max_of_three(max_of_three(sc[9], sc[10], sc[11]), max_of_three(sc[12], sc[13], sc[14]), sc[15]);
+        const float m_a = max_of_three(max_of_three(s[0], s[1], s[2]), max_of_three(s[3], s[4], s[5]), max_of_three(s[6], s[7], s[8]));
+        const float m_b = max_of_three(max_of_three(s[9], s[10], s[11]), max_of_three(s[12], s[13], s[14]), s[15]);
         const float m_step = half_wave_max(max_of_two(m_a, m_b)) * a.scale_log2e;
-        // Running maxima are left behind the true ones by up to kBehind: the probabilities reach 2^kBehind then, which fp16 and the sums hold as well
-        // as 1, and sums and outputs are rescaled a few times in all, not in most steps.
         if (__builtin_expect(__any(m_step > m_run + kBehind), 0)) {
             const float m_new = m_step > m_run + kBehind ? m_step : m_run;
             const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
@@ -249,20 +251,17 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
             for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
         }
         half8v pb[2];
-        float sums[2] = {l_run, 0.f};   // of the rounded probabilities, as the products see them: two per instruction
+        float sums[2] = {l_run, 0.f};
         const half2v ones = {(_Float16)1.f, (_Float16)1.f};
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-            const half2v p = {(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2e, -m_run)),
-                              (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i + 1], a.scale_log2e, -m_run))};
+            const half2v p = {(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2e, -m_run)),
+                              (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], a.scale_log2e, -m_run))};
             pb[i >> 3][i & 7] = p[0];
             pb[i >> 3][(i & 7) + 1] = p[1];
             sums[(i >> 1) & 1] = __builtin_amdgcn_fdot2(p, ones, sums[(i >> 1) & 1], false);
         }
         l_run = sums[0] + sums[1];
-        if (next2) asm volatile("s_waitcnt vmcnt(14)" ::: "memory");
-        else if (next) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         const uint32_t vtile = lds_address(tiles + kWaveTile);
         u32x2 w[8];
         auto read_v = [&](auto f) {
@@ -289,33 +288,23 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
         product(std::integral_constant<int, 5>{});
         product(std::integral_constant<int, 6>{});
         product(std::integral_constant<int, 7>{});
-        if (next2) request_v(step + 2 * kWaves, buf);
-        step += kWaves;
+        step = next;
         buf ^= 1;
     }
 
-    // The states of the wavefronts that had a step meet in LDS; the weights are worked out once per (row, wavefront)
-    if (__any(mbits == 0)) {   // padding
-        if (mbits == 0) m_run = kLowest, l_run = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[dt][i] = mbits == 0 ? 0.f : o[dt][i];
-    }
+    // The states of the eight wavefronts meet in LDS; the weights are worked out once per (row, wavefront)
     l_run += __shfl_xor(l_run, 32, 64);
-    const int walked = min(b1 - b0, kWaves);
+    if (reaches_draft && mbits == 0) l_run = kPaddingMark;
     __syncthreads();   // every wavefront has left its tiles
     uint8_t *const ex = lds + wave * kExWave;
     float2v *const state = reinterpret_cast<float2v *>(lds + kWaveState), *const weights = reinterpret_cast<float2v *>(lds + kWaveWeights);
     if (h == 0) state[c * kWaves + wave] = (float2v){m_run, l_run};
-    if (wave < walked && c < tile.rows) {
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
+    for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-                *reinterpret_cast<float4v *>(ex + c * kExRow + (8 * dt + 2 * b + h) * 16) =
-                    (float4v){o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]};
-    }
+        for (int b = 0; b < 4; ++b)
+            *reinterpret_cast<float4v *>(ex + c * kExRow + (8 * dt + 2 * b + h) * 16) =
+                (float4v){o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]};
     __syncthreads();
     auto row_max = [&](int row) {
         float m_all = kLowest;
@@ -326,7 +315,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
     if (tid < kWaveRows * kWaves) {
         const float2v me = state[tid];
         const float wgt = __builtin_amdgcn_exp2f(me[0] - row_max(tid / kWaves));
-        weights[tid] = (float2v){wgt, wgt * me[1]};
+        weights[tid] = me[1] < 0.f ? (float2v){0.f, kPaddingMark} : (float2v){wgt, wgt * me[1]};
     }
     __syncthreads();
     const bool last = a.nsplit == 1;
@@ -336,16 +325,18 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
     for (int it = 0; it < 2; ++it) {   // thread t: four consecutive outputs of a row, 32 threads per row
         const int item = tid + it * (64 * kWaves);
         const int rho = item >> 5, quad = item & 31;
-        if (rho >= tile.rows) continue;
         float4v val = {0.f, 0.f, 0.f, 0.f};
         float l_all = 0.f;
-        for (int w = 0; w < walked; ++w) {
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
             const float2v wl = weights[rho * kWaves + w];
             l_all += wl[1];
             val += wl[0] * *reinterpret_cast<const float4v *>(lds + w * kExWave + rho * kExRow + quad * 16);
         }
+        if (rho >= tile.rows) continue;
+        if (l_all < 0.f) val = (float4v){0.f, 0.f, 0.f, 0.f}, l_all = kPaddingMark;
         if (last) {
-            val *= l_all == 0.f ? 0.f : 1.f / l_all;   // a row that sees no key: zeros
+            if (l_all > 0.f || l_all != l_all) val *= 1.f / l_all;
             typedef _Float16 half4v __attribute__((ext_vector_type(4)));
             half4v hv = {(_Float16)val[0], (_Float16)val[1], (_Float16)val[2], (_Float16)val[3]};
             int qrow, head;
@@ -367,7 +358,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
     __syncthreads();
     if (ticket_sh != (uint32_t)(a.nsplit - 1)) return;
     if (tid == 0) __hip_atomic_store(&a.tickets[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    merge_tile<kWaveRows>(unit_o, unit_ml, a.out, tid, 64 * kWaves, tile, a.nsplit);
+    merge_tile<kWaveRows, true>(unit_o, unit_ml, a.out, tid, 64 * kWaves, tile, a.nsplit);
 }
 
 // ---- taller row tiles: K and V tiles turned into fp16 once and shared --------------------------------------
@@ -420,10 +411,13 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_shared_kernel(const
 
     __shared__ uint64_t row_bits[kRowsPad];
     __shared__ uint32_t bad_keys[2][kWaves];   // [buffer][wavefront]: keys whose K or V scale, of the ones it turned, is no number
-    uint32_t mask_byte[8];
-    const int mcol = min(lane, M - 1);
+    const bool reaches_draft = b1 * kKeyBlock > P;   // uniform over the workgroup
+    uint32_t mask_byte[8] = {};
+    if (reaches_draft) {
+        const int mcol = min(lane, M - 1);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mask_byte[i] = a.mask[(size_t)min(wave * 8 + i, M - 1) * M + mcol];
+        for (int i = 0; i < 8; ++i) mask_byte[i] = a.mask[(size_t)min(wave * 8 + i, M - 1) * M + mcol];
+    }
     half8v qf[8];   // lane (c, h): elements 16 j + 8 h .. of its row
     {
         const _Float16 *row = a.q + ((size_t)my_row * a.Hq + my_head) * kHeadDim + 8 * h;
@@ -460,16 +454,16 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_shared_kernel(const
     };
     fetch(std::integral_constant<int, 0>{});
     fetch(std::integral_constant<int, 1>{});
+    uint64_t mbits = 0, any_bits = 0;   // draft keys that this row sees, and that any row sees
+    if (reaches_draft) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        asm volatile("" : "+v"(mask_byte[i]));
-        const uint64_t bits = __ballot(mask_byte[i] != 0 && wave * 8 + i < M && lane < M);
-        if (lane == i) row_bits[wave * 8 + i] = bits;
-    }
-    __syncthreads();
-    const uint64_t mbits = row_bits[my_row];   // draft keys that this row sees; none: padding, which sees nothing at all
-    uint64_t any_bits = 0;                     // draft keys that any row sees
-    if (b1 * kKeyBlock > P) {   // uniform over the workgroup: the range has draft keys
+        for (int i = 0; i < 8; ++i) {
+            asm volatile("" : "+v"(mask_byte[i]));
+            const uint64_t bits = __ballot(mask_byte[i] != 0 && wave * 8 + i < M && lane < M);
+            if (lane == i) row_bits[wave * 8 + i] = bits;
+        }
+        __syncthreads();
+        mbits = row_bits[my_row];
         any_bits = row_bits[lane];   // rows beyond M are clear
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) any_bits |= (uint64_t)__shfl_xor((unsigned long long)any_bits, off, 64);
@@ -569,8 +563,6 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_shared_kernel(const
         meet();
     };
     const int plain_end = min(P, b1 * kKeyBlock);   // keys before it are visible to every row, and this workgroup's
-    // Running maxima are left behind the true ones by up to kBehind: the probabilities reach 2^kBehind then, which fp16 and the sums hold as well as 1,
-    // and sums and outputs are rescaled a few times in all, not in most steps.
     auto softmax = [&](auto buf_tag, int t) {
         constexpr int BUF = decltype(buf_tag)::value;
         const int key0 = (b0 + t * WK + kw) * kKeyBlock;
@@ -646,16 +638,10 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_shared_kernel(const
 #pragma unroll
     for (int f = 0; f < 8; ++f) o[f & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[2 * (f & 3) + (f >> 2)], pb[f >> 2], o[f & 3], 0, 0, 0);   // the last round's values
     if (!behind) meet();
-    if (__any(mbits == 0)) {   // padding
-        if (mbits == 0) m_run = kLowest, l_run = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[dt][i] = mbits == 0 ? 0.f : o[dt][i];
-    }
 
     // the key groups' states of each row meet in LDS
     l_run += __shfl_xor(l_run, 32, 64);
+    if (reaches_draft && mbits == 0) l_run = kPaddingMark;
     __syncthreads();   // every wavefront has left the tiles
     uint8_t *const ex = lds + wave * kExWave;
     float2v *const state = reinterpret_cast<float2v *>(lds + kWaves * kExWave);   // [wavefront][row]
@@ -689,8 +675,9 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_shared_kernel(const
             val += wgt * *reinterpret_cast<const float4v *>(lds + (w * WR + group) * kExWave + row * kExRow + quad * 16);
         }
         if (rho >= tile.rows) continue;
+        if (of[0][1] < 0.f) val = (float4v){0.f, 0.f, 0.f, 0.f}, l_all = kPaddingMark;
         if (last) {
-            val *= l_all == 0.f ? 0.f : 1.f / l_all;
+            if (l_all > 0.f || l_all != l_all) val *= 1.f / l_all;
             typedef _Float16 half4v __attribute__((ext_vector_type(4)));
             half4v hv = {(_Float16)val[0], (_Float16)val[1], (_Float16)val[2], (_Float16)val[3]};
             int qrow, head;
@@ -733,15 +720,18 @@ __global__ __launch_bounds__(256) void tree_attn_kv8_merge_kernel(const float *_
     for (int s = 1; s < NS; ++s) m_all = fmaxf(m_all, st[s][0]);
     float den = 0.f;
     float4v num = {0.f, 0.f, 0.f, 0.f};
+    bool padding = false;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
+        padding |= st[s][1] < 0.f;
         const float wgt = s < nsplit ? __builtin_amdgcn_exp2f(st[s][0] - m_all) : 0.f;
         if (s < nsplit) {   // uniform
             den += wgt * st[s][1];
             num += wgt * os[s];
         }
     }
-    const float inv = den == 0.f ? 0.f : 1.f / den;
+    const float inv = padding || den == 0.f ? 0.f : 1.f / den;
+    if (padding) num = (float4v){0.f, 0.f, 0.f, 0.f};
     typedef _Float16 half4v __attribute__((ext_vector_type(4)));
     half4v hv = {(_Float16)(num[0] * inv), (_Float16)(num[1] * inv), (_Float16)(num[2] * inv), (_Float16)(num[3] * inv)};
     *reinterpret_cast<half4v *>(out + ((size_t)qrow * Hq + h) * kHeadDim + d4 * 4) = hv;
@@ -752,8 +742,8 @@ struct Kv8Plan { int row_groups, tile_rows, tiles_per_kv, ranges, fused, tenths;
 static int kv8_steps(int M, int P) { return (P + M + kKeyBlock - 1) / kKeyBlock; }
 
 // The number of ranges with the smallest estimate, at most one workgroup per CU (which also bounds the partial results).  Estimates are in tenths of
-// a microsecond, from a sweep over 1 to 64 query rows, 8 to 64 query heads, 4 to 16 KV heads and 64 to 131072 keys, both formats: `base` for a kernel
-// that walks one round, `round` more for every further one; a merge by a second kernel 35, by the tile's last workgroup 5 and 1 per 10 rows read.
+// a microsecond, from a sweep over 1 to 64 query rows, 8 to 64 query heads, 4 to 16 KV heads and 64 to 131072 keys, both formats: `base` and `round`
+// for every round that a kernel walks; a merge by a second kernel 35, by the tile's last workgroup 5 and 1 per 10 rows read.
 static Kv8Plan kv8_cut(int pairs, int Hkv, int steps, int row_groups, int base, int round)
 {
     Kv8Plan p;
@@ -774,16 +764,22 @@ static Kv8Plan kv8_cut(int pairs, int Hkv, int steps, int row_groups, int base, 
     return p;
 }
 
-// A round of the wave kernel takes up to 2 us (256 keys of 32 rows; it turns every code into a number once per 32 rows), one of the shared kernel 1.1 us
-// (64 keys of 128 rows, the same work), but that starts and ends more slowly.  Measured, wave / shared kernel, us: 37 rows of 28/4 heads over 3333
-// keys 15.4 / 18.4, over 60000 keys 69.7 / 65.1; 60 rows of 64/8 heads over 64 keys 9.8 / 13.2, over 2048 19.3 / 19.6, over 16001 76 / 51 (int8) and
-// 64 / 50 (e4m3); 16 rows of 64/8 heads over 8000 keys 20.7 / 22.3, over 32000 44 / 35 (int8); 64 rows of 16/16 heads over 16000 keys 26 / 31.
-static Kv8Plan kv8_plan(int M, int P, int Hq, int Hkv)
+// A round of the wave kernel takes 1.8 us with int8 codes and 1.4 with e4m3 (256 keys of 32 rows; it turns every code into a number once per 32 rows), one
+// of the shared kernel 1.1 us (64 keys of 128 rows, the same work), but that starts and ends more slowly.  Measured, wave and shared kernel, us:
+//   rows, heads, keys        int8           e4m3
+//   60, 64/8,  2048          18.1  19.5     15.8  19.2
+//   60, 64/8,  4096          24.9  22.7     21.5  22.4
+//   60, 64/8, 16001          66.2  48.7     54.9  47.6
+//   37, 28/4, 16000          27.5  28.8     23.8  28.3
+//   37, 28/4, 60000          72.3  63.7     59.7  62.4
+//   16, 64/8, 32000          41.3  33.7     35.4  33.1
+//   64, 16/16, 16000         27.4  29.7     24.7  29.8
+static Kv8Plan kv8_plan(int M, int P, int Hq, int Hkv, int format)
 {
     const int pairs = Hq / Hkv * M, steps = kv8_steps(M, P);
-    const Kv8Plan wave = kv8_cut(pairs, Hkv, steps, 1, 92, 18);
+    const Kv8Plan wave = kv8_cut(pairs, Hkv, steps, 1, 80, format == kInt8 ? 18 : 14);
     if (pairs <= kWaveRows) return wave;   // one row group would be at work
-    const Kv8Plan shared = kv8_cut(pairs, Hkv, steps, kRowGroups, 120, 11);
+    const Kv8Plan shared = kv8_cut(pairs, Hkv, steps, kRowGroups, 110, 11);
     return shared.tenths < wave.tenths ? shared : wave;
 }
 
@@ -850,7 +846,7 @@ int tree_verify_attn_kv8(const void *q, const void *k, const void *v, const void
         workspace_misaligned(workspace))
         return W4A16_EALIGN;
     if (!workspace || workspace_bytes < tree_verify_attn_kv8_workspace_bytes(M, P, Hq, Hkv, D)) return W4A16_EWORKSPACE;
-    const Kv8Plan pl = kv8_plan(M, P, Hq, Hkv);
+    const Kv8Plan pl = kv8_plan(M, P, Hq, Hkv, format);
     const int units = Hkv * pl.tiles_per_kv, steps = kv8_steps(M, P);
     Kv8Args a;
     a.by_tiles = divider(pl.tiles_per_kv);

@@ -238,6 +238,7 @@ def test_graph_replays_equal_the_eager_calls():
 # many rows over a long prefix: taller row tiles, whose codes become fp16 numbers once for 128 rows
 TALL = [
     (60, 8192, 64, 8),      # 480 rows per KV head
+    (60, 16001, 64, 8),
     (64, 8191, 64, 8),      # draft keys from the last key of a step to the third step on
     (64, 6002, 64, 8),      # the last step holds two keys
     (37, 24000, 28, 4),     # 259 rows: tiles of 87
@@ -306,3 +307,21 @@ def test_rows_of_padding_are_zero_whatever_the_prefix_holds(M, P, Hq, Hkv, fmt):
     c.q[1, 0], c.q[M - 1, 0, 5], c.q[M - 2, 0, 5] = np.inf, np.nan, -np.inf
     out = c.run()
     assert (out[[1, M - 2, M - 1]] == 0).all() and np.isnan(out[0]).any()
+
+
+def test_nan_keys_and_hidden_rows_under_many_rows_of_e4m3():
+    """as the three above in one, over a prefix that makes the tall tiles worth it for e4m3 as well"""
+    M, P, n = 60, 16001, 44
+    c = Call(150, M, P, 64, 8, B.KV8_E4M3, tree="random")
+    c.mask[n:], c.mask[:, n:] = 0, 0
+    for at, head in ((7, 3), (P + 20, 5)):
+        c.ks[at, head], c.k[at, head] = np.nan, 0
+    out = c.run()
+    c.check(out)
+    lost = np.isnan(out[:n]).any(axis=(0, 2))
+    assert lost[24:32].all() and lost[40:48].all() and lost.sum() == 16 and (out[n:] == 0).all()
+    rng = np.random.default_rng(M)
+    for codes, scales in ((c.k, c.ks), (c.v, c.vs)):
+        codes[P + n:] = rng.choice(np.array([0x7F, 0xFF, 0x80, 0x7E], dtype=np.uint8), codes[P + n:].shape)
+        scales[P + n:] = rng.choice(np.array([np.nan, np.inf, -np.inf, 65504.0, 1.0], dtype=np.float16), scales[P + n:].shape)
+    np.testing.assert_array_equal(c.run().view(np.uint16), out.view(np.uint16))
