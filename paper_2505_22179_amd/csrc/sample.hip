@@ -13,9 +13,11 @@
 //   sample_draw_kernel   exact weight of what certainly stays, by segments of 512 tokens, and a list of the tokens in those few bins; the row's last
 //                        workgroup sorts the list, which gives the exact cut, draws the segment and then the token inside it
 // A list of more than kList tokens (thousands of nearly equal logits) is given up: the last workgroup then finds the cut by digits of the logits.
-// Measured, the three kernels: 1 row of 32000 tokens, top-k 4 + 8 + 11 us; 7 rows of 128256, top-p 4 + 10 + 16; 60 rows of 128256, all limits
+// Measured, the three kernels: 1 row of 32000 tokens, top-k 4 + 8 + 10 us; 7 rows of 128256, top-p 4 + 9 + 16; 60 rows of 128256, all limits
 // 8 + 14 + 20, where reading the logits once takes 6.  What bounds them: for few rows the chain of dependent steps (three launches, two meetings of a
 // row's workgroups, each several trips to memory); for many the vector units, which put every token in its bin and weigh the kept ones in fp64.
+// One kernel for the first two, with bins of each workgroup's own width that its row's last one puts together, was no faster (21.0, 30.0 and 39.6 us in
+// all, against 21.6, 28.2 and 41.9).
 #include "internal.h"
 #include "devscope.h"
 
@@ -110,55 +112,12 @@ struct SampleArgs {
     unsigned long long *lists;       // [M][groups][kList]
     uint32_t *tickets;               // [2 M]
 };
-struct ChunkTop { float top; int32_t at; float least; int32_t unused; };
+// a chunk's largest logit and its first token (order_of; that of -inf and kNoToken if it has none), and its smallest number (~order_key)
+struct ChunkTop { unsigned long long order, deep; };
+__device__ __forceinline__ ChunkTop chunk_top(float top, int at, float least) { return {order_of(top, at), (uint32_t)~order_key(least)}; }
 // weights of all above the first border bin, and of all between the border bins and the k-th token's; the length of the group's list
 struct GroupMass { unsigned long long above, between, listed, unused; };
 struct RowCut { int32_t first, last, k_bin, above_k; };   // border bins of top-p (first .. last), bin of the k-th token (kNoBin: none), tokens in the bins above it
-
-// the rule of row m and, in at, the first token of its largest logit (kNoToken: the row has no token); every lane of a wavefront calls it
-__device__ __forceinline__ RowRule row_rule(const SampleArgs &a, int m, int &at)
-{
-    const int lane = threadIdx.x & 63;
-    // all loads together: a limit that is not given reads the uniform number instead
-    float t = (a.temperature ? a.temperature : a.uniform)[m], p = (a.top_p ? a.top_p : a.uniform)[m], min_p = (a.min_p ? a.min_p : a.uniform)[m];
-    int k = (a.top_k ? a.top_k : reinterpret_cast<const int32_t *>(a.uniform))[m];
-    if (!a.temperature) t = 1.f;
-    if (!a.top_k) k = 0;
-    if (!a.top_p) p = 1.f;
-    if (!a.min_p) min_p = 0.f;
-    ChunkTop c = {-__builtin_inff(), kNoToken, __builtin_inff(), 0};
-    if (lane < a.chunks) c = a.tops[m * a.chunks + lane];
-#pragma unroll
-    for (int off = 1; off < kChunks; off <<= 1) {
-        const float v = __shfl_xor(c.top, off, 64), least = __shfl_xor(c.least, off, 64);
-        const int j = __shfl_xor(c.at, off, 64);
-        if (v > c.top || (v == c.top && j < c.at)) c.top = v, c.at = j;
-        c.least = fminf(c.least, least);
-    }
-    c.top = __shfl(c.top, 0, 64);   // lanes beyond kChunks hold nothing
-    c.least = __shfl(c.least, 0, 64);
-    at = __shfl(c.at, 0, 64);
-    RowRule r;
-    r.u = a.uniform[m];
-    r.top = c.top;
-    r.greedy = !(t > 0.f) || k == 1 || p <= 0.f || min_p > 1.f;
-    r.inv_t = r.greedy ? 0.0 : 1.0 / (double)t;
-    r.k = k > 0 && k < a.V ? k : 0;
-    r.p = p < 1.f ? (double)p : 2.0;
-    r.min_w = min_p > 0.f ? (double)min_p : 0.0;
-    // the bins span the distances that there are, so that they stay narrow at high temperatures
-    r.deepest = r.greedy ? 0.f : fmaxf((float)(0.5 * kFarthest * (double)t), 0x1p-149f);
-    const float span = fminf(r.depth(c.least), r.deepest);
-    r.bins_per = span > 0.f ? fminf((float)kBins / span, 3.0e38f) : 0.f;
-    return r;
-}
-
-// the uniform number as a rank of weight units below total
-__device__ __forceinline__ uint64_t drawn_rank(float u, uint64_t total)
-{
-    const uint64_t r = u > 0.f ? (uint64_t)(fminf(u, 0x1.fffffep-1f) * (double)total) : 0;
-    return r < total ? r : total - 1;
-}
 
 // Inclusive sum over a wavefront's lanes, on the vector ALU: within rows of 16 lanes by shifts, then over rows.
 template <int CONTROL, int ROWS>
@@ -182,6 +141,57 @@ __device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane)   // lane unif
 {
     return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
 }
+// the greatest of a wavefront's lanes, in each of them
+__device__ __forceinline__ uint64_t max_wave(uint64_t v)
+{
+    auto join = [&](uint64_t o) { v = o > v ? o : v; };
+    join(moved<0x111, 0xf>(v));
+    join(moved<0x112, 0xf>(v));
+    join(moved<0x114, 0xf>(v));
+    join(moved<0x118, 0xf>(v));
+    join(moved<0x142, 0xa>(v));
+    join(moved<0x143, 0xc>(v));
+    return of_lane(v, 63);
+}
+
+// the rule of row m and, in at, the first token of its largest logit (kNoToken: the row has no token); every lane of a wavefront calls it
+__device__ __forceinline__ RowRule row_rule(const SampleArgs &a, int m, int &at)
+{
+    const int lane = threadIdx.x & 63;
+    // all loads together: a limit that is not given reads the uniform number instead
+    float t = (a.temperature ? a.temperature : a.uniform)[m], p = (a.top_p ? a.top_p : a.uniform)[m], min_p = (a.min_p ? a.min_p : a.uniform)[m];
+    int k = (a.top_k ? a.top_k : reinterpret_cast<const int32_t *>(a.uniform))[m];
+    if (!a.temperature) t = 1.f;
+    if (!a.top_k) k = 0;
+    if (!a.top_p) p = 1.f;
+    if (!a.min_p) min_p = 0.f;
+    ChunkTop c = chunk_top(-__builtin_inff(), kNoToken, __builtin_inff());
+    if (lane < a.chunks) c = a.tops[m * a.chunks + lane];
+    const uint64_t order = max_wave(c.order);
+    const float least = order_number(~(uint32_t)max_wave(c.deep));
+    at = (int32_t)~(uint32_t)order;
+    RowRule r;
+    r.u = a.uniform[m];
+    r.top = order_number((uint32_t)(order >> 32));
+    r.greedy = !(t > 0.f) || k == 1 || p <= 0.f || min_p > 1.f;
+    r.inv_t = r.greedy ? 0.0 : 1.0 / (double)t;
+    r.k = k > 0 && k < a.V ? k : 0;
+    r.p = p < 1.f ? (double)p : 2.0;
+    r.min_w = min_p > 0.f ? (double)min_p : 0.0;
+    // the bins span the distances that there are, so that they stay narrow at high temperatures
+    r.deepest = r.greedy ? 0.f : fmaxf((float)(0.5 * kFarthest * (double)t), 0x1p-149f);
+    const float span = fminf(r.depth(least), r.deepest);
+    r.bins_per = span > 0.f ? fminf((float)kBins / span, 3.0e38f) : 0.f;
+    return r;
+}
+
+// the uniform number as a rank of weight units below total
+__device__ __forceinline__ uint64_t drawn_rank(float u, uint64_t total)
+{
+    const uint64_t r = u > 0.f ? (uint64_t)(fminf(u, 0x1.fffffep-1f) * (double)total) : 0;
+    return r < total ? r : total - 1;
+}
+
 // One 64-bit value as two device-scope halves: read by another workgroup of the same kernel.
 __device__ __forceinline__ void store_shared(unsigned long long *p, uint64_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ uint64_t load_shared(unsigned long long *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
@@ -235,24 +245,24 @@ __global__ __launch_bounds__(kSampleThreads) void sample_top_kernel(const Sample
         const int i = first + e * kSampleThreads + tid;
         v[e] = i < a.V ? x[i] : -__builtin_inff();
     }
-    ChunkTop c = {-__builtin_inff(), kNoToken, __builtin_inff(), 0};
+    float top = -__builtin_inff(), least = __builtin_inff();
+    int at = kNoToken;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {   // NaN and -inf are no tokens
-        if (v[e] > c.top) c.top = v[e], c.at = first + e * kSampleThreads + tid;
-        if (v[e] > -__builtin_inff()) c.least = fminf(c.least, v[e]);
+        if (v[e] > top) top = v[e], at = first + e * kSampleThreads + tid;
+        if (v[e] > -__builtin_inff()) least = fminf(least, v[e]);
     }
     __shared__ ChunkTop of_wave[kSampleWaves];
-    auto join = [&](const ChunkTop &o) {
-        if (o.top > c.top || (o.top == c.top && o.at < c.at)) c.top = o.top, c.at = o.at;
-        c.least = fminf(c.least, o.least);
-    };
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) join({__shfl_xor(c.top, off, 64), __shfl_xor(c.at, off, 64), __shfl_xor(c.least, off, 64), 0});
+    ChunkTop c = chunk_top(top, at, least);
+    c = {max_wave(c.order), max_wave(c.deep)};
     if (lane == 0) of_wave[tid >> 6] = c;
     __syncthreads();
     if (tid == 0) {
 #pragma unroll
-        for (int w = 1; w < kSampleWaves; ++w) join(of_wave[w]);
+        for (int w = 1; w < kSampleWaves; ++w) {
+            c.order = of_wave[w].order > c.order ? of_wave[w].order : c.order;
+            c.deep = of_wave[w].deep > c.deep ? of_wave[w].deep : c.deep;
+        }
         a.tops[m * a.chunks + blockIdx.x] = c;
     }
 }
