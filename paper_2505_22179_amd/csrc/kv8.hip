@@ -264,7 +264,7 @@ int w4a16_kv8_read(const void *k, const void *v, const void *k_scale, const void
     if (rows == 0) return W4A16_OK;
     const int lanes = D / 8, whole = kReadThreads * kReadPasses / lanes;   // at least 16 heads
     const size_t heads = (size_t)rows * Hkv, groups = (heads + whole - 1) / whole;
-    if (groups > 0x7FFFFFFFu) return W4A16_EUNSUP;
+    if (groups >= (1u << 24)) return W4A16_EUNSUP;   // 2^32 threads: more than 128 GiB of codes
     hipLaunchKernelGGL(format == kInt8 ? kv8_read_kernel<kInt8> : kv8_read_kernel<kE4m3>, dim3((unsigned)groups, 2), dim3(kReadThreads), 0,
                        (hipStream_t)stream, (const uint8_t *)k, (const uint8_t *)v, (const _Float16 *)k_scale, (const _Float16 *)v_scale,
                        (_Float16 *)k_out, (_Float16 *)v_out, (size_t)first * Hkv, heads, whole, lanes);

@@ -325,3 +325,67 @@ def test_nan_keys_and_hidden_rows_under_many_rows_of_e4m3():
         codes[P + n:] = rng.choice(np.array([0x7F, 0xFF, 0x80, 0x7E], dtype=np.uint8), codes[P + n:].shape)
         scales[P + n:] = rng.choice(np.array([np.nan, np.inf, -np.inf, 65504.0, 1.0], dtype=np.float16), scales[P + n:].shape)
     np.testing.assert_array_equal(c.run().view(np.uint16), out.view(np.uint16))
+
+
+@pytest.mark.parametrize("M,Hq", [(3, 64), (16, 512)])   # one row tile per KV head, and tiles of 128 rows
+def test_a_cache_of_more_than_4_gib(M, Hq):
+    """P = 560000 rows of 64 heads: 4.6 GB of K codes and as much of V.  All keys are zero but a few, on both sides of the 4 GiB boundary, and the draft's:
+    append, read, attention, acceptance."""
+    P, Hkv, fmt = 560000, 64, B.KV8_INT8
+    print(f"attn_kv8 long cache M={M} Hq={Hq}", flush=True)
+    T, edge = P + M, 2 ** 32 // (Hkv * D)
+    rng = np.random.default_rng(M)
+    k, v = (torch.zeros(T, Hkv, D, dtype=torch.uint8, device=DEV) for _ in range(2))
+    ks, vs = (torch.ones(T, Hkv, dtype=torch.float16, device=DEV) for _ in range(2))
+    at = np.array([0, 1, edge - 1, edge, edge + 1, P - 1])
+    small = Call(160, 1, len(at) - 1, Hkv, Hkv, fmt)
+    for big, part in ((k, small.k), (v, small.v), (ks, small.ks * np.float16(3)), (vs, small.vs)):
+        big[torch.from_numpy(at).to(DEV)] = dev(part)
+    qkv = (rng.standard_normal((M, (Hq + 2 * Hkv) * D)) * 2).astype(np.float16)
+    pos, (cos, sin) = np.arange(M, dtype=np.int32), I.make_rope_tables(M, D)
+    q = torch.empty(M, Hq, D, dtype=torch.float16, device=DEV)
+    B.rope_append_kv8(dev(qkv), None, None, 0.0, dev(pos), dev(cos), dev(sin), M, q, k, v, ks, vs, fmt, M, P, Hq, Hkv, D)
+    draft = qkv.reshape(M, -1, D)[:, Hq + Hkv:]
+    codes, scales = R.kv8_quantise(draft, fmt)
+    np.testing.assert_array_equal(v[P:].cpu().numpy(), codes)
+    np.testing.assert_array_equal(vs[P:].cpu().numpy(), scales)
+    # read: the last rows
+    rows = P + M - (edge - 2)
+    k16, v16 = torch.empty(rows, Hkv, D, dtype=torch.float16, device=DEV), torch.empty(rows, Hkv, D, dtype=torch.float16, device=DEV)
+    B.w4a16_kv8_read(k, v, ks, vs, fmt, edge - 2, rows, Hkv, D, k16, v16)
+    seen = np.concatenate([at, P + np.arange(M)])
+    take = lambda t: t[torch.from_numpy(seen).to(DEV)].cpu().numpy()
+    kk, vv = R.kv8_values(take(k), take(ks), fmt), R.kv8_values(take(v), take(vs), fmt)
+    late = seen >= edge - 2
+    np.testing.assert_array_equal(k16[torch.from_numpy(seen[late] - (edge - 2)).to(DEV)].cpu().numpy(), kk[late].astype(np.float16))
+    np.testing.assert_array_equal(v16[torch.from_numpy(seen[late] - (edge - 2)).to(DEV)].cpu().numpy(), vv[late].astype(np.float16))
+    assert not (k16[0].any() or v16[0].any())
+    del k16, v16
+    # attention: a row sees the committed rows -- P - 6 of them zeros -- and the draft up to itself
+    mask = I.chain_tree(M)[2]
+    out = torch.empty(M, Hq, D, dtype=torch.float16, device=DEV)
+    B.tree_verify_attn_kv8(q, k, v, ks, vs, fmt, dev(mask), out, M, P, Hq, Hkv, D, D ** -0.5, B.new_workspace(B.tree_verify_attn_kv8_workspace_bytes(M, P, Hq, Hkv, D)))
+    out, qh = out.cpu().numpy().astype(np.float64), q.cpu().numpy().astype(np.float64)
+    rep, reach = Hq // Hkv, 0
+    for i in range(M):
+        for head in range(0, Hq, max(1, Hq // 16) + 1):
+            g = head // rep
+            visible = np.concatenate([np.ones(len(at), dtype=bool), mask[i] != 0])
+            s = (kk[visible, g] @ qh[i, head]) * D ** -0.5
+            m = max(s.max(), 0.0)
+            w = np.exp(s - m)
+            den = w.sum() + (P - len(at)) * np.exp(-m)
+            want, spread = (w / den) @ vv[visible, g], (w / den) @ np.abs(vv[visible, g])
+            qk = np.abs(qh[i, head]).sum() * np.abs(kk[visible, g]).max() * D ** -0.5
+            # as at the top; a zero key's probability of exp(-m), 2^-11 of it off in the sum as well
+            tol = spread * (2 * 2.0 ** -11 * 1.01 + 2 * 128 * 2.0 ** -24 * min(qk, 64.0 * 8)) + np.abs(want) * 2.0 ** -11 + 2.0 ** -25 + T * 2.0 ** -25 * np.abs(vv[visible, g]).max() / T ** 0.5
+            assert (np.abs(out[i, head] - want) <= tol).all(), (i, head, np.abs(out[i, head] - want).max(), tol.min())
+            reach += np.abs(want).max() > 0.05
+    assert reach > M   # the planted rows do show
+    # acceptance moves rows beyond the boundary
+    parent, token = np.array([-1, 0, 0] + [2] * (M - 3), dtype=np.int32), np.arange(M, dtype=np.int32)
+    target = np.array([2] + [M + 5] * (M - 1), dtype=np.int32)
+    path, result = torch.empty(M, dtype=torch.int32, device=DEV), torch.empty(2, dtype=torch.int32, device=DEV)
+    third = [t[P + 2].clone() for t in (k, v, ks, vs)]
+    B.tree_accept_kv8(dev(parent), dev(token), dev(target), M, path, result, k, v, ks, vs, P, Hkv, D)
+    assert result.tolist() == [2, M + 5] and all(torch.equal(t[P + 1], w) for t, w in zip((k, v, ks, vs), third))

@@ -1,6 +1,7 @@
 """Host-only checks of the entry points around the 8-bit cache: bad arguments are refused before any GPU call."""
 import ctypes
 
+import numpy as np
 import pytest
 
 from paper_2505_22179_amd import binding as B
@@ -104,3 +105,9 @@ def test_lm_head_sample_refuses():
     for M in (1, 7, 64):
         for V in (1, 1000, 128256, 262144):
             assert 0 < B.lm_head_sample_workspace_bytes(M, V) <= B.lm_head_sample_workspace_bytes(64, 262144)
+
+
+def test_sample_workspace_serves_every_smaller_call():
+    Vs = (1, 511, 513, 4096, 4097, 8192, 32000, 65537, 128256, 200001, 262144)
+    sizes = np.array([[B.lm_head_sample_workspace_bytes(M, V) for V in Vs] for M in range(1, 65)])
+    assert (np.diff(sizes, axis=0) >= 0).all() and (np.diff(sizes, axis=1) >= 0).all()
