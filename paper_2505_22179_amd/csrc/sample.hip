@@ -43,15 +43,15 @@ __device__ __forceinline__ double exp_minus(double y)
     const double t = y * 1.4426950408889634074;
     const double n = rint(t);
     const double f = (n - t) * 0.69314718055994530942;
-    double r = 1.0 / 39916800.0;
-    r = fma(r, f, 1.0 / 3628800.0);
-    r = fma(r, f, 1.0 / 362880.0);
-    r = fma(r, f, 1.0 / 40320.0);
-    r = fma(r, f, 1.0 / 5040.0);
-    r = fma(r, f, 1.0 / 720.0);
-    r = fma(r, f, 1.0 / 120.0);
-    r = fma(r, f, 1.0 / 24.0);
-    r = fma(r, f, 1.0 / 6.0);
+    // the coefficients in scalar registers, as third operands: else every multiply-add of the chain copies one first
+    constexpr double c[10] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5};
+    double r = c[0];
+#pragma unroll
+    for (int i = 1; i < 9; ++i) {
+        double at = c[i];
+        asm("" : "+s"(at));
+        r = fma(r, f, at);
+    }
     r = fma(r, f, 0.5);
     r = fma(r, f, 1.0);
     r = fma(r, f, 1.0);
@@ -533,8 +533,10 @@ __device__ __forceinline__ void number_to_lds(const float *src, float *lds_base)
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, (__attribute__((address_space(3))) void *)lds_base, 4, 0, 0);
 }
 
-// A wavefront takes segments of 512 tokens, `rounds` of them; their logits come straight to LDS, two segments ahead, and are looked at in loops that are not
-// unrolled: code that runs once is fetched from memory, and unrolled over 16 tokens it took 2 us longer than the work.
+constexpr int kEarlyLds = kSampleWaves * 2 * kSegment * 4;   // two segments of each wavefront
+// A wavefront takes segments of 512 tokens, `rounds` of them; their logits come straight to LDS, two segments ahead, and are looked at in loops that are
+// hardly unrolled: code that runs once is fetched from memory, and unrolled over 16 tokens it took 2 us longer than the work.  (LDS of a size given at
+// the launch: before a read of an array that is declared with its size the compiler waits for every transfer under way.)
 __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const SampleArgs a)
 {
     const int tid = threadIdx.x, lane = tid & 63, m = blockIdx.y, V = a.V;
@@ -542,8 +544,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const Sampl
     const float *x = a.logits + (size_t)m * V;
     constexpr int kSteps = kSegment / 64;
     __shared__ unsigned long long list[kList];
-    __shared__ float4 early[kSampleWaves * 2 * kSegment / 4];
-    static_assert(sizeof(TailLds) <= sizeof(early), "the tail's LDS lies where the segments were");
+    extern __shared__ float4 early[];   // kEarlyLds bytes
+    static_assert(sizeof(TailLds) <= kEarlyLds, "the tail's LDS lies where the segments were");
     TailLds &tail = *reinterpret_cast<TailLds *>(early);
     __shared__ unsigned long long sums[2];
     __shared__ uint32_t listed;
@@ -582,7 +584,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const Sampl
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         const float *const here = mine + (round & 1) * kSegment + lane;
         uint64_t kept = 0;
-#pragma unroll 1
+#pragma unroll 2
         for (int e = 0; e < kSteps; ++e) {
             const float v = here[e * 64];
             const float d = r.depth(v);
@@ -825,7 +827,7 @@ int lm_head_sample(const float *logits, int M, int V, const float *temperature, 
     const auto grid = [M](int groups) { return dim3((unsigned)groups, (unsigned)M); };
     hipLaunchKernelGGL(sample_top_kernel, grid(a.chunks), dim3(kSampleThreads), 0, (hipStream_t)stream, a);
     if (top_k || top_p) hipLaunchKernelGGL(sample_bins_kernel, grid(a.bin_groups), dim3(kSampleThreads), 0, (hipStream_t)stream, a);
-    hipLaunchKernelGGL(sample_draw_kernel, grid(a.groups), dim3(kSampleThreads), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL(sample_draw_kernel, grid(a.groups), dim3(kSampleThreads), kEarlyLds, (hipStream_t)stream, a);
     return launch_status();
 }
 
