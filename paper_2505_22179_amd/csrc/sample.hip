@@ -13,8 +13,8 @@
 //   sample_draw_kernel   exact weight of what certainly stays, by segments of 512 tokens, and a list of the tokens in those few bins; the row's last
 //                        workgroup sorts the list, which gives the exact cut, draws the segment and then the token inside it
 // A list of more than kList tokens (thousands of nearly equal logits) is given up: the last workgroup then finds the cut by digits of the logits.
-// Measured, the three kernels: 1 row of 32000 tokens, top-k 4 + 8 + 10 us; 7 rows of 128256, top-p 4 + 9 + 16; 60 rows of 128256, all limits
-// 8 + 14 + 20, where reading the logits once takes 6.  What bounds them: for few rows the chain of dependent steps (three launches, two meetings of a
+// Measured, the three kernels: 1 row of 32000 tokens, top-k 4 + 8 + 9 us; 7 rows of 128256, top-p 4 + 9 + 16; 60 rows of 128256, all limits
+// 8 + 14 + 18, where reading the logits once takes 6.  What bounds them: for few rows the chain of dependent steps (three launches, two meetings of a
 // row's workgroups, each several trips to memory); for many the vector units, which put every token in its bin and weigh the kept ones in fp64.
 // One kernel for the first two, with bins of each workgroup's own width that its row's last one puts together, was no faster (21.0, 30.0 and 39.6 us in
 // all, against 21.6, 28.2 and 41.9).
@@ -681,45 +681,72 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const Sampl
         __shared__ uint32_t to_k_bin, staying;
         if (tid == 0) to_k_bin = 0, staying = 0;
         __syncthreads();
-        unsigned long long *const upto = tail.upto;
-        sort_list(list, tail, n, r, cut);
-        // weights down the list; its places where something ends are found by the entry ahead of them
-        auto logit = [&](uint32_t i) { return order_number((uint32_t)(list[i] >> 32)); };
-        auto bin_at = [&](uint32_t i) { return r.bin(r.depth(logit(i))); };
-        uint64_t so_far = 0;
-#pragma unroll 1
-        for (uint32_t i0 = 0; i0 < n; i0 += kSampleThreads) {
-            const uint32_t i = i0 + tid;
-            uint64_t to[1] = {0}, all[1];
-            if (i < n) {
-                to[0] = units(exp_minus(r.below(logit(i))));
-                if (bin_at(i) < cut.k_bin && (i + 1 == n || bin_at(i + 1) >= cut.k_bin)) to_k_bin = i + 1;   // one entry of all, or none
-            }
-            scan_block(to, all);
-            if (i < n) upto[i] = so_far + to[0];
-            so_far += all[0];
-        }
-        __syncthreads();
-        const uint32_t above_k_bin = to_k_bin;
-        const uint32_t allowed = cut.k_bin == kNoBin ? n : above_k_bin + (uint32_t)(r.k - cut.above_k);   // entries that top-k leaves, one at least
+        auto logit_of = [&](uint64_t o) { return order_number((uint32_t)(o >> 32)); };
         const bool apart = cut.k_bin > cut.last;   // tokens between the border bins and the k-th token's come before the latter
-        const double limit = r.p * (double)(all_above + all_between + upto[allowed - 1]);
-        auto stays = [&](uint32_t i) {   // holds for a first stretch of the list
-            if (i >= allowed) return false;
-            const uint64_t ahead = all_above + (i ? upto[i - 1] : 0) + (apart && i >= above_k_bin ? all_between : 0);
-            return r.p >= 1.0 || (double)ahead < limit || ahead == 0;
-        };
+        auto allowed_by_k = [&](uint32_t above_k_bin) { return cut.k_bin == kNoBin ? n : above_k_bin + (uint32_t)(r.k - cut.above_k); };   // one at least
+        auto stays_at = [&](uint64_t ahead, double limit) { return r.p >= 1.0 || (double)ahead < limit || ahead == 0; };   // holds for a first stretch of the list
+        if (n <= 64) {
+            // One entry per lane, in every wavefront alike: an entry's place and the weight ahead of it are sums over the greater ones.  No sorting and one
+            // barrier: 1.5 to 2 us less than the way below, which longer lists take.
+            const uint64_t o = (uint32_t)lane < n ? list[lane] : 0;
+            const float x_o = logit_of(o);
+            const double w_o = (uint32_t)lane < n ? exp_minus(r.below(x_o)) : 0.0;
+            const uint64_t own = units(w_o);
+            uint32_t place = 0;
+            uint64_t ahead = all_above;
+            for (uint32_t q = 0; q < n; ++q) {   // uniform
+                const bool greater = of_lane(o, q) > o;
+                place += greater;
+                ahead += greater ? of_lane(own, q) : 0;
+            }
+            const uint32_t above_k_bin = (uint32_t)__popcll(__ballot((uint32_t)lane < n && r.bin(r.depth(x_o)) < cut.k_bin)), allowed = allowed_by_k(above_k_bin);
+            const bool in_k = (uint32_t)lane < n && place < allowed;
+            const double limit = r.p * (double)(all_above + all_between + of_lane(scan_wave(in_k ? own : 0), 63));
+            if (apart && place >= above_k_bin) ahead += all_between;
+            const bool stays = in_k && stays_at(ahead, limit);
+            cut_order = __any(stays) ? ~max_wave(stays ? ~o : 0) : max_wave(o) + 1;
+            if (wave == 0 && stays && (r.min_w == 0.0 || w_o >= r.min_w)) atomicAdd(&segment_mass[~(uint32_t)o / kSegment], (unsigned long long)own);
+            __syncthreads();
+        } else {
+            unsigned long long *const upto = tail.upto;
+            sort_list(list, tail, n, r, cut);
+            // weights down the list; its places where something ends are found by the entry ahead of them
+            auto logit = [&](uint32_t i) { return logit_of(list[i]); };
+            auto bin_at = [&](uint32_t i) { return r.bin(r.depth(logit(i))); };
+            uint64_t so_far = 0;
 #pragma unroll 1
-        for (uint32_t i = tid; i < n; i += kSampleThreads)
-            if (stays(i) && !stays(i + 1)) staying = i + 1;   // one entry of all, or none
-        __syncthreads();
-        const uint32_t stay = staying;
-        cut_order = stay ? list[stay - 1] : list[0] + 1;
+            for (uint32_t i0 = 0; i0 < n; i0 += kSampleThreads) {
+                const uint32_t i = i0 + tid;
+                uint64_t to[1] = {0}, all[1];
+                if (i < n) {
+                    to[0] = units(exp_minus(r.below(logit(i))));
+                    if (bin_at(i) < cut.k_bin && (i + 1 == n || bin_at(i + 1) >= cut.k_bin)) to_k_bin = i + 1;   // one entry of all, or none
+                }
+                scan_block(to, all);
+                if (i < n) upto[i] = so_far + to[0];
+                so_far += all[0];
+            }
+            __syncthreads();
+            const uint32_t above_k_bin = to_k_bin;
+            const uint32_t allowed = allowed_by_k(above_k_bin);
+            const double limit = r.p * (double)(all_above + all_between + upto[allowed - 1]);
+            auto stays = [&](uint32_t i) {
+                if (i >= allowed) return false;
+                const uint64_t ahead = all_above + (i ? upto[i - 1] : 0) + (apart && i >= above_k_bin ? all_between : 0);
+                return stays_at(ahead, limit);
+            };
 #pragma unroll 1
-        for (uint32_t i = tid; i < stay; i += kSampleThreads)
-            if (r.min_w == 0.0 || exp_minus(r.below(logit(i))) >= r.min_w)
-                atomicAdd(&segment_mass[(~(uint32_t)list[i]) / kSegment], (unsigned long long)(upto[i] - (i ? upto[i - 1] : 0)));
-        __syncthreads();
+            for (uint32_t i = tid; i < n; i += kSampleThreads)
+                if (stays(i) && !stays(i + 1)) staying = i + 1;   // one entry of all, or none
+            __syncthreads();
+            const uint32_t stay = staying;
+            cut_order = stay ? list[stay - 1] : list[0] + 1;
+#pragma unroll 1
+            for (uint32_t i = tid; i < stay; i += kSampleThreads)
+                if (r.min_w == 0.0 || exp_minus(r.below(logit(i))) >= r.min_w)
+                    atomicAdd(&segment_mass[(~(uint32_t)list[i]) / kSegment], (unsigned long long)(upto[i] - (i ? upto[i - 1] : 0)));
+            __syncthreads();
+        }
     } else {
         __syncthreads();
     }
