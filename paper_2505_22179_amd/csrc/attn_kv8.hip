@@ -738,34 +738,41 @@ __global__ __launch_bounds__(256) void tree_attn_kv8_merge_kernel(const float *_
 }
 
 // How a call is cut up: even row tiles of up to 32 row_groups rows, key ranges per tile, who merges the ranges.
-struct Kv8Plan { int row_groups, tile_rows, tiles_per_kv, ranges, fused, tenths; };
+struct Kv8Plan { int row_groups, tile_rows, tiles_per_kv, ranges, fused, time; };
 static int kv8_steps(int M, int P) { return (P + M + kKeyBlock - 1) / kKeyBlock; }
 
-// The number of ranges with the smallest estimate, at most one workgroup per CU (which also bounds the partial results).  Estimates are in tenths of
-// a microsecond, from a sweep over 1 to 64 query rows, 8 to 64 query heads, 4 to 16 KV heads and 64 to 131072 keys, both formats: `base` and `round`
-// for every round that a kernel walks; a merge by a second kernel 35, by the tile's last workgroup 5 and 1 per 10 rows read.
-static Kv8Plan kv8_cut(int pairs, int Hkv, int steps, int row_groups, int base, int round)
+// The number of ranges with the smallest estimate, at most one workgroup per CU (which also bounds the partial results).  Estimates are in hundredths of a
+// microsecond.  Those of the wave kernel were fitted over 38 sizes (1 to 64 query rows, 2 to 16 KV heads, 64 to 131072 keys, both formats) with
+// up to 19 numbers of ranges and both ways to merge them; the number they pick is 1 % slower than the best in the mean, 9 % at most.
+static Kv8Plan kv8_cut(int pairs, int Hkv, int steps, int row_groups, int format)
 {
     Kv8Plan p;
     p.row_groups = row_groups;
     even_tiles(pairs, kWaveRows * row_groups, p.tile_rows, p.tiles_per_kv);
-    const int units = Hkv * p.tiles_per_kv, key_groups = kWaves / row_groups;
+    const int units = Hkv * p.tiles_per_kv, rows = p.tile_rows;
     int most = kChipTiles / units;
     most = most > kMaxRanges ? kMaxRanges : most;
     most = most > steps ? steps : most;
-    p.tenths = 0x7FFFFFFF;
+    p.time = 0x7FFFFFFF;
     for (int r = 1; r <= (most < 1 ? 1 : most); ++r) {
-        const int rounds = ((steps + r - 1) / r + key_groups - 1) / key_groups;
-        const int last_arriver = 5 + p.tile_rows * r / 10;
-        const bool fused = r > 1 && row_groups == 1 && units <= kMaxTickets && last_arriver < 35;
-        const int tenths = base + rounds * round + (r == 1 ? 0 : fused ? last_arriver : 35);
-        if (tenths < p.tenths) p.ranges = r, p.fused = fused, p.tenths = tenths;
+        const int range = (steps + r - 1) / r;   // steps of the longest
+        bool fused = false;
+        int time;
+        if (row_groups == 1) {
+            const int slots = r <= 4 ? 4 : r <= 8 ? 8 : r <= 16 ? 16 : kMaxRanges;   // ranges that the merge is compiled for
+            const int by_kernel = 240 + 7 * slots, by_last = 60 + (32 * rows + (3 * rows + 80) * slots) / 10;
+            fused = r > 1 && units <= kMaxTickets && by_last < by_kernel;
+            time = 580 + 7 * rows + range * (format == kInt8 ? 24 : 19) + (r == 1 ? 0 : fused ? by_last : by_kernel);
+        } else {   // a round: a step of each key group
+            time = 1100 + (range + kWaves / row_groups - 1) / (kWaves / row_groups) * 110 + (r == 1 ? 0 : 350);
+        }
+        if (time < p.time) p.ranges = r, p.fused = fused, p.time = time;
     }
     return p;
 }
 
-// A round of the wave kernel takes 1.8 us with int8 codes and 1.4 with e4m3 (256 keys of 32 rows; it turns every code into a number once per 32 rows), one
-// of the shared kernel 1.1 us (64 keys of 128 rows, the same work), but that starts and ends more slowly.  Measured, wave and shared kernel, us:
+// 256 keys of 32 rows take the wave kernel 1.9 us with int8 codes and 1.5 with e4m3 (it turns every code into a number once per 32 rows), the same work,
+// 64 keys of 128 rows, the shared kernel 1.1 us, but that starts and ends more slowly.  Measured, wave and shared kernel, us:
 //   rows, heads, keys        int8           e4m3
 //   60, 64/8,  2048          18.1  19.5     15.8  19.2
 //   60, 64/8,  4096          24.9  22.7     21.5  22.4
@@ -777,10 +784,10 @@ static Kv8Plan kv8_cut(int pairs, int Hkv, int steps, int row_groups, int base, 
 static Kv8Plan kv8_plan(int M, int P, int Hq, int Hkv, int format)
 {
     const int pairs = Hq / Hkv * M, steps = kv8_steps(M, P);
-    const Kv8Plan wave = kv8_cut(pairs, Hkv, steps, 1, 80, format == kInt8 ? 18 : 14);
+    const Kv8Plan wave = kv8_cut(pairs, Hkv, steps, 1, format);
     if (pairs <= kWaveRows) return wave;   // one row group would be at work
-    const Kv8Plan shared = kv8_cut(pairs, Hkv, steps, kRowGroups, 110, 11);
-    return shared.tenths < wave.tenths ? shared : wave;
+    const Kv8Plan shared = kv8_cut(pairs, Hkv, steps, kRowGroups, format);
+    return shared.time < wave.time ? shared : wave;
 }
 
 static int check_attn_kv8(int M, int P, int Hq, int Hkv, int D)

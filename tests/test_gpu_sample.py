@@ -256,3 +256,38 @@ def test_one_step_from_the_projection_to_the_token():
     for m in range(M):
         t, p, margin = R.sample(x[m], float(np.float32(0.8)), 50, 1.0, 0.0, float(u[m]))
         assert margin < 1e-9 or (int(token[m]) == t and abs(float(prob[m]) - p) <= 1e-6 * p)
+
+
+def test_two_graphs_that_share_a_workspace():
+    """attention and sampling of two steps of different sizes, captured apart, replayed in turn with eager calls in between, all on one workspace"""
+    rng = np.random.default_rng(21)
+    d = lambda a, t=torch.float32: torch.as_tensor(np.asarray(a), dtype=t).to(DEV)
+    D, fmt, V = 128, B.KV8_INT8, 40000
+    steps = []
+    ws = B.new_workspace(max(B.tree_verify_attn_kv8_workspace_bytes(60, 9000, 64, 8, D), B.lm_head_sample_workspace_bytes(60, V)))
+    for M, P, Hq, Hkv in ((60, 9000, 64, 8), (3, 1500, 32, 8)):
+        x, _ = rows(30 + M, M, V)
+        codes = [d(rng.integers(0, 256, (P + M, Hkv, D)), torch.uint8) for _ in range(2)]
+        scales = [d(rng.integers(8, 16, (P + M, Hkv)) / 2048.0, torch.float16) for _ in range(2)]
+        q, out = d(rng.standard_normal((M, Hq, D)), torch.float16), torch.empty(M, Hq, D, dtype=torch.float16, device=DEV)
+        args = d(x), M, V, d(rng.uniform(0.5, 1.5, M)), d(rng.integers(1, 400, M), torch.int32), d(rng.uniform(0.6, 1, M)), None, d(rng.random(M))
+        token, prob, mask = torch.empty(M, dtype=torch.int32, device=DEV), torch.empty(M, device=DEV), torch.tril(torch.ones(M, M, dtype=torch.uint8, device=DEV))
+
+        def step(q=q, codes=codes, scales=scales, mask=mask, out=out, M=M, P=P, Hq=Hq, Hkv=Hkv, args=args, token=token, prob=prob):
+            B.tree_verify_attn_kv8(q, *codes, *scales, fmt, mask, out, M, P, Hq, Hkv, D, D ** -0.5, ws)
+            B.lm_head_sample(*args, token, prob, ws)
+
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        steps.append((step, graph, (out, token, prob), [t.clone() for t in (out, token, prob)]))
+    for turn in range(3):
+        for step, graph, got, want in steps:
+            for t in got:
+                t.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), turn
+        steps[turn % 2][0]()
