@@ -67,7 +67,7 @@ typedef float float2v __attribute__((ext_vector_type(2)));
 // as well as 1, and sums and outputs are rescaled a few times in all, not in most steps.
 constexpr float kBehind = 8.f;
 // A row whose mask row is empty is padding and sees nothing, committed keys included.  Only ranges with draft keys read the mask (in the others it would cost
-// up to 1.2 us of 15): they give such rows this sum, and whoever joins the ranges writes zeros.
+// up to 1.2 us of 15): they give such rows kPaddingMark for a sum, and whoever joins the ranges writes zeros.
 
 struct Kv8Args {
     uint32_t by_tiles, by_ranges;   // divider() of tiles_per_kv and nsplit
@@ -362,15 +362,16 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
 }
 
 // ---- taller row tiles: K and V tiles turned into fp16 once and shared --------------------------------------
-// A workgroup's eight wavefronts are WR row groups of 32 rows times 8 / WR key groups.  In a round each key group takes one 32-key step:
-// its WR wavefronts fetch the step's codes into registers two rounds ahead, turn their share into fp16 values and write those to LDS one round
-// ahead (two buffers, one barrier per round), in the layouts of tree_attn_wave_kernel's tiles: the products read values, and
-// codes are converted once per 32 WR rows.  What the wavefronts of a key group have of a row meets at the end in LDS.
+// A workgroup's eight wavefronts are WR = 4 row groups of 32 rows times WK = 2 key groups.  In a round each key group takes one 32-key step:
+// its four wavefronts fetch the step's codes into registers two rounds ahead, turn their share into fp16 values and write those to LDS one round
+// ahead (two buffers), in the layouts of tree_attn_wave_kernel's tiles: the products read values, and
+// codes are converted once per 128 rows.  What the wavefronts of a key group have of a row meets at the end in LDS.
 // Four row groups: two conversions of 16 codes per wavefront, step and lane, beside 32 probabilities' arithmetic.  Two row groups take 59 to 71 us where four
-// take 50 (60 rows of 64/8 heads over 16001 keys), eight leave too few rows in a tile for most calls.
-// Half of the wavefronts run a phase behind the others, so that a SIMD's matrix unit and its vector unit are both at work: 50.5 us at that size, against
-// 54 in step with each other.  What bounds it there is the vector unit (maxima, exponentials, conversions: 2400 cycles a round, of which the matrix
-// steps need 1030), and 13 us before the first round, after the last one and in the merge.
+// take 50 (60 rows of 64/8 heads over 16001 keys); eight, of which fewer calls have the rows, no less than four.
+// A round is two phases, products (with the next round's conversions in their shadow) and softmax, a barrier behind each.  Half of the wavefronts run a phase
+// behind the others, so that a SIMD's matrix unit and its vector unit are both at work: 50 us at that size, against 54 in step with each other.  A
+// round takes 2400 cycles there, of which the matrix steps need 1030 and LDS reads, at 128 B a cycle, 1250; 13 us go by before the first round, after the last
+// one and in the merge.
 constexpr int kTile16 = kKeyBlock * kHeadDim * 2;          // fp16 values of a K or V tile
 constexpr int kStep16 = 2 * kTile16;
 constexpr int kRowGroups = 4;
