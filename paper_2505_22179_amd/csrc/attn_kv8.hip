@@ -45,8 +45,9 @@ __device__ __forceinline__ void clear_codes(uint8_t *tile, uint32_t keys, int la
 // As tree_attn_wave_kernel: eight wavefronts carry the same 32 rows, wavefront w takes key steps w, w + 8, ... of the workgroup's range and
 // meets the others only at the end.  A step is 32 keys: 4 KB of K codes, 4 KB of V codes and 64 scales, brought straight to LDS one step
 // ahead of their use (two buffers per wavefront; two steps ahead was no faster over long prefixes and 0.3 us slower over short ones).
-// What bounds it: with few rows over a long prefix, memory (7 rows of 32/8 heads over 131072 keys: 268 MB of codes in 53 us, 5.0 TB/s); over a short
-// one, its own length (1 row of 64/8 heads over 2049 keys: 8 us, of which the walk takes 3.5, arguments, mask and Q 2, the merges 2.5); with many rows
+// What bounds it: with few rows over a long prefix, memory (7 rows of 32/8 heads over 131072 keys: 268 MB of codes in 53 us, 5.0 TB/s, as fast as 128-byte
+// pieces can be read: a kernel that does nothing else takes 53 to 56); over a short
+// one, its own length (1 row of 64/8 heads over 2049 keys: 9 us, of which the walk takes 3.5, arguments, mask and Q 2, the merges 2.5); with many rows
 // the turning of codes into numbers, which every 32 rows do again.
 //   K fragments   lane (c, h) of a pair of matrix steps takes the 16 codes of chunk 2 j + h of key c: its first eight are slots 8 h .. of the first
 //                 step, the others of the second (any order of the contraction serves, Q's fragments follow it)
