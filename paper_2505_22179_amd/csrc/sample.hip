@@ -6,7 +6,8 @@
 // of the row's total where sums in fp32 would be off by 1e-5 -- tokens near a border would change with the split.  Tokens more than e^31 below the
 // row's largest weigh nothing (262144 of them 1e-8 of the total at most) and take part in nothing.
 //
-// Three kernels, each of several workgroups per row, pass over the logits once:
+// Rows of up to kChunk tokens take one kernel, a workgroup per row (sample_row_kernel).  Longer ones take three, each of several workgroups per
+// row, that pass over the logits once:
 //   sample_top_kernel    the largest logit of each chunk of kChunk tokens, its token, and the smallest number
 //   sample_bins_kernel   counts and weights (fp32 is enough here) in kBins bins of even width in max - x; the row's last workgroup finds the
 //                        few bins in which the limits of top-k and top-p fall, whatever the rounding.  Not launched without such limits.
@@ -88,6 +89,8 @@ struct RowRule {
     // (depth < deepest; not so for NaN and -inf) and which bin they are in.
     __device__ __forceinline__ float depth(float x) const { return x == top ? 0.f : __builtin_fmaf(-0.5f, x, 0.5f * top); }
     __device__ __forceinline__ int bin(float depth) const { return (int)fminf(depth * bins_per, (float)(kBins - 1)); }
+    __device__ __forceinline__ float per_octave() const { return (float)(inv_t * -2.0 * 1.44269504088896340736); }   // of a weight, by depth
+    __device__ __forceinline__ bool limited() const { return k != 0 || p < 1.0; }
     // distance below the largest logit in units of the temperature, of tokens that take part
     __device__ __forceinline__ double below(float x) const { return x == top ? 0.0 : ((double)top - (double)x) * inv_t; }
 };
@@ -154,36 +157,43 @@ __device__ __forceinline__ uint64_t max_wave(uint64_t v)
     return of_lane(v, 63);
 }
 
-// the rule of row m and, in at, the first token of its largest logit (kNoToken: the row has no token); every lane of a wavefront calls it
-__device__ __forceinline__ RowRule row_rule(const SampleArgs &a, int m, int &at)
+// what row m asks for
+struct RowParams { float t, p, min_p, u; int k; };
+__device__ __forceinline__ RowParams row_params(const SampleArgs &a, int m)
 {
-    const int lane = threadIdx.x & 63;
     // all loads together: a limit that is not given reads the uniform number instead
-    float t = (a.temperature ? a.temperature : a.uniform)[m], p = (a.top_p ? a.top_p : a.uniform)[m], min_p = (a.min_p ? a.min_p : a.uniform)[m];
-    int k = (a.top_k ? a.top_k : reinterpret_cast<const int32_t *>(a.uniform))[m];
-    if (!a.temperature) t = 1.f;
-    if (!a.top_k) k = 0;
-    if (!a.top_p) p = 1.f;
-    if (!a.min_p) min_p = 0.f;
-    ChunkTop c = chunk_top(-__builtin_inff(), kNoToken, __builtin_inff());
-    if (lane < a.chunks) c = a.tops[m * a.chunks + lane];
-    const uint64_t order = max_wave(c.order);
-    const float least = order_number(~(uint32_t)max_wave(c.deep));
-    at = (int32_t)~(uint32_t)order;
+    RowParams q = {(a.temperature ? a.temperature : a.uniform)[m], (a.top_p ? a.top_p : a.uniform)[m], (a.min_p ? a.min_p : a.uniform)[m], a.uniform[m],
+                   (a.top_k ? a.top_k : reinterpret_cast<const int32_t *>(a.uniform))[m]};
+    if (!a.temperature) q.t = 1.f;
+    if (!a.top_k) q.k = 0;
+    if (!a.top_p) q.p = 1.f;
+    if (!a.min_p) q.min_p = 0.f;
+    return q;
+}
+__device__ __forceinline__ RowRule row_rule(const RowParams &q, int V, const ChunkTop &of_row)
+{
     RowRule r;
-    r.u = a.uniform[m];
-    r.top = order_number((uint32_t)(order >> 32));
-    r.greedy = !(t > 0.f) || k == 1 || p <= 0.f || min_p > 1.f;
-    r.inv_t = r.greedy ? 0.0 : 1.0 / (double)t;
-    r.k = k > 0 && k < a.V ? k : 0;
-    r.p = p < 1.f ? (double)p : 2.0;
-    r.min_w = min_p > 0.f ? (double)min_p : 0.0;
+    r.u = q.u;
+    r.top = order_number((uint32_t)(of_row.order >> 32));
+    r.greedy = !(q.t > 0.f) || q.k == 1 || q.p <= 0.f || q.min_p > 1.f;
+    r.inv_t = r.greedy ? 0.0 : 1.0 / (double)q.t;
+    r.k = q.k > 0 && q.k < V ? q.k : 0;
+    r.p = q.p < 1.f ? (double)q.p : 2.0;
+    r.min_w = q.min_p > 0.f ? (double)q.min_p : 0.0;
     // the bins span the distances that there are, so that they stay narrow at high temperatures
-    r.deepest = r.greedy ? 0.f : fmaxf((float)(0.5 * kFarthest * (double)t), 0x1p-149f);
-    const float span = fminf(r.depth(least), r.deepest);
+    r.deepest = r.greedy ? 0.f : fmaxf((float)(0.5 * kFarthest * (double)q.t), 0x1p-149f);
+    const float span = fminf(r.depth(order_number(~(uint32_t)of_row.deep)), r.deepest);
     r.bins_per = span > 0.f ? fminf((float)kBins / span, 3.0e38f) : 0.f;
     return r;
 }
+__device__ __forceinline__ ChunkTop join_lanes(const ChunkTop &c) { return {max_wave(c.order), max_wave(c.deep)}; }
+// of row m, as sample_top_kernel left it; every lane of a wavefront calls it
+__device__ __forceinline__ ChunkTop row_top(const SampleArgs &a, int m)
+{
+    const int lane = threadIdx.x & 63;
+    return join_lanes(lane < a.chunks ? a.tops[m * a.chunks + lane] : chunk_top(-__builtin_inff(), kNoToken, __builtin_inff()));
+}
+__device__ __forceinline__ int32_t token_of(const ChunkTop &c) { return (int32_t)~(uint32_t)c.order; }   // kNoToken: none
 
 // the uniform number as a rank of weight units below total
 __device__ __forceinline__ uint64_t drawn_rank(float u, uint64_t total)
@@ -254,17 +264,65 @@ __global__ __launch_bounds__(kSampleThreads) void sample_top_kernel(const Sample
     }
     __shared__ ChunkTop of_wave[kSampleWaves];
     ChunkTop c = chunk_top(top, at, least);
-    c = {max_wave(c.order), max_wave(c.deep)};
+    c = join_lanes(c);
     if (lane == 0) of_wave[tid >> 6] = c;
     __syncthreads();
-    if (tid == 0) {
-#pragma unroll
-        for (int w = 1; w < kSampleWaves; ++w) {
-            c.order = of_wave[w].order > c.order ? of_wave[w].order : c.order;
-            c.deep = of_wave[w].deep > c.deep ? of_wave[w].deep : c.deep;
-        }
-        a.tops[m * a.chunks + blockIdx.x] = c;
+    if (tid < 64) {
+        c = join_lanes(of_wave[lane & (kSampleWaves - 1)]);
+        if (tid == 0) a.tops[m * a.chunks + blockIdx.x] = c;
     }
+}
+
+__device__ __forceinline__ void into_bins(unsigned long long *bins, const RowRule &r, float depth, float per_octave)   // a token that takes part
+{
+    const float w = __builtin_amdgcn_exp2f(depth * per_octave);
+    atomicAdd(&bins[r.bin(depth)], (1ull << 48) + (unsigned long long)(uint32_t)(w * 2147483648.f + 0.5f));
+}
+
+// The bins in which the limits fall, from the counts and weights of bins 2 tid and 2 tid + 1 of the whole row; every thread of a workgroup calls it.
+__device__ __forceinline__ RowCut find_cut(const RowRule &r, int V, const uint64_t (&count)[2], const uint64_t (&mass)[2])
+{
+    const int tid = threadIdx.x;
+    __shared__ int k_bin, above_k, p_first, p_last;
+    __shared__ unsigned long long k_low, k_high;
+    uint64_t to[2] = {count[0] + count[1], mass[0] + mass[1]}, all[2];
+    if (tid == 0) k_bin = kNoBin, above_k = 0, p_first = kNoBin, p_last = -1;
+    scan_block(to, all);
+    const uint64_t count_to[2] = {to[0] - count[1], to[0]}, mass_to[2] = {to[1] - mass[1], to[1]};
+    const bool limited_k = r.k && (uint64_t)r.k < all[0];   // uniform
+    if (limited_k) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (count_to[e] >= (uint64_t)r.k && count_to[e] - count[e] < (uint64_t)r.k) {   // one bin of all
+                k_bin = 2 * tid + e;
+                above_k = (int)(count_to[e] - count[e]);
+                k_low = mass_to[e] - mass[e];
+                k_high = mass_to[e];
+            }
+        __syncthreads();
+    }
+    if (r.p < 1.0) {
+        // The weights here are off by less than 2^-17 of each (an fp32 exponent of up to 45 with three roundings) and by V 2^-32 in all: the true border lies between
+        // `low` and `high`, and so in the bins that reach over one and begin below the other
+        const double slack = (double)V * 0.5 + 1.0;   // in units of 2^-31
+        const double low = r.p * (double)(limited_k ? k_low : all[1]) * (1.0 - 0x1p-16) - slack;
+        const double high = r.p * (double)(limited_k ? k_high : all[1]) * (1.0 + 0x1p-16) + slack;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (count[e] != 0 && 2 * tid + e <= k_bin) {
+                const bool top = count_to[e] == count[e], bottom = count_to[e] == all[0] || 2 * tid + e == k_bin;
+                const double from = (double)(mass_to[e] - mass[e]), until = (double)mass_to[e];
+                auto reaches = [&](double t) { return t * (1.0 + 0x1p-16) + slack >= low; };
+                auto begins = [&](double t) { return t * (1.0 - 0x1p-16) - slack < high; };
+                // the first bin that reaches over `low` begins where the one before, which does not, ends; likewise the last: few come here
+                if (reaches(until) && (top || !reaches(from))) atomicMin(&p_first, 2 * tid + e);
+                if ((top || begins(from)) && (bottom || !begins(until))) atomicMax(&p_last, 2 * tid + e);
+            }
+    } else if (tid == 0) {
+        p_first = p_last = k_bin;   // kNoBin: the row has fewer tokens than its limit, and nothing is cut
+    }
+    __syncthreads();
+    return {p_first, p_last, k_bin, above_k};
 }
 
 // Rows without a limit of this kind leave at once, and so does a row's every workgroup.
@@ -284,19 +342,18 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(const Sampl
     int chunk = blockIdx.x * a.bin_chunks;
     const int chunks_end = min(chunk + a.bin_chunks, a.chunks);
     fetch(chunk);
-    int at;
-    const RowRule r = row_rule(a, m, at);
-    if (at == kNoToken || r.greedy || (r.k == 0 && r.p >= 1.0)) return;   // uniform over the row
+    const RowParams params = row_params(a, m);
+    const ChunkTop row = row_top(a, m);
+    const RowRule r = row_rule(params, a.V, row);
+    if (token_of(row) == kNoToken || r.greedy || !r.limited()) return;   // uniform over the row
     for (int b = tid; b < kBins; b += kSampleThreads) bins[b] = 0;
     __syncthreads();
-    const float per_octave = (float)(r.inv_t * -2.0 * 1.44269504088896340736);
+    const float per_octave = r.per_octave();
     while (true) {
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             const float d = r.depth(v[e]);
-            if (!(d < r.deepest)) continue;
-            const float w = __builtin_amdgcn_exp2f(d * per_octave);
-            atomicAdd(&bins[r.bin(d)], (1ull << 48) + (unsigned long long)(uint32_t)(w * 2147483648.f + 0.5f));
+            if (d < r.deepest) into_bins(bins, r, d, per_octave);
         }
         if (++chunk >= chunks_end) break;   // uniform
         fetch(chunk);
@@ -326,46 +383,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(const Sampl
                 }
             }
     }
-    __shared__ int k_bin, above_k, p_first, p_last;
-    __shared__ unsigned long long k_low, k_high;
-    uint64_t to[2] = {count[0] + count[1], mass[0] + mass[1]}, all[2];
-    if (tid == 0) k_bin = kNoBin, above_k = 0, p_first = kNoBin, p_last = -1;
-    scan_block(to, all);
-    const uint64_t count_to[2] = {to[0] - count[1], to[0]}, mass_to[2] = {to[1] - mass[1], to[1]};
-    const bool limited_k = r.k && (uint64_t)r.k < all[0];   // uniform
-    if (limited_k) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (count_to[e] >= (uint64_t)r.k && count_to[e] - count[e] < (uint64_t)r.k) {   // one bin of all
-                k_bin = 2 * tid + e;
-                above_k = (int)(count_to[e] - count[e]);
-                k_low = mass_to[e] - mass[e];
-                k_high = mass_to[e];
-            }
-        __syncthreads();
-    }
-    if (r.p < 1.0) {
-        // The weights here are off by less than 2^-17 of each (an fp32 exponent of up to 45 with three roundings) and by V 2^-32 in all: the true border lies between
-        // `low` and `high`, and so in the bins that reach over one and begin below the other
-        const double slack = (double)a.V * 0.5 + 1.0;   // in units of 2^-31
-        const double low = r.p * (double)(limited_k ? k_low : all[1]) * (1.0 - 0x1p-16) - slack;
-        const double high = r.p * (double)(limited_k ? k_high : all[1]) * (1.0 + 0x1p-16) + slack;
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (count[e] != 0 && 2 * tid + e <= k_bin) {
-                const bool top = count_to[e] == count[e], bottom = count_to[e] == all[0] || 2 * tid + e == k_bin;
-                const double from = (double)(mass_to[e] - mass[e]), until = (double)mass_to[e];
-                auto reaches = [&](double t) { return t * (1.0 + 0x1p-16) + slack >= low; };
-                auto begins = [&](double t) { return t * (1.0 - 0x1p-16) - slack < high; };
-                // the first bin that reaches over `low` begins where the one before, which does not, ends; likewise the last: few come here
-                if (reaches(until) && (top || !reaches(from))) atomicMin(&p_first, 2 * tid + e);
-                if ((top || begins(from)) && (bottom || !begins(until))) atomicMax(&p_last, 2 * tid + e);
-            }
-    } else if (tid == 0) {
-        p_first = p_last = k_bin;   // kNoBin: the row has fewer tokens than its limit, and nothing is cut
-    }
-    __syncthreads();
-    if (tid == 0) a.cuts[m] = {p_first, p_last, k_bin, above_k};
+    const RowCut cut = find_cut(r, a.V, count, mass);
+    if (tid == 0) a.cuts[m] = cut;
 }
 
 // Cuts a row by digits of its logits, for lists that are too long; every thread of one workgroup calls it.  by_mass: the last token with less than
@@ -534,114 +553,41 @@ __device__ __forceinline__ void number_to_lds(const float *src, float *lds_base)
 }
 
 constexpr int kEarlyLds = kSampleWaves * 2 * kSegment * 4;   // two segments of each wavefront
-// A wavefront takes segments of 512 tokens, `rounds` of them; their logits come straight to LDS, two segments ahead, and are looked at in loops that are
-// hardly unrolled: code that runs once is fetched from memory, and unrolled over 16 tokens it took 2 us longer than the work.  (LDS of a size given at
-// the launch: before a read of an array that is declared with its size the compiler waits for every transfer under way.)
-__global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const SampleArgs a)
+constexpr int kSteps = kSegment / 64;
+// One segment by one wavefront, its logits in LDS, i0 the index of the lane's first: what stays for certain and is not below min_p (the sum in lane 63), and,
+// per lane, all above the first border bin and all between the border bins and the k-th token's; tokens in border bins go to the list.
+__device__ __forceinline__ uint64_t weigh_segment(const float *segment, int i0, int V, const RowRule &r, const RowCut &cut, unsigned long long *list, uint32_t &listed,
+                                                  uint64_t &above, uint64_t &between)
 {
-    const int tid = threadIdx.x, lane = tid & 63, m = blockIdx.y, V = a.V;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const float *x = a.logits + (size_t)m * V;
-    constexpr int kSteps = kSegment / 64;
-    __shared__ unsigned long long list[kList];
-    extern __shared__ float4 early[];   // kEarlyLds bytes
-    static_assert(sizeof(TailLds) <= kEarlyLds, "the tail's LDS lies where the segments were");
-    TailLds &tail = *reinterpret_cast<TailLds *>(early);
-    __shared__ unsigned long long sums[2];
-    __shared__ uint32_t listed;
-    float *const mine = reinterpret_cast<float *>(early) + wave * 2 * kSegment;
-    const int segment0 = blockIdx.x * kSampleWaves * a.rounds + wave;
-    const int rounds = min(a.rounds, (a.segments - segment0 + kSampleWaves - 1) / kSampleWaves);   // not above 0: none
-    auto request = [&](int round) {
-        const int i0 = (segment0 + round * kSampleWaves) * kSegment + lane;
-#pragma unroll
-        for (int e = 0; e < kSteps; ++e) number_to_lds(x + min(i0 + e * 64, V - 1), mine + (round & 1) * kSegment + e * 64);
-    };
-    if (rounds > 0) request(0);
-    if (rounds > 1) request(1);
-    RowCut cut = {kNoBin, kNoBin, kNoBin, 0};
-    if (a.top_k || a.top_p) cut = a.cuts[m];   // of use where sample_bins_kernel has written it
-    int at;
-    const RowRule r = row_rule(a, m, at);
-    if (at == kNoToken || r.greedy) {   // uniform over the row
-        if (blockIdx.x == 0 && tid == 0) {
-            a.token[m] = at;
-            a.prob[m] = at == kNoToken ? 0.f : 1.f;
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may land in LDS that has been given to others
-        return;
-    }
-    const bool limited = r.k != 0 || r.p < 1.0;   // uniform over the row
-    if (!limited) cut = {kNoBin, kNoBin, kNoBin, 0};
-    if (tid == 0) listed = 0, sums[0] = sums[1] = 0;
-    __syncthreads();
-    unsigned long long *const row_kept = a.kept + (size_t)m * a.segments;
-    uint64_t above = 0, between = 0;
-#pragma unroll 1
-    for (int round = 0; round < rounds; ++round) {
-        const int segment = segment0 + round * kSampleWaves, i0 = segment * kSegment + lane;
-        if (round + 1 < rounds) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");   // the next segment may be under way
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        const float *const here = mine + (round & 1) * kSegment + lane;
-        uint64_t kept = 0;
+    const float *const here = segment + (threadIdx.x & 63);
+    uint64_t kept = 0;
 #pragma unroll 2
-        for (int e = 0; e < kSteps; ++e) {
-            const float v = here[e * 64];
-            const float d = r.depth(v);
-            const int b = r.bin(d);
-            if (!(d < r.deepest) || i0 + e * 64 >= V || (b > cut.last && b > cut.k_bin)) continue;   // takes no part, or is beyond the limits
-            if (b >= cut.first && (b <= cut.last || b == cut.k_bin)) {   // a border bin
-                const uint32_t n = atomicAdd(&listed, 1u);
-                if (n < kList) list[n] = order_of(v, i0 + e * 64);
-            } else {
-                const double w = exp_minus(r.below(v));
-                const uint64_t n = units(w);
-                above += b < cut.first ? n : 0;
-                between += b < cut.first ? 0 : n;
-                kept += b < cut.first && w >= r.min_w ? n : 0;
-            }
+    for (int e = 0; e < kSteps; ++e) {
+        const float v = here[e * 64];
+        const float d = r.depth(v);
+        const int b = r.bin(d);
+        if (!(d < r.deepest) || i0 + e * 64 >= V || (b > cut.last && b > cut.k_bin)) continue;   // takes no part, or is beyond the limits
+        if (b >= cut.first && (b <= cut.last || b == cut.k_bin)) {   // a border bin
+            const uint32_t n = atomicAdd(&listed, 1u);
+            if (n < kList) list[n] = order_of(v, i0 + e * 64);
+        } else {
+            const double w = exp_minus(r.below(v));
+            const uint64_t n = units(w);
+            above += b < cut.first ? n : 0;
+            between += b < cut.first ? 0 : n;
+            kept += b < cut.first && w >= r.min_w ? n : 0;
         }
-        if (round + 2 < rounds) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this segment has been read
-            request(round + 2);
-        }
-        kept = scan_wave(kept);
-        if (lane == 63) store_shared(row_kept + segment, kept);
     }
-    above = scan_wave(above);
-    between = scan_wave(between);
-    if (lane == 63) {
-        atomicAdd(&sums[0], (unsigned long long)above);
-        atomicAdd(&sums[1], (unsigned long long)between);
-    }
-    __syncthreads();
-    GroupMass *const masses = a.masses + m * a.groups;
-    unsigned long long *const lists = a.lists + (size_t)m * a.groups * kList;
-    if (tid < 2) store_shared(&masses[blockIdx.x].above + tid, sums[tid]);
-    if (tid == 2) store_shared(&masses[blockIdx.x].listed, listed);
-    for (uint32_t n = tid; n < min(listed, (uint32_t)kList); n += kSampleThreads) store_shared(lists + (size_t)blockIdx.x * kList + n, list[n]);
-    if (!last_of_row(a.tickets + gridDim.y + m, a.groups)) return;
+    return scan_wave(kept);
+}
 
-    // ---- the row's last workgroup: the exact cut, then the draw
-    // Every wavefront fetches what the groups found (lane = group), and, not knowing their counts yet, the first 64 entries of the lists that it
-    // will gather: groups wave, wave + 8, ...
-    __shared__ unsigned long long segment_mass[kSegments];
-    static_assert(kSegments == kSampleThreads && kSegment == kSampleThreads, "a thread per segment, and per token of one");
-    GroupMass found = {0, 0, 0, 0};
-    if (lane < a.groups) {
-        found.above = load_shared(&masses[lane].above);
-        found.between = load_shared(&masses[lane].between);
-        found.listed = load_shared(&masses[lane].listed);
-    }
-    const uint64_t own_kept = tid < a.segments ? load_shared(row_kept + tid) : 0;
-    constexpr int kParts = kGroups / kSampleWaves;
-    uint64_t entry[kParts];
-#pragma unroll
-    for (int q = 0; q < kParts; ++q) entry[q] = load_shared(lists + (size_t)min(wave + q * kSampleWaves, a.groups - 1) * kList + lane);
-    segment_mass[tid] = own_kept;
-    const uint64_t listed_to = scan_wave(found.listed);
-    const uint64_t all_above = of_lane(scan_wave(found.above), 63), all_between = of_lane(scan_wave(found.between), 63);
-    const uint32_t n = (uint32_t)of_lane(listed_to, 63);
+// The exact cut, then the draw, by one workgroup: list holds the row's n tokens in border bins (in any order; nothing if they are more than kList),
+// segment_mass what stays for certain of each segment.
+__device__ __forceinline__ void finish_row(const SampleArgs &a, int m, const RowRule &r, const RowCut &cut, unsigned long long *list, uint32_t n, uint64_t all_above,
+                                           uint64_t all_between, unsigned long long *segment_mass, TailLds &tail)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V;
+    const float *x = a.logits + (size_t)m * V;
     uint64_t cut_order = 0;   // tokens of this order and earlier ones stay
     if (n > kList) {
         DigitBins &digits = tail.digits;
@@ -670,14 +616,6 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const Sampl
         }
         __syncthreads();
     } else if (n > 0) {
-#pragma unroll
-        for (int q = 0; q < kParts; ++q) {
-            const int c = wave + q * kSampleWaves;
-            if (c >= a.groups) break;   // uniform over the wavefront
-            const uint32_t count = (uint32_t)of_lane(found.listed, c), base = (uint32_t)of_lane(listed_to, c) - count;
-            if ((uint32_t)lane < count) list[base + lane] = entry[q];
-            for (uint32_t i = 64 + lane; i < count; i += 64) list[base + i] = load_shared(lists + (size_t)c * kList + i);
-        }
         __shared__ uint32_t to_k_bin, staying;
         if (tid == 0) to_k_bin = 0, staying = 0;
         __syncthreads();
@@ -751,6 +689,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const Sampl
         __syncthreads();
     }
     // the segment, then the token
+    static_assert(kSegments == kSampleThreads && kSegment == kSampleThreads, "a thread per segment, and per token of one");
     __shared__ uint64_t chosen_rank;
     __shared__ int chosen;
     uint64_t mass[1] = {segment_mass[tid]}, total[1], all[1];
@@ -770,6 +709,186 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const Sampl
         a.token[m] = i;
         a.prob[m] = (float)(w * kOne / (double)total[0]);
     }
+}
+
+// A wavefront takes segments of 512 tokens, `rounds` of them; their logits come straight to LDS, two segments ahead, and are looked at in loops that are
+// hardly unrolled: code that runs once is fetched from memory, and unrolled over 16 tokens it took 2 us longer than the work.  (LDS of a size given at
+// the launch: before a read of an array that is declared with its size the compiler waits for every transfer under way.)
+__global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const SampleArgs a)
+{
+    const int tid = threadIdx.x, lane = tid & 63, m = blockIdx.y, V = a.V;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const float *x = a.logits + (size_t)m * V;
+    __shared__ unsigned long long list[kList];
+    extern __shared__ float4 early[];   // kEarlyLds bytes
+    static_assert(sizeof(TailLds) <= kEarlyLds, "the tail's LDS lies where the segments were");
+    TailLds &tail = *reinterpret_cast<TailLds *>(early);
+    __shared__ unsigned long long sums[2];
+    __shared__ uint32_t listed;
+    float *const mine = reinterpret_cast<float *>(early) + wave * 2 * kSegment;
+    const int segment0 = blockIdx.x * kSampleWaves * a.rounds + wave;
+    const int rounds = min(a.rounds, (a.segments - segment0 + kSampleWaves - 1) / kSampleWaves);   // not above 0: none
+    auto request = [&](int round) {
+        const int i0 = (segment0 + round * kSampleWaves) * kSegment + lane;
+#pragma unroll
+        for (int e = 0; e < kSteps; ++e) number_to_lds(x + min(i0 + e * 64, V - 1), mine + (round & 1) * kSegment + e * 64);
+    };
+    if (rounds > 0) request(0);
+    if (rounds > 1) request(1);
+    RowCut cut = {kNoBin, kNoBin, kNoBin, 0};
+    if (a.top_k || a.top_p) cut = a.cuts[m];   // of use where sample_bins_kernel has written it
+    const RowParams params = row_params(a, m);
+    const ChunkTop row = row_top(a, m);
+    const RowRule r = row_rule(params, V, row);
+    if (token_of(row) == kNoToken || r.greedy) {   // uniform over the row
+        if (blockIdx.x == 0 && tid == 0) {
+            a.token[m] = token_of(row);
+            a.prob[m] = token_of(row) == kNoToken ? 0.f : 1.f;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may land in LDS that has been given to others
+        return;
+    }
+    if (!r.limited()) cut = {kNoBin, kNoBin, kNoBin, 0};   // uniform over the row
+    if (tid == 0) listed = 0, sums[0] = sums[1] = 0;
+    __syncthreads();
+    unsigned long long *const row_kept = a.kept + (size_t)m * a.segments;
+    uint64_t above = 0, between = 0;
+#pragma unroll 1
+    for (int round = 0; round < rounds; ++round) {
+        const int segment = segment0 + round * kSampleWaves, i0 = segment * kSegment + lane;
+        if (round + 1 < rounds) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");   // the next segment may be under way
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const uint64_t kept = weigh_segment(mine + (round & 1) * kSegment, i0, V, r, cut, list, listed, above, between);
+        if (round + 2 < rounds) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this segment has been read
+            request(round + 2);
+        }
+        if (lane == 63) store_shared(row_kept + segment, kept);
+    }
+    above = scan_wave(above);
+    between = scan_wave(between);
+    if (lane == 63) {
+        atomicAdd(&sums[0], (unsigned long long)above);
+        atomicAdd(&sums[1], (unsigned long long)between);
+    }
+    __syncthreads();
+    GroupMass *const masses = a.masses + m * a.groups;
+    unsigned long long *const lists = a.lists + (size_t)m * a.groups * kList;
+    if (tid < 2) store_shared(&masses[blockIdx.x].above + tid, sums[tid]);
+    if (tid == 2) store_shared(&masses[blockIdx.x].listed, listed);
+    for (uint32_t n = tid; n < min(listed, (uint32_t)kList); n += kSampleThreads) store_shared(lists + (size_t)blockIdx.x * kList + n, list[n]);
+    if (!last_of_row(a.tickets + gridDim.y + m, a.groups)) return;
+
+    // ---- the row's last workgroup: the exact cut, then the draw
+    // Every wavefront fetches what the groups found (lane = group), and, not knowing their counts yet, the first 64 entries of the lists that it
+    // will gather: groups wave, wave + 8, ...
+    __shared__ unsigned long long segment_mass[kSegments];
+    GroupMass found = {0, 0, 0, 0};
+    if (lane < a.groups) {
+        found.above = load_shared(&masses[lane].above);
+        found.between = load_shared(&masses[lane].between);
+        found.listed = load_shared(&masses[lane].listed);
+    }
+    const uint64_t own_kept = tid < a.segments ? load_shared(row_kept + tid) : 0;
+    constexpr int kParts = kGroups / kSampleWaves;
+    uint64_t entry[kParts];
+#pragma unroll
+    for (int q = 0; q < kParts; ++q) entry[q] = load_shared(lists + (size_t)min(wave + q * kSampleWaves, a.groups - 1) * kList + lane);
+    segment_mass[tid] = own_kept;
+    const uint64_t listed_to = scan_wave(found.listed);
+    const uint64_t all_above = of_lane(scan_wave(found.above), 63), all_between = of_lane(scan_wave(found.between), 63);
+    const uint32_t n = (uint32_t)of_lane(listed_to, 63);
+    if (n <= kList) {
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) {
+            const int c = wave + q * kSampleWaves;
+            if (c >= a.groups) break;   // uniform over the wavefront
+            const uint32_t count = (uint32_t)of_lane(found.listed, c), base = (uint32_t)of_lane(listed_to, c) - count;
+            if ((uint32_t)lane < count) list[base + lane] = entry[q];
+            for (uint32_t i = 64 + lane; i < count; i += 64) list[base + i] = load_shared(lists + (size_t)c * kList + i);
+        }
+    }
+    finish_row(a, m, r, cut, list, n, all_above, all_between, segment_mass, tail);
+}
+
+// Rows of up to kChunk tokens, a workgroup each: everything from one reading of the logits, which stay in LDS.  Measured against the three kernels
+// above, us: 1 row of 1000 tokens, top-k and top-p 10.9 and 18.7, of 8192, top-k 14.1 and 19.9; 60 rows of 8192, all limits 16.4 and 22.1.  Beyond kChunk
+// a workgroup's time grows by 4 us for every kChunk tokens, that of the three kernels by less than 1.
+__global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const SampleArgs a)
+{
+    const int tid = threadIdx.x, lane = tid & 63, m = blockIdx.x, V = a.V;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const float *x = a.logits + (size_t)m * V;
+    __shared__ unsigned long long list[kList], bins[kBins], segment_mass[kSegments];
+    extern __shared__ float4 early[];   // kEarlyLds bytes
+    TailLds &tail = *reinterpret_cast<TailLds *>(early);
+    __shared__ ChunkTop of_wave[kSampleWaves];
+    __shared__ unsigned long long sums[2];
+    __shared__ uint32_t listed;
+    float *const mine = reinterpret_cast<float *>(early) + wave * 2 * kSegment;
+    const int rounds = min(2, (a.segments - wave + kSampleWaves - 1) / kSampleWaves);   // not above 0: none
+    for (int round = 0; round < rounds; ++round) {
+        const int i0 = (wave + round * kSampleWaves) * kSegment + lane;
+#pragma unroll
+        for (int e = 0; e < kSteps; ++e) number_to_lds(x + min(i0 + e * 64, V - 1), mine + round * kSegment + e * 64);
+    }
+    const RowParams params = row_params(a, m);
+    bins[2 * tid] = bins[2 * tid + 1] = 0;
+    segment_mass[tid] = 0;
+    if (tid == 0) listed = 0, sums[0] = sums[1] = 0;
+    float top = -__builtin_inff(), least = __builtin_inff();
+    int at = kNoToken;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    auto each = [&](auto &&use) {   // logits of this wavefront, with their indices
+        for (int round = 0; round < rounds; ++round) {
+            const int i0 = (wave + round * kSampleWaves) * kSegment + lane;
+#pragma unroll 4
+            for (int e = 0; e < kSteps; ++e)
+                if (i0 + e * 64 < V) use(mine[round * kSegment + e * 64 + lane], i0 + e * 64);
+        }
+    };
+    each([&](float v, int i) {   // NaN and -inf are no tokens
+        if (v > top) top = v, at = i;
+        if (v > -__builtin_inff()) least = fminf(least, v);
+    });
+    const ChunkTop own = join_lanes(chunk_top(top, at, least));
+    if (lane == 0) of_wave[wave] = own;
+    __syncthreads();
+    const ChunkTop row = join_lanes(of_wave[lane & (kSampleWaves - 1)]);
+    const RowRule r = row_rule(params, V, row);
+    if (token_of(row) == kNoToken || r.greedy) {   // uniform
+        if (tid == 0) {
+            a.token[m] = token_of(row);
+            a.prob[m] = token_of(row) == kNoToken ? 0.f : 1.f;
+        }
+        return;
+    }
+    RowCut cut = {kNoBin, kNoBin, kNoBin, 0};
+    if (r.limited()) {   // uniform
+        const float per_octave = r.per_octave();
+        each([&](float v, int) {
+            const float d = r.depth(v);
+            if (d < r.deepest) into_bins(bins, r, d, per_octave);
+        });
+        __syncthreads();
+        const unsigned long long n[2] = {bins[2 * tid], bins[2 * tid + 1]}, weights = (1ull << 48) - 1;
+        const uint64_t count[2] = {n[0] >> 48, n[1] >> 48}, mass[2] = {n[0] & weights, n[1] & weights};
+        cut = find_cut(r, V, count, mass);
+    }
+    uint64_t above = 0, between = 0;
+    for (int round = 0; round < rounds; ++round) {
+        const int segment = wave + round * kSampleWaves;
+        const uint64_t kept = weigh_segment(mine + round * kSegment, segment * kSegment + lane, V, r, cut, list, listed, above, between);
+        if (lane == 63) segment_mass[segment] = kept;
+    }
+    above = scan_wave(above);
+    between = scan_wave(between);
+    if (lane == 63) {
+        atomicAdd(&sums[0], (unsigned long long)above);
+        atomicAdd(&sums[1], (unsigned long long)between);
+    }
+    __syncthreads();   // the segments have been read as well
+    finish_row(a, m, r, cut, list, listed, sums[0], sums[1], segment_mass, tail);
 }
 
 }  // namespace w4
@@ -852,6 +971,10 @@ int lm_head_sample(const float *logits, int M, int V, const float *temperature, 
     a.bins = (unsigned long long *)(ws + at[5]);
     a.lists = (unsigned long long *)(ws + at[6]);
     const auto grid = [M](int groups) { return dim3((unsigned)groups, (unsigned)M); };
+    if (V <= kChunk) {
+        hipLaunchKernelGGL(sample_row_kernel, dim3((unsigned)M), dim3(kSampleThreads), kEarlyLds, (hipStream_t)stream, a);
+        return launch_status();
+    }
     hipLaunchKernelGGL(sample_top_kernel, grid(a.chunks), dim3(kSampleThreads), 0, (hipStream_t)stream, a);
     if (top_k || top_p) hipLaunchKernelGGL(sample_bins_kernel, grid(a.bin_groups), dim3(kSampleThreads), 0, (hipStream_t)stream, a);
     hipLaunchKernelGGL(sample_draw_kernel, grid(a.groups), dim3(kSampleThreads), kEarlyLds, (hipStream_t)stream, a);
