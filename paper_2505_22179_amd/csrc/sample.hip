@@ -812,8 +812,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const Sampl
 }
 
 // Rows of up to kChunk tokens, a workgroup each: everything from one reading of the logits, which stay in LDS.  Measured against the three kernels
-// above, us: 1 row of 1000 tokens, top-k and top-p 10.9 and 18.7, of 8192, top-k 14.1 and 19.9; 60 rows of 8192, all limits 16.4 and 22.1.  Beyond kChunk
-// a workgroup's time grows by 4 us for every kChunk tokens, that of the three kernels by less than 1.
+// above, us: 1 row of 1000 tokens, top-k and top-p 10.9 and 18.7, of 8192, top-k 14.1 and 19.9; 60 rows of 8192, all limits 16.4 and 22.1.  A
+// workgroup's time grows by 3 to 4 us from 1000 tokens to 8192, that of the three kernels by 2 from 1000 to 32000.
 __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const SampleArgs a)
 {
     const int tid = threadIdx.x, lane = tid & 63, m = blockIdx.x, V = a.V;

@@ -291,3 +291,23 @@ def test_two_graphs_that_share_a_workspace():
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, want)), turn
         steps[turn % 2][0]()
+
+
+@pytest.mark.parametrize("V", [2049, 5000, 8191, 8192, 8193])
+def test_equal_logits_around_one_workgroups_row(V):
+    """as in the largest call; a second, lower level of equal logits lies beyond the first"""
+    M, rng = 40, np.random.default_rng(V)
+    u = rng.integers(0, 1 << 24, M).astype(np.float64) / (1 << 24)
+    first = rng.permutation(V)[:V // 2]
+    x = np.full((M, V), -1.0, dtype=np.float32)
+    x[:, first] = 1.0
+    order = np.concatenate([np.sort(first), np.setdiff1d(np.arange(V), first)])   # falling logits, then by index
+    k = rng.integers(2, V // 2, M)
+    token, prob = run(x, top_k=k, u=u)
+    for m in range(M):
+        assert token[m] == order[:k[m]][int(u[m] * k[m])]
+    np.testing.assert_array_equal(prob, (1.0 / k).astype(np.float32))
+    k = rng.integers(V // 2 + 1, V, M)
+    for m, t in enumerate(run(x, top_k=k, u=u)[0]):   # all of the first level and some of the second
+        assert t in order[:k[m]]
+    check(x[:4], top_k=k[:4], top_p=[0.9, 0.5, 0.99, 1.0], min_p=[0, 0, 0.01, 0], u=u[:4])
