@@ -6,7 +6,7 @@
 // of the row's total where sums in fp32 would be off by 1e-5 -- tokens near a border would change with the split.  Tokens more than e^31 below the
 // row's largest weigh nothing (262144 of them 1e-8 of the total at most) and take part in nothing.
 //
-// Rows of up to kChunk tokens take one kernel, a workgroup per row (sample_row_kernel).  Longer ones take three, each of several workgroups per
+// Short rows take one kernel, a workgroup per row (sample_row_kernel).  Longer ones take three, each of several workgroups per
 // row, that pass over the logits once:
 //   sample_top_kernel    the largest logit of each chunk of kChunk tokens, its token, and the smallest number
 //   sample_bins_kernel   counts and weights (fp32 is enough here) in kBins bins of even width in max - x; the row's last workgroup finds the
@@ -833,22 +833,30 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const Sampl
     finish_row(a, m, r, cut, list, n, all_above, all_between, segment_mass, tail);
 }
 
-// Rows of up to kChunk tokens, a workgroup each: everything from one reading of the logits, which stay in LDS.  Measured against the three kernels
-// above, us: 1 row of 1000 tokens, top-k and top-p 10.9 and 18.7, of 8192, top-k 14.1 and 19.9; 60 rows of 8192, all limits 16.4 and 22.1.  A
-// workgroup's time grows by 3 to 4 us from 1000 tokens to 8192, that of the three kernels by 2 from 1000 to 32000.
+// Tokens of a row that one workgroup takes.  Measured against the three kernels above, us (1 row of 1000 tokens, top-k and top-p: 10.8 and 18.7):
+//   tokens          top-k        top-p        none
+//    8192, 1 row    13.5  19.9   15.4  21.2   10.5  12.0
+//   12000, 1 row    16.4  20.5   19.5  21.1   13.7  12.2
+//   12000, 60 rows  18.1  22.6   23.1  26.0   14.4  13.7
+//   16384, 1 row    19.0  20.5   23.7  22.1   16.7  12.4
+constexpr int kRowMost = 12288, kRowMostUnlimited = 8192;
+__host__ __device__ constexpr int row_rounds(int segments) { return segments <= 2 * kSampleWaves ? 2 : (segments + kSampleWaves - 1) / kSampleWaves; }   // of a wavefront
+constexpr int row_lds(int segments) { return kSampleWaves * row_rounds(segments) * kSegment * 4; }
+static_assert(row_lds(1) >= (int)sizeof(TailLds), "the tail's LDS lies where the segments were");
+// Short rows, a workgroup each: everything from one reading of the logits, which stay in LDS.
 __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const SampleArgs a)
 {
     const int tid = threadIdx.x, lane = tid & 63, m = blockIdx.x, V = a.V;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float *x = a.logits + (size_t)m * V;
     __shared__ unsigned long long list[kList], bins[kBins], segment_mass[kSegments];
-    extern __shared__ float4 early[];   // kEarlyLds bytes
+    extern __shared__ float4 early[];   // row_lds bytes
     TailLds &tail = *reinterpret_cast<TailLds *>(early);
     __shared__ ChunkTop of_wave[kSampleWaves];
     __shared__ unsigned long long sums[2];
     __shared__ uint32_t listed;
-    float *const mine = reinterpret_cast<float *>(early) + wave * 2 * kSegment;
-    const int rounds = min(2, (a.segments - wave + kSampleWaves - 1) / kSampleWaves);   // not above 0: none
+    const int rounds = (a.segments - wave + kSampleWaves - 1) / kSampleWaves;   // not above 0: none
+    float *const mine = reinterpret_cast<float *>(early) + wave * row_rounds(a.segments) * kSegment;
     for (int round = 0; round < rounds; ++round) {
         const int i0 = (wave + round * kSampleWaves) * kSegment + lane;
 #pragma unroll
@@ -994,8 +1002,12 @@ int lm_head_sample(const float *logits, int M, int V, const float *temperature, 
     a.bins = (unsigned long long *)(ws + at[5]);
     a.lists = (unsigned long long *)(ws + at[6]);
     const auto grid = [M](int groups) { return dim3((unsigned)groups, (unsigned)M); };
-    if (V <= kChunk) {
-        hipLaunchKernelGGL(sample_row_kernel, dim3((unsigned)M), dim3(kSampleThreads), kEarlyLds, (hipStream_t)stream, a);
+    if (V <= (top_k || top_p ? kRowMost : kRowMostUnlimited)) {
+        static bool lds_ok = false;   // LDS above 48 KB needs an opt-in, once
+        if (!lds_ok && hipFuncSetAttribute(reinterpret_cast<const void *>(sample_row_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, row_lds(kRowMost / kSegment)) != hipSuccess)
+            return W4A16_EHIP;
+        lds_ok = true;
+        hipLaunchKernelGGL(sample_row_kernel, dim3((unsigned)M), dim3(kSampleThreads), row_lds(a.segments), (hipStream_t)stream, a);
         return launch_status();
     }
     hipLaunchKernelGGL(sample_top_kernel, grid(a.chunks), dim3(kSampleThreads), 0, (hipStream_t)stream, a);

@@ -293,7 +293,7 @@ def test_two_graphs_that_share_a_workspace():
         steps[turn % 2][0]()
 
 
-@pytest.mark.parametrize("V", [2049, 5000, 8191, 8192, 8193])
+@pytest.mark.parametrize("V", [2049, 5000, 8191, 8192, 8193, 12288, 12289])
 def test_equal_logits_around_one_workgroups_row(V):
     """as in the largest call; a second, lower level of equal logits lies beyond the first"""
     M, rng = 40, np.random.default_rng(V)
@@ -311,3 +311,12 @@ def test_equal_logits_around_one_workgroups_row(V):
     for m, t in enumerate(run(x, top_k=k, u=u)[0]):   # all of the first level and some of the second
         assert t in order[:k[m]]
     check(x[:4], top_k=k[:4], top_p=[0.9, 0.5, 0.99, 1.0], min_p=[0, 0, 0.01, 0], u=u[:4])
+
+
+@pytest.mark.parametrize("limits", LIMITS)
+@pytest.mark.parametrize("V", [8192, 8500, 12287, 12288, 12289])
+def test_random_rows_around_one_workgroups_row(V, limits):
+    x, rng = rows(V, 3, V)
+    has = lambda n: n in limits or limits == "all"
+    check(x, rng.uniform(0.4, 2.5, 3), rng.integers(1, 3000, 3) if has("k") else None, rng.uniform(0.3, 1, 3) if has("p") else None,
+          rng.uniform(0, 0.05, 3) if has("min") else None, rng.random(3))
