@@ -311,8 +311,9 @@ size_t tree_verify_attn_kv8_workspace_bytes(int M, int P, int Hq, int Hkv, int D
 
 /* tree_verify_attn over an 8-bit cache of P + M rows: the attention over the values that w4a16_kv8_read returns.  Probabilities are rounded
  * to fp16 for the product with the values; softmax, sums and accumulation are fp32.  A row whose mask row is empty is padding (a tree
- * shorter than M): it sees nothing, committed rows included, and gets zeros.  What a mask hides may be anything, NaN scales and codes
- * included; a row that sees a key or value of scale NaN is NaN.  P <= 2^30; otherwise arguments, sizes and errors as tree_verify_attn, and `workspace` must
+ * shorter than M): it sees nothing, committed rows included, and gets zeros.  What a mask hides from a row may be anything, whoever else sees it:
+ * NaN scales, codes that are no numbers or, scaled, no fp16 numbers (the appends write none).  A row that sees a key or value of scale NaN is NaN; what a row that
+ * sees such a code gets is not finite for a value, unspecified for a key.  P <= 2^30; otherwise arguments, sizes and errors as tree_verify_attn, and `workspace` must
  * hold tree_verify_attn_kv8_workspace_bytes and have been initialised with w4a16_workspace_init (W4A16_EWORKSPACE otherwise). */
 int tree_verify_attn_kv8(const void *q, const void *k, const void *v, const void *k_scale, const void *v_scale, int format, const uint8_t *mask,
                          void *out, int M, int P, int Hq, int Hkv, int D, float scale, void *workspace, size_t workspace_bytes, void *stream);

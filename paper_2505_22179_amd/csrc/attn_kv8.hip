@@ -40,6 +40,25 @@ __device__ __forceinline__ void clear_codes(uint8_t *tile, uint32_t keys, int la
         if ((keys >> (8 * i + (lane >> 3))) & 1u) *reinterpret_cast<u32x4 *>(tile + i * 1024 + lane * 16) = (u32x4){0, 0, 0, 0};
     asm volatile("" ::: "memory");
 }
+// The keys of a step, in LDS, with V codes that are no numbers under their scales.  Nearly always there are none, and nothing but the first look is taken.
+template <int FMT>
+__device__ __forceinline__ uint32_t keys_without_numbers(const uint8_t *tile, const uint32_t *scales, int lane)
+{
+    bool suspect = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        suspect |= kv8_suspect<FMT>(FMT == kInt8 ? (u32x4){} : *reinterpret_cast<const u32x4 *>(tile + i * 1024 + lane * 16), scales[8 * i + (lane >> 3)]);
+    uint32_t keys = 0;
+    if (__builtin_expect(__any(suspect), 0)) {   // uniform
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t lanes = __ballot(kv8_no_numbers<FMT>(*reinterpret_cast<const u32x4 *>(tile + i * 1024 + lane * 16), scales[8 * i + (lane >> 3)]));
+#pragma unroll 1
+            for (int r = 0; r < 8; ++r) keys |= (uint32_t)(((lanes >> (8 * r)) & 0xFFu) != 0) << (8 * i + r);
+        }
+    }
+    return keys;
+}
 
 // ---- row tiles of at most 32 rows: wavefronts with K and V tiles of their own -------------------------------
 // As tree_attn_wave_kernel: eight wavefronts carry the same 32 rows, wavefront w takes key steps w, w + 8, ... of the workgroup's range and
@@ -184,7 +203,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
         // A scale that is no number marks a head that held an infinity or a NaN.  Such keys take no part in the products (a hidden one must
         // not reach the rows that do not see it): their scales are taken as zero and the scores of the rows that see them become NaN.
         const uint64_t nan_lanes = __ballot((scales[lane] & 0x7FFFu) >= kHalfInf);
-        const uint32_t bad = (uint32_t)nan_lanes | (uint32_t)(nan_lanes >> 32);   // bit i: key i of the step
+        uint32_t bad = (uint32_t)nan_lanes | (uint32_t)(nan_lanes >> 32);   // bit i: key i of the step
         uint32_t ks = scales[c];
         if ((ks & 0x7FFFu) >= kHalfInf) ks = 0;
         const _Float16 k_scale = __builtin_bit_cast(_Float16, (uint16_t)ks);
@@ -229,10 +248,13 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
             const uint32_t vis = seen >> (4 * h);
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = ((vis >> (8 * (i >> 2) + (i & 3))) & 1u) ? s[i] : -__builtin_inff();
-            uint32_t by_any = seen;
+            uint8_t *const values = mine + buf * kWaveBuf + kWaveTile;
+            uint32_t by_any = seen, strange = 0;   // keys that any row sees; keys whose values other rows are to be kept from (a single row has no others)
+            if (M > 1) strange = keys_without_numbers<FMT>(values, scales + 32, lane);
 #pragma unroll
             for (int off = 1; off < kWaveRows; off <<= 1) by_any |= (uint32_t)__shfl_xor((int)by_any, off, 64);
-            clear_codes(mine + buf * kWaveBuf + kWaveTile, ~by_any, lane);
+            bad |= strange;
+            clear_codes(values, strange | ~by_any, lane);
         }
         if (bad) {   // uniform, rare
             const uint32_t hit = (seen & bad) >> (4 * h);
@@ -476,14 +498,18 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_shared_kernel(const
         const int key0 = (b0 + t * WK + kw) * kKeyBlock;
         if (__builtin_expect(key0 + kKeyBlock > P, 0)) {   // uniform: the step has draft keys, which not every row sees
             // A scale that is no number marks a head that held an infinity or a NaN: taken as zero here, so that it does not reach the rows that
-            // do not see it, and noted for the scores of those that do.  What no row sees may never have been written: zero as well.
+            // do not see it, and noted for the scores of those that do; likewise V codes that are no numbers.  What no row sees may never have been
+            // written: zero as well.
             uint32_t bad = 0;
 #pragma unroll
             for (int i = 0; i < CL; ++i) {
-                const bool no_number = (scales[S][i] & 0x7FFFu) >= kHalfInf;
-                const uint64_t lanes = __ballot(no_number);
-#pragma unroll
-                for (int r = 0; r < 8; ++r) bad |= (uint32_t)((lanes >> (8 * r)) & 1) << (8 * ((rh * CL + i) & 3) + r);
+                bool no_number = false;
+                if (__builtin_expect(__any(kv8_suspect<FMT>(stages_k ? (u32x4){} : codes[S][i], scales[S][i])), 0)) {   // uniform
+                    no_number = (scales[S][i] & 0x7FFFu) >= kHalfInf || (!stages_k && kv8_no_numbers<FMT>(codes[S][i], scales[S][i]));
+                    const uint64_t lanes = __ballot(no_number);
+#pragma unroll 1
+                    for (int r = 0; r < 8; ++r) bad |= (uint32_t)(((lanes >> (8 * r)) & 0xFFu) != 0) << (8 * ((rh * CL + i) & 3) + r);
+                }
                 const int draft = key0 + step_key(i) - P;
                 if (no_number || (draft >= 0 && !(draft < 64 && ((any_bits >> (draft & 63)) & 1)))) codes[S][i] = (u32x4){0, 0, 0, 0}, scales[S][i] = 0;
             }

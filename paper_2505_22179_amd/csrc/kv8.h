@@ -88,6 +88,39 @@ __device__ __forceinline__ void kv8_values(uint32_t w, _Float16 scale, half2v &l
     }
 }
 
+// Codes that are no numbers, or no fp16 numbers under their head's scale (bits).  The appends write none, but what a mask hides may hold them, and a probability
+// of zero would make NaN of them.  kv8_suspect, for sixteen codes: whether there may be any -- an e4m3 byte of seven ones, or a scale under which the largest
+// number, 448 or 128, comes to 65520 or is none; kv8_no_numbers: whether there are (few come here, so its loop is a loop).
+template <int FMT>
+__device__ __forceinline__ bool kv8_suspect(uint32_t __attribute__((ext_vector_type(4))) w, uint32_t scale)
+{
+    constexpr uint32_t kLargest = FMT == kInt8 ? 0x5FFCu : 0x5800u;   // 511, 128
+    uint32_t ones = 0;
+    if constexpr (FMT == kE4m3) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ones |= (w[e] & 0x7F7F7F7Fu) + 0x01010101u;
+    }
+    return (ones & 0x80808080u) != 0 || (scale & 0x7FFFu) > kLargest;
+}
+template <int FMT>
+__device__ __forceinline__ bool kv8_no_numbers(uint32_t __attribute__((ext_vector_type(4))) w, uint32_t scale)
+{
+    const half2v s = {__builtin_bit_cast(_Float16, (uint16_t)scale), __builtin_bit_cast(_Float16, (uint16_t)scale)};
+    bool any = false;
+#pragma unroll 1
+    for (int e = 0; e < 4; ++e) {
+        half2v n[2];
+        kv8_numbers<FMT>(w[0], n[0], n[1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t x = __builtin_bit_cast(uint32_t, (half2v)(n[i] * s)) & 0x7FFF7FFFu;
+            any |= (x & 0xFFFFu) >= kHalfInf || x >= (kHalfInf << 16);
+        }
+        w = __builtin_shufflevector(w, w, 1, 2, 3, 0);
+    }
+    return any;
+}
+
 inline bool kv8_format_known(int format) { return format == kInt8 || format == kE4m3; }
 
 }  // namespace w4

@@ -389,3 +389,37 @@ def test_a_cache_of_more_than_4_gib(M, Hq):
     third = [t[P + 2].clone() for t in (k, v, ks, vs)]
     B.tree_accept_kv8(dev(parent), dev(token), dev(target), M, path, result, k, v, ks, vs, P, Hkv, D)
     assert result.tolist() == [2, M + 5] and all(torch.equal(t[P + 1], w) for t, w in zip((k, v, ks, vs), third))
+
+
+STRANGE = {   # (format, code, scale): values that no append writes -- no number, or beyond fp16
+    "nan": (B.KV8_E4M3, 0x7F, 0.25),
+    "minus_nan_zero_scale": (B.KV8_E4M3, 0xFF, np.nan),
+    "e4m3_beyond_fp16": (B.KV8_E4M3, 0x7E, 256.0),
+    "int8_beyond_fp16": (B.KV8_INT8, 0x80, 512.0),
+    "int8_infinite": (B.KV8_INT8, 0x7F, np.inf),
+}
+
+
+@pytest.mark.parametrize("strange", list(STRANGE))
+@pytest.mark.parametrize("M,P,Hq,Hkv", [(12, 96, 8, 2), (33, 31, 8, 1), (64, 1000, 28, 4), (60, 16001, 64, 8)])
+def test_codes_that_are_no_numbers_stay_with_the_rows_that_see_them(M, P, Hq, Hkv, strange):
+    """a draft key that some rows see and others do not: what it holds reaches the rows that see it, of its KV head, and leaves the others' bits alone"""
+    fmt, code, scale = STRANGE[strange]
+    print(f"attn_kv8 strange codes M={M} P={P} Hq={Hq} Hkv={Hkv} {strange}", flush=True)
+    c = Call(170 + M, M, P, Hq, Hkv, fmt, tree="random")
+    clean = c.run()
+    c.check(clean)
+    seen_by = c.mask.sum(0)
+    node = int(np.flatnonzero((seen_by > 1) & (seen_by < M))[-1])
+    sees, kvh = c.mask[:, node] != 0, Hkv - 1
+    heads = slice(kvh * (Hq // Hkv), Hq)
+    for which in "kv":
+        d = Call(170 + M, M, P, Hq, Hkv, fmt, tree="random")
+        getattr(d, which)[P + node, kvh, 77] = code
+        getattr(d, which + "s")[P + node, kvh] = scale
+        out = d.run()
+        same = np.ones((M, Hq), dtype=bool)
+        same[sees, heads] = False
+        np.testing.assert_array_equal(out[same].view(np.uint16), clean[same].view(np.uint16))
+        if which == "v":
+            assert not np.isfinite(out[sees, heads, 77].astype(np.float64)).any()
