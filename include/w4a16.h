@@ -160,7 +160,8 @@ size_t tree_verify_attn_workspace_bytes(int M, int P, int Hq, int Hkv, int D);
  * q, out fp16 [M, Hq, D]; k, v fp16 [P+M, Hkv, D] (draft keys at rows P..P+M-1); mask uint8 [M, M]
  * row-major.  Softmax and accumulation in fp32.  Requires D == 128, 1 <= M <= 64, Hq % Hkv == 0,
  * Hq/Hkv <= 8, P >= 0, a finite scale > 0 (W4A16_EINVAL otherwise), and every row must see at least
- * one key.  `workspace` as for w4a16_gemm,
+ * one key (one that sees none gets NaN).  A row with an empty mask row sees the committed keys; to tree_verify_attn_kv8 it is padding.
+ * `workspace` as for w4a16_gemm,
  * sized by tree_verify_attn_workspace_bytes and initialised by w4a16_workspace_init.  How the call is split
  * follows from its sizes alone, so every workspace of at least that size gives the same bits.  A smaller one is
  * refused, or -- where it still holds a simpler split of the call -- served with that one: a result of the

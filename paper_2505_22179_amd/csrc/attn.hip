@@ -1013,14 +1013,14 @@ __global__ __launch_bounds__(256) void tree_attn_merge_kernel(const float *__res
         den += wgt * ls[s];
         num += wgt * os[s];
     }
-    const float inv = den == 0.f ? 0.f : 1.f / den;   // as in merge_ranges
+    const float inv = 1.f / den;   // as in merge_ranges
     typedef _Float16 half4v __attribute__((ext_vector_type(4)));
     half4v hv = {(_Float16)(num[0] * inv), (_Float16)(num[1] * inv), (_Float16)(num[2] * inv), (_Float16)(num[3] * inv)};
     *reinterpret_cast<half4v *>(out + ((size_t)qrow * Hq + h) * kHeadDim + d4 * 4) = hv;
 }
 
-void launch_attn_merge(const float *part_o, const float *part_ml, void *out, int M, int Hq, int group, int ranges, int tile_rows,
-                       int tiles_per_kv, hipStream_t stream)
+static void launch_attn_merge(const float *part_o, const float *part_ml, void *out, int M, int Hq, int group, int ranges, int tile_rows,
+                              int tiles_per_kv, hipStream_t stream)
 {
     const int quads = M * Hq * (kHeadDim / 4);
     const dim3 grid((unsigned)((quads + 255) / 256));

@@ -172,7 +172,7 @@ __device__ __forceinline__ void merge_ranges(PartialBuffer unit_o, PartialBuffer
                 den += wgt * ls[it][s];
                 num += wgt * os[it][s];
             }
-            const float inv = padding || den == 0.f ? 0.f : 1.f / den;
+            const float inv = MARKS && (padding || den == 0.f) ? 0.f : 1.f / den;   // a row that sees no key: 0 / 0, as from one range
             if (padding) num = (float4v){0.f, 0.f, 0.f, 0.f};
             int qrow, h;
             tile.locate(trow, qrow, h);
@@ -231,9 +231,5 @@ __device__ __forceinline__ void read_transposed_rows(short4v &lo, short4v &hi, u
                  : "=&v"(lo), "=&v"(hi)
                  : "v"(lds_addr), "n"(OFFSET), "n"(OFFSET + 8 * 256));
 }
-
-// the merge by a second kernel (attn.hip)
-void launch_attn_merge(const float *part_o, const float *part_ml, void *out, int M, int Hq, int group, int ranges, int tile_rows,
-                       int tiles_per_kv, hipStream_t stream);
 
 }  // namespace w4

@@ -262,3 +262,20 @@ def test_constant_values_come_back_exactly():
         B.w4a16_set_param("attn_splits", splits)
         got = run_attn(a).astype(np.float32)
         assert np.abs(got - 0.375).max() <= 2.0 ** -11 * 0.375 * 2, np.abs(got - 0.375).max()
+
+
+def test_a_row_that_sees_no_key_is_nan_however_the_call_is_split():
+    """its sum is zero: the same bits from one key range and from several, by either merge, in every kernel"""
+    M, Hq, Hkv = 64, 16, 4
+    a = I.make_attn(9100, M, 0, Hq, Hkv, 128, tree="random", depth=6)
+    a.mask[[5, M - 1]] = 0
+    for row_tiles in (0, 2, 4):
+        B.w4a16_set_param("attn_row_tiles", row_tiles)
+        for pack in (1, 2, 4):
+            B.w4a16_set_param("attn_pack", pack)
+            for splits, merge in ((1, 0), (2, 1), (2, 2)):
+                B.w4a16_set_param("attn_splits", splits)
+                B.w4a16_set_param("attn_fused_merge", merge)
+                out = run_attn(a)
+                lost = np.isnan(out)
+                assert lost[[5, M - 1]].all() and lost.sum() == 2 * Hq * 128, (row_tiles, pack, splits, merge)
