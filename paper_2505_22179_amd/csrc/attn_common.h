@@ -172,7 +172,7 @@ __device__ __forceinline__ void merge_ranges(PartialBuffer unit_o, PartialBuffer
                 den += wgt * ls[it][s];
                 num += wgt * os[it][s];
             }
-            const float inv = MARKS && (padding || den == 0.f) ? 0.f : 1.f / den;   // a row that sees no key: 0 / 0, as from one range
+            const float inv = padding ? 0.f : 1.f / den;   // a row that sees no key, or none but scores of -inf: 0 / 0, as from one range
             if (padding) num = (float4v){0.f, 0.f, 0.f, 0.f};
             int qrow, h;
             tile.locate(trow, qrow, h);

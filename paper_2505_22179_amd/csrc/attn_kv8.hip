@@ -359,7 +359,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
         if (rho >= tile.rows) continue;
         if (l_all < 0.f) val = (float4v){0.f, 0.f, 0.f, 0.f}, l_all = kPaddingMark;
         if (last) {
-            if (l_all > 0.f || l_all != l_all) val *= 1.f / l_all;
+            if (!(l_all < 0.f)) val *= 1.f / l_all;   // 0 / 0 where every score is -inf
             typedef _Float16 half4v __attribute__((ext_vector_type(4)));
             half4v hv = {(_Float16)val[0], (_Float16)val[1], (_Float16)val[2], (_Float16)val[3]};
             int qrow, head;
@@ -705,7 +705,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_shared_kernel(const
         if (rho >= tile.rows) continue;
         if (of[0][1] < 0.f) val = (float4v){0.f, 0.f, 0.f, 0.f}, l_all = kPaddingMark;
         if (last) {
-            if (l_all > 0.f || l_all != l_all) val *= 1.f / l_all;
+            if (!(l_all < 0.f)) val *= 1.f / l_all;   // 0 / 0 where every score is -inf
             typedef _Float16 half4v __attribute__((ext_vector_type(4)));
             half4v hv = {(_Float16)val[0], (_Float16)val[1], (_Float16)val[2], (_Float16)val[3]};
             int qrow, head;
@@ -758,7 +758,7 @@ __global__ __launch_bounds__(256) void tree_attn_kv8_merge_kernel(const float *_
             num += wgt * os[s];
         }
     }
-    const float inv = padding || den == 0.f ? 0.f : 1.f / den;
+    const float inv = padding ? 0.f : 1.f / den;
     if (padding) num = (float4v){0.f, 0.f, 0.f, 0.f};
     typedef _Float16 half4v __attribute__((ext_vector_type(4)));
     half4v hv = {(_Float16)(num[0] * inv), (_Float16)(num[1] * inv), (_Float16)(num[2] * inv), (_Float16)(num[3] * inv)};

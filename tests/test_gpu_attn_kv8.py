@@ -423,3 +423,17 @@ def test_codes_that_are_no_numbers_stay_with_the_rows_that_see_them(M, P, Hq, Hk
         np.testing.assert_array_equal(out[same].view(np.uint16), clean[same].view(np.uint16))
         if which == "v":
             assert not np.isfinite(out[sees, heads, 77].astype(np.float64)).any()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,P,Hq,Hkv", [(1, 0, 8, 2), (3, 300, 8, 2), (40, 5000, 64, 8), (60, 16001, 64, 8)])
+def test_scores_that_are_all_minus_infinity_are_nan(M, P, Hq, Hkv, fmt):
+    """a row's weights are then 0 / 0, as in tree_verify_attn: by one range, by several and by either merge"""
+    c = Call(180 + M, M, P, Hq, Hkv, fmt)
+    c.k[:, :, 9] = 1 if fmt == B.KV8_INT8 else 0x38      # one: positive in every key
+    clean = c.run()
+    c.q[M - 1, 2, 9] = -np.inf
+    out = c.run()
+    assert np.isnan(out[M - 1, 2]).all()
+    out[M - 1, 2] = clean[M - 1, 2]
+    np.testing.assert_array_equal(out.view(np.uint16), clean.view(np.uint16))
