@@ -58,9 +58,10 @@ size_t w4a16_packed_bytes(int N, int K, int G);
  * a simpler split of the call -- served with that one: a result of the same accuracy with other roundings. */
 size_t w4a16_workspace_bytes(int M_max, int N, int K, int G);
 
-/* Zero the ticket area at the start of a workspace.  Must be enqueued once before the first
- * w4a16_gemm / tree_verify_attn that uses the buffer; each of those calls leaves the tickets zero
- * again, so one initialisation serves any number of later calls (of any shape that fits).  Two
+/* Zero the ticket area at the start of a workspace.  Must be enqueued once before the first call that uses the buffer
+ * and needs its tickets: w4a16_gemm and its fused forms, w4a16_decoder_layer, tree_verify_attn, tree_verify_attn_kv8, lm_head_sample.
+ * Each of those calls leaves the tickets zero again and lm_head_topk leaves them alone (in a workspace of its stated size), so one
+ * initialisation serves any number of later calls (of any kind and shape that fits).  Two
  * calls that may run concurrently must not share a workspace.  A workspace must be 256-byte aligned
  * (W4A16_EALIGN otherwise): workgroups exchange partial sums through it inside a kernel, cache line by
  * cache line, and no line may belong to two of them. */
@@ -334,8 +335,9 @@ size_t lm_head_packed_bytes(int V, int K);
  * `packed` receives lm_head_packed_bytes(V, K) bytes. */
 int lm_head_pack(const void *W, void *packed, int V, int K, void *stream);
 
-/* Scratch lm_head_topk wants for these sizes: softmax statistics of the logits in groups of 64 to 512 tokens.  Less is accepted,
- * down to ceil(V / 512) * M * (8 + 8 * top_k) + 256 bytes, where it may cost a pass over the logits. */
+/* Scratch lm_head_topk wants for these sizes: the ticket area, which it leaves alone, and softmax statistics of the logits in groups of
+ * 64 to 512 tokens.  Less is accepted, down to ceil(V / 512) * M * (8 + 8 * top_k) + 256 bytes, where it may cost a pass over the logits; the
+ * ticket area is then written, and w4a16_workspace_init is due before a call that needs it. */
 size_t lm_head_workspace_bytes(int M, int V, int K, int top_k);
 
 /* Draft-side language-model head with log-softmax and top-k (paper section 2.1: the draft model uses

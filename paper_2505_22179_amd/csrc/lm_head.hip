@@ -872,7 +872,7 @@ size_t lm_head_workspace_bytes(int M, int V, int K, int top_k)
 {
     if (check_lm_head(M, V, K, top_k) != W4A16_OK) return 0;
     const size_t least = lm_least_bytes(M, V, top_k), finest = (size_t)M * ((V + 63) / 64) * sizeof(LmStat);   // the smallest granules
-    return finest > least ? finest : least;
+    return kTicketBytes + (finest > least ? finest : least);
 }
 
 int lm_head_plan_describe(int M, int V, int K, int *out)
@@ -906,7 +906,9 @@ int lm_head_topk(const void *x, const void *packed, int M, int V, int K, int top
     // the logits kernel leaves its statistics; a workspace below the stated size may have room for coarser ones only, which then take a pass
     const bool fine = workspace_bytes >= (size_t)M * grid.x * sizeof(LmStat);
     const int granule = fine ? plan.nw * plan.twl * 16 : kLmChunk, granules = fine ? (int)grid.x : lm_chunks(V);
-    LmStat *const all_stats = reinterpret_cast<LmStat *>(workspace), *const stats = fine ? all_stats : nullptr;
+    // behind the tickets, which other calls on this workspace need at zero; a workspace below the stated size has no room for that
+    const size_t tickets = workspace_bytes >= lm_head_workspace_bytes(M, V, K, top_k) ? kTicketBytes : 0;
+    LmStat *const all_stats = reinterpret_cast<LmStat *>((uint8_t *)workspace + tickets), *const stats = fine ? all_stats : nullptr;
     if (plan.shared) {
 #define W4_LM_SHARED(MTL_, NW_, TWL_, D_)                                                                               \
     if (mtl == MTL_ && plan.nw == NW_ && plan.twl == TWL_)                                                              \

@@ -320,3 +320,36 @@ def test_random_rows_around_one_workgroups_row(V, limits):
     has = lambda n: n in limits or limits == "all"
     check(x, rng.uniform(0.4, 2.5, 3), rng.integers(1, 3000, 3) if has("k") else None, rng.uniform(0.3, 1, 3) if has("p") else None,
           rng.uniform(0, 0.05, 3) if has("min") else None, rng.random(3))
+
+
+@pytest.mark.parametrize("M,V", [(1, 20000), (7, 40000), (60, 33000)])
+def test_one_workspace_for_the_head_and_the_sampler(M, V):
+    """lm_head_topk keeps its statistics behind the tickets that lm_head_sample, the linears and the attention count with: one initialisation serves them all"""
+    K, top_k = 256, 3
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    half = lambda *s, std=1.0: (torch.randn(*s, generator=gen, device=DEV) * std).half()
+    x, W = half(M, K), half(V, K, std=0.1)
+    packed = torch.empty(B.lm_head_packed_bytes(V, K), dtype=torch.uint8, device=DEV)
+    B.lm_head_pack(W, packed, V, K)
+    rng = np.random.default_rng(M)
+    f = lambda a, t=torch.float32: torch.as_tensor(a, dtype=t, device=DEV)
+    limits = f(rng.uniform(0.5, 1.5, M)), f(rng.integers(1, 400, M), torch.int32), f(rng.uniform(0.5, 1.0, M)), f(rng.uniform(0, 0.05, M)), f(rng.random(M))
+
+    def step(head_ws, sample_ws):
+        logits, idx = torch.empty(M, V, device=DEV), torch.empty(M, top_k, dtype=torch.int32, device=DEV)
+        lp, token, prob = torch.empty(M, top_k, device=DEV), torch.full((M,), -1, dtype=torch.int32, device=DEV), torch.full((M,), -1.0, device=DEV)
+        B.lm_head_topk(x, packed, M, V, K, top_k, logits, idx, lp, head_ws)
+        B.lm_head_sample(logits, M, V, *limits, token, prob, sample_ws)
+        torch.cuda.synchronize()
+        return logits, idx, lp, token, prob
+
+    head_bytes, sample_bytes = B.lm_head_workspace_bytes(M, V, K, top_k), B.lm_head_sample_workspace_bytes(M, V)
+    want = step(torch.empty(head_bytes, dtype=torch.uint8, device=DEV), B.new_workspace(sample_bytes))
+    assert (want[3] >= 0).all()
+    shared = B.new_workspace(max(head_bytes, sample_bytes))
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(step(shared, shared), want))
+        assert not shared[:16384].any()
+    exact = B.new_workspace(head_bytes)
+    B.lm_head_topk(x, packed, M, V, K, top_k, *(torch.empty_like(t) for t in want[:3]), exact)
+    assert not exact[:16384].any()

@@ -111,3 +111,9 @@ def test_sample_workspace_serves_every_smaller_call():
     Vs = (1, 511, 513, 4096, 4097, 8192, 32000, 65537, 128256, 200001, 262144)
     sizes = np.array([[B.lm_head_sample_workspace_bytes(M, V) for V in Vs] for M in range(1, 65)])
     assert (np.diff(sizes, axis=0) >= 0).all() and (np.diff(sizes, axis=1) >= 0).all()
+
+
+@pytest.mark.parametrize("M,V,K,top_k", [(1, 1, 128, 1), (1, 32000, 4096, 10), (60, 128256, 8192, 1), (64, 262144, 4096, 16)])
+def test_the_lm_heads_workspace_has_a_ticket_area(M, V, K, top_k):
+    """16384 bytes at its start, behind which it keeps statistics of 64 tokens each: the tickets of other calls on the same workspace stay at zero"""
+    assert B.lm_head_workspace_bytes(M, V, K, top_k) >= 16384 + M * -(-V // 64) * 8
