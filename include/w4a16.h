@@ -442,6 +442,13 @@ int w4a16_plan_describe(int M, int N, int K, int G, int *out);
  * workspace gets too.  Host only: touches no GPU.  Errors as tree_verify_attn's size and workspace checks. */
 int tree_verify_attn_plan_describe(int M, int P, int Hq, int Hkv, int D, size_t workspace_bytes, int *out);
 
+/* How tree_verify_attn_kv8 splits a call, so that a test can show which kernels, splits and merges it has compared with the oracle.  out receives
+ * 5 ints: [0] rows of a row tile (the last may have fewer), [1] row tiles per KV head, [2] key ranges per tile, [3] 1 if the last workgroup
+ * of a tile merges its ranges (else a second kernel does, where there are several), [4] 1 for the kernel whose workgroups share tiles of up to 128 rows,
+ * 0 for the one whose wavefronts bring key tiles of their own to up to 32.  Host only: touches no GPU.  Errors as tree_verify_attn_kv8's checks of
+ * format and sizes. */
+int tree_verify_attn_kv8_plan_describe(int M, int P, int Hq, int Hkv, int D, int format, int *out);
+
 /* The logits kernel lm_head_topk would run with the current knobs.  out receives 3 ints: [0] 1 if the wavefronts of a
  * workgroup share x through LDS, 0 if each fetches its own, [1] wavefronts per workgroup, [2] vocabulary tiles per
  * wavefront.  16 wavefronts mean the kernel that keeps x in LDS: four of them share each of the workgroup's four tiles,

@@ -19,7 +19,7 @@ EXPORTS = (
     "tree_verify_attn", "tree_accept", "rms_norm", "rope_append", "lm_head_workspace_bytes", "lm_head_topk",
     "lm_head_packed_bytes", "lm_head_pack", "w4a16_decoder_layer", "w4a16_plan_describe", "w4a16_gemm_static", "w4a16_weight_is_symmetric",
     "tree_verify_attn_plan_describe", "lm_head_plan_describe", "rope_append_qk_norm", "rope_append_kv8", "w4a16_kv8_read", "tree_accept_kv8",
-    "tree_verify_attn_kv8", "tree_verify_attn_kv8_workspace_bytes", "lm_head_sample", "lm_head_sample_workspace_bytes",
+    "tree_verify_attn_kv8", "tree_verify_attn_kv8_workspace_bytes", "tree_verify_attn_kv8_plan_describe", "lm_head_sample", "lm_head_sample_workspace_bytes",
 )
 
 EPI_NONE, EPI_RESIDUAL, EPI_SILU_MUL = 0, 1, 2
@@ -94,6 +94,7 @@ def load() -> ctypes.CDLL:
     L.tree_verify_attn_kv8_workspace_bytes.restype = sz
     L.tree_verify_attn_kv8_workspace_bytes.argtypes = [i, i, i, i, i]
     L.tree_verify_attn_kv8.argtypes = [vp, vp, vp, vp, vp, i, vp, vp, i, i, i, i, i, ctypes.c_float, vp, sz, vp]
+    L.tree_verify_attn_kv8_plan_describe.argtypes = [i, i, i, i, i, i, ctypes.POINTER(ctypes.c_int)]
     L.tree_accept_kv8.argtypes = [vp, vp, vp, i, vp, vp, vp, vp, vp, vp, i, i, i, vp]
     L.w4a16_decoder_layer.argtypes = [ctypes.POINTER(LayerWeights), vp, i, i, vp, vp, vp, i, vp, vp, vp,
                                       ctypes.POINTER(LayerScratch), vp]
@@ -398,6 +399,13 @@ def tree_verify_attn_kv8(q, k, v, k_scale, v_scale, fmt: int, mask, out, M: int,
         0 if workspace is None else workspace.numel() * workspace.element_size(), _raw_stream(_current_device()))
     if rc:
         _check(rc, "tree_verify_attn_kv8")
+
+
+def tree_verify_attn_kv8_plan_describe(M: int, P: int, Hq: int, Hkv: int, D: int, fmt: int) -> tuple:
+    """(rows of a row tile, row tiles per KV head, key ranges per tile, merged by the tile's last workgroup, tiles of up to 128 rows); host only."""
+    out = (ctypes.c_int * 5)()
+    _check(load().tree_verify_attn_kv8_plan_describe(M, P, Hq, Hkv, D, fmt, out), "tree_verify_attn_kv8_plan_describe")
+    return tuple(out)
 
 
 def tree_accept_kv8(parent, token, target, M: int, path, result, k, v, k_scale, v_scale, P: int, Hkv: int, D: int) -> None:

@@ -766,10 +766,11 @@ __global__ __launch_bounds__(256) void tree_attn_kv8_merge_kernel(const float *_
 }
 
 // How a call is cut up: even row tiles of up to 32 row_groups rows, key ranges per tile, who merges the ranges.
-struct Kv8Plan { int row_groups, tile_rows, tiles_per_kv, ranges, fused, time; };
+struct Kv8Plan { int row_groups, tile_rows, tiles_per_kv, ranges, fused; int64_t time; };
 static int kv8_steps(int M, int P) { return (P + M + kKeyBlock - 1) / kKeyBlock; }
 
-// The number of ranges with the smallest estimate, at most one workgroup per CU (which also bounds the partial results).  Estimates are in hundredths of a
+// The number of ranges with the smallest estimate.  Where tiles have several, there is at most one workgroup per CU (which also bounds the partial results);
+// more tiles than CUs take one range each and go in turns, since LDS holds one workgroup.  Estimates are in hundredths of a
 // microsecond.  Those of the wave kernel were fitted over 38 sizes (1 to 64 query rows, 2 to 16 KV heads, 64 to 131072 keys, both formats) with
 // up to 19 numbers of ranges and both ways to merge them; the number they pick is 1 % slower than the best in the mean, 9 % at most.
 static Kv8Plan kv8_cut(int pairs, int Hkv, int steps, int row_groups, int format)
@@ -781,18 +782,19 @@ static Kv8Plan kv8_cut(int pairs, int Hkv, int steps, int row_groups, int format
     int most = kChipTiles / units;
     most = most > kMaxRanges ? kMaxRanges : most;
     most = most > steps ? steps : most;
-    p.time = 0x7FFFFFFF;
+    p.time = INT64_MAX;
     for (int r = 1; r <= (most < 1 ? 1 : most); ++r) {
-        const int range = (steps + r - 1) / r;   // steps of the longest
+        const int64_t range = (steps + r - 1) / r;   // steps of the longest
+        const int turns = (units * r + kChipTiles - 1) / kChipTiles;
         bool fused = false;
-        int time;
+        int64_t time;
         if (row_groups == 1) {
             const int slots = r <= 4 ? 4 : r <= 8 ? 8 : r <= 16 ? 16 : kMaxRanges;   // ranges that the merge is compiled for
             const int by_kernel = 240 + 7 * slots, by_last = 60 + (32 * rows + (3 * rows + 80) * slots) / 10;
             fused = r > 1 && units <= kMaxTickets && by_last < by_kernel;
-            time = 580 + 7 * rows + range * (format == kInt8 ? 24 : 19) + (r == 1 ? 0 : fused ? by_last : by_kernel);
+            time = turns * (580 + 7 * rows + range * (format == kInt8 ? 24 : 19)) + (r == 1 ? 0 : fused ? by_last : by_kernel);
         } else {   // a round: a step of each key group
-            time = 1100 + (range + kWaves / row_groups - 1) / (kWaves / row_groups) * 110 + (r == 1 ? 0 : 350);
+            time = turns * (1100 + (range + kWaves / row_groups - 1) / (kWaves / row_groups) * 110) + (r == 1 ? 0 : 350);
         }
         if (time < p.time) p.ranges = r, p.fused = fused, p.time = time;
     }
@@ -809,6 +811,14 @@ static Kv8Plan kv8_cut(int pairs, int Hkv, int steps, int row_groups, int format
 //   37, 28/4, 60000          72.3  63.7     59.7  62.4
 //   16, 64/8, 32000          41.3  33.7     35.4  33.1
 //   64, 16/16, 16000         27.4  29.7     24.7  29.8
+// and where the wave kernel takes more than one turn (two, four, four, eight):
+//   64, 256/32, 16001        271.7 159.7    207.2 155.9
+//   64, 512/64,  2000        91.0  49.1     77.8  48.3
+//   64, 512/64, 16001        502.7 300.6    419.7 302.2
+//   64, 1024/128, 3000       235.3 129.8    204.2 128.3
+//   33, 1024/128,  40        36.7  23.1     36.6  22.6     (five turns and two)
+//    8, 4096/512, 4000       197.5 181.1    190.6 181.4    (four turns and two)
+// The estimates take the slower kernel at the last of these, by 5 to 9 %, and at 37 rows of 28/4 heads over 16000 int8 keys, by up to 5 %.
 static Kv8Plan kv8_plan(int M, int P, int Hq, int Hkv, int format)
 {
     const int pairs = Hq / Hkv * M, steps = kv8_steps(M, P);
@@ -867,6 +877,21 @@ size_t tree_verify_attn_kv8_workspace_bytes(int M, int P, int Hq, int Hkv, int D
 {
     if (check_attn_kv8(M, P, Hq, Hkv, D) != W4A16_OK) return 0;
     return kTicketBytes + (size_t)kChipTiles * kSharedRows * (kHeadDim + 2) * sizeof(float);
+}
+
+int tree_verify_attn_kv8_plan_describe(int M, int P, int Hq, int Hkv, int D, int format, int *out)
+{
+    if (!out) return W4A16_ENULL;
+    if (!kv8_format_known(format)) return W4A16_EINVAL;
+    const int rc = check_attn_kv8(M, P, Hq, Hkv, D);
+    if (rc != W4A16_OK) return rc;
+    const Kv8Plan pl = kv8_plan(M, P, Hq, Hkv, format);
+    out[0] = pl.tile_rows;
+    out[1] = pl.tiles_per_kv;
+    out[2] = pl.ranges;
+    out[3] = pl.fused;
+    out[4] = pl.row_groups != 1;
+    return W4A16_OK;
 }
 
 int tree_verify_attn_kv8(const void *q, const void *k, const void *v, const void *k_scale, const void *v_scale, int format, const uint8_t *mask,

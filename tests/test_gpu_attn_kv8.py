@@ -437,3 +437,44 @@ def test_scores_that_are_all_minus_infinity_are_nan(M, P, Hq, Hkv, fmt):
     assert np.isnan(out[M - 1, 2]).all()
     out[M - 1, 2] = clean[M - 1, 2]
     np.testing.assert_array_equal(out.view(np.uint16), clean.view(np.uint16))
+
+
+PLANS = [   # M, P, Hq, Hkv, formats, what the call's plan has to be: rows of a tile, tiles per KV head, ranges, last workgroup merges, tiles of up to 128 rows
+    (1, 700, 64, 8, FORMATS, (8, 1, None, 1, 0)),            # tiles of 32 rows: merged by their last workgroup,
+    (12, 33000, 64, 8, [B.KV8_E4M3], (32, 3, 10, 0, 0)),     # by a second kernel,
+    (64, 100, 64, 64, FORMATS, (32, 2, 1, 0, 0)),            # one range
+    (5, 77, 1024, 1024, FORMATS, (5, 1, 1, 0, 0)),           # 1024 workgroups
+    (64, 8191, 64, 8, FORMATS, (128, 4, 8, 0, 1)),           # tiles of 128 rows
+    (37, 24000, 28, 4, [B.KV8_INT8], (87, 3, 21, 0, 1)),
+    (12, 64000, 64, 8, [B.KV8_E4M3], (96, 1, 32, 0, 1)),
+    (64, 500, 512, 64, FORMATS, (128, 4, 1, 0, 1)),          # one range: 256 workgroups
+    (33, 40, 1024, 128, FORMATS, (88, 3, 1, 0, 1)),          # 384
+    (8, 300, 4096, 512, FORMATS, (64, 1, 1, 0, 1)),          # 512
+    (64, 0, 512, 64, FORMATS, (128, 4, 1, 0, 1)),
+]
+
+
+@pytest.mark.parametrize("M,P,Hq,Hkv,fmt,plan", [(*c[:4], fmt, c[5]) for c in PLANS for fmt in c[4]])
+def test_every_kind_of_plan(M, P, Hq, Hkv, fmt, plan):
+    """parity, rows of padding, hidden rows that hold anything and NaN keys, with the kernel and the merge that run known"""
+    print(f"attn_kv8 plan M={M} P={P} Hq={Hq} Hkv={Hkv} fmt={fmt}", flush=True)
+    got = B.tree_verify_attn_kv8_plan_describe(M, P, Hq, Hkv, D, fmt)
+    assert all(w is None or g == w for g, w in zip(got, plan)), got
+    c = Call(190 + M + P, M, P, Hq, Hkv, fmt)
+    n = M - M // 4
+    c.mask[n:], c.mask[:, n:] = 0, 0
+    clean = c.run()
+    c.check(clean)
+    assert (clean[n:] == 0).all()
+    rng = np.random.default_rng(M)
+    for codes, scales in ((c.k, c.ks), (c.v, c.vs)):
+        codes[P + n:] = rng.choice(np.array([0x7F, 0xFF, 0x80, 0x7E], dtype=np.uint8), codes[P + n:].shape)
+        scales[P + n:] = rng.choice(np.array([np.nan, np.inf, -np.inf, 65504.0, 1.0], dtype=np.float16), scales[P + n:].shape)
+    np.testing.assert_array_equal(c.run().view(np.uint16), clean.view(np.uint16))
+    if M > 1:   # a draft key that not every node sees
+        node, group = int(np.argmin(c.mask[:n, :n].sum(0))), Hq // Hkv
+        c.vs[P + node, 0], c.v[P + node, 0] = np.nan, 0
+        out, sees = c.run(), c.mask[:, node] != 0
+        assert np.isnan(out[sees, :group]).all()
+        out[sees, :group] = clean[sees, :group]
+        np.testing.assert_array_equal(out.view(np.uint16), clean.view(np.uint16))

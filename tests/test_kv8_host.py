@@ -117,3 +117,40 @@ def test_sample_workspace_serves_every_smaller_call():
 def test_the_lm_heads_workspace_has_a_ticket_area(M, V, K, top_k):
     """16384 bytes at its start, behind which it keeps statistics of 64 tokens each: the tickets of other calls on the same workspace stay at zero"""
     assert B.lm_head_workspace_bytes(M, V, K, top_k) >= 16384 + M * -(-V // 64) * 8
+
+
+def plan(M, P, Hq, Hkv, fmt):
+    return B.tree_verify_attn_kv8_plan_describe(M, P, Hq, Hkv, 128, fmt)
+
+
+def test_attn_kv8_plan_describe_refuses():
+    f, out = B.load().tree_verify_attn_kv8_plan_describe, (ctypes.c_int * 5)()
+    assert f(60, 2048, 64, 8, 128, B.KV8_INT8, out) == 0 and f(60, 2048, 64, 8, 128, B.KV8_INT8, None) == ENULL
+    for sizes in ((0, 1, 8, 8, 128), (1, -1, 8, 8, 128), (1, 1, 9, 8, 128)):
+        assert f(*sizes, B.KV8_E4M3, out) == EINVAL
+    assert f(60, 2048, 64, 8, 128, 0, out) == EINVAL
+    for sizes in ((65, 1, 8, 8, 128), (1, 1, 8, 8, 64), (1, 2 ** 30 + 1, 8, 8, 128), (1, 1, 72, 8, 128), (1, 1, 4097, 4097, 128)):
+        assert f(*sizes, B.KV8_E4M3, out) == EUNSUP
+
+
+@pytest.mark.parametrize("fmt", [B.KV8_INT8, B.KV8_E4M3])
+def test_attn_kv8_plans_cover_the_call(fmt):
+    """every row in a tile, every key step in a range, partial results within the workspace, tickets within their area"""
+    for Hq, Hkv in ((1, 1), (7, 1), (8, 8), (28, 4), (64, 8), (128, 128), (512, 64), (4096, 512), (4096, 4096)):
+        for M in (1, 2, 5, 17, 33, 64):
+            for P in (0, 31, 100, 2048, 16001, 131072, 2 ** 30):
+                rows, tiles, ranges, fused, tall = plan(M, P, Hq, Hkv, fmt)
+                pairs, pad = Hq // Hkv * M, 128 if tall else 32
+                assert 1 <= rows <= pad and (tiles - 1) * rows < pairs <= tiles * rows
+                assert 1 <= ranges <= min(32, -(-(P + M) // 32))
+                assert ranges == 1 or Hkv * tiles * ranges <= 256
+                assert not fused or (ranges > 1 and not tall and Hkv * tiles <= 4096)
+
+
+@pytest.mark.parametrize("fmt", [B.KV8_INT8, B.KV8_E4M3])
+@pytest.mark.parametrize("M,P,Hq,Hkv", [(64, 0, 512, 64), (64, 16001, 256, 32), (64, 16001, 512, 64), (64, 3000, 1024, 128), (24, 4000, 1024, 256), (64, 100, 192, 192)])
+def test_more_row_tiles_than_compute_units_go_in_turns(M, P, Hq, Hkv, fmt):
+    """LDS holds one workgroup per compute unit: tiles of 32 rows would take two to eight turns, tiles of 128 take one or two"""
+    pairs = Hq // Hkv * M
+    assert Hkv * -(-pairs // 32) > 256
+    assert plan(M, P, Hq, Hkv, fmt)[4] == 1
