@@ -2,9 +2,9 @@
 // include/w4a16.h.
 //
 // A token's weight is w = exp((x - max) / T), evaluated in fp64 and held as a whole number of 2^-44: sums of whole numbers do not depend
-// on their order, so any split of a row gives the same token, and a border (a cumulative weight against p, or against u) is off by 1e-11
-// of the row's total where sums in fp32 would be off by 1e-5 -- tokens near a border would change with the split.  Tokens more than e^31 below the
-// row's largest weigh nothing (262144 of them 1e-8 of the total at most) and take part in nothing.
+// on their order, so any split of a row gives the same token, and a border (a cumulative weight against p, or against u) is off by at most V 2^-45
+// of the row's total (the largest weight is 1; 7.5e-9 for 262144 tokens) where sums in fp32 would be off by 1e-5 -- tokens near a border would change with
+// the split.  Tokens more than e^31 below the row's largest weigh nothing (262144 of them 9e-9 of the total at most) and take part in nothing.
 //
 // Short rows take one kernel, a workgroup per row (sample_row_kernel).  Longer ones take three, each of several workgroups per
 // row, that pass over the logits once:
@@ -13,12 +13,21 @@
 //                        few bins in which the limits of top-k and top-p fall, whatever the rounding.  Not launched without such limits.
 //   sample_draw_kernel   exact weight of what certainly stays, by segments of 512 tokens, and a list of the tokens in those few bins; the row's last
 //                        workgroup sorts the list, which gives the exact cut, draws the segment and then the token inside it
-// A list of more than kList tokens (thousands of nearly equal logits) is given up: the last workgroup then finds the cut by digits of the logits.
+// A list of more than kList tokens is given up: the last workgroup then finds the cut by digits of the logits, in some seven passes over the row by itself.
+// Thousands of nearly equal logits come to that, and so does a top-p border among many small weights: bins are (largest - smallest) / 1024 wide, and the border is
+// known to 2^-16 of the row's weight (find_cut).  Normal logits of standard deviation 2.2 with some larger ones, us by top-p (none: no limits):
+//   tokens, rows, T       none  0.9   0.99  0.995 0.999 0.9999
+//   128256,  1, 1.0       12.7  22.0  23.8  24.3  30.4  642
+//   128256,  1, 1.5       12.6  25.8  25.7  26.2  25.8  27.8
+//   128256, 60, 1.0       33.6  49.5  51.7  52.2  1138  1152
+//   262144,  1, 1.0       14.0  24.7  26.8  28.6  1249  1150
+//   262144, 60, 1.0       54.5  76.3  77.5  81.5  2258  2292
+//   262144, 60, 1.5       54.6  86.4  2081  2224  1472  2276
 // Measured, the three kernels: 1 row of 32000 tokens, top-k 4 + 8 + 9 us; 7 rows of 128256, top-p 4 + 9 + 16; 60 rows of 128256, all limits
 // 8 + 14 + 18, where reading the logits once takes 6.  What bounds them: for few rows the chain of dependent steps (three launches, two meetings of a
 // row's workgroups, each several trips to memory); for many the vector units, which put every token in its bin and weigh the kept ones in fp64.
-// One kernel for the first two, with bins of each workgroup's own width that its row's last one puts together, was no faster (21.0, 30.0 and 39.6 us in
-// all, against 21.6, 28.2 and 41.9).
+// One kernel for the first two, with bins of each workgroup's own width that its row's last one puts together, took 21.0, 30.0 and 39.6 us in all, against
+// 21.6, 28.2 and 41.9 at the time: 3 and 5 % less at two of these sizes, 6 % more at the other, and not taken for that.
 #include "internal.h"
 #include "devscope.h"
 
@@ -929,7 +938,8 @@ using namespace w4;
 extern "C" {
 
 // How a call's rows are split: about 512 workgroups at most, two per CU at work together.  More would wait for the first ones, in each of
-// which a few us pass before the first logit is looked at: 60 rows of 128256 tokens take 42 us with 512, 54 with 1024, 44 with 256.
+// which a few us pass before the first logit is looked at: with 384, 512, 768 and 1024, 60 rows of 128256 tokens take 42.8, 40.7, 42.7 and 48 us with all
+// limits, 56, 51.6, 52.7 and 55.8 with top-p, 30 rows 33.4, 34.6, 34.6 and 40.7.
 constexpr int kMost = 512;
 static_assert((kChunks * W4A16_MAX_M + kMost - 1) / kMost * kChunk < 1 << 16, "a bin counts the tokens of a group in 16 bits");
 static void sample_split(int M, int V, SampleArgs &a)

@@ -353,3 +353,42 @@ def test_one_workspace_for_the_head_and_the_sampler(M, V):
     exact = B.new_workspace(head_bytes)
     B.lm_head_topk(x, packed, M, V, K, top_k, *(torch.empty_like(t) for t in want[:3]), exact)
     assert not exact[:16384].any()
+
+
+@pytest.mark.parametrize("limits", ["p", "kp", "all"])
+@pytest.mark.parametrize("V,T", [(128256, 1.0), (262144, 1.0), (262144, 1.5), (12000, 1.0)])
+@pytest.mark.parametrize("p", [0.95, 0.999, 0.9999, 0.99999])
+def test_top_p_next_to_one(V, T, p, limits):
+    """Thousands of small weights lie around the border.  Half of the rows fall with the index, so that a uniform number next to one draws the border's
+    token.  The definition leaves a border open by b = V (2^-45 + e^-31) of the row's weight, in top_p and in u: the token has to be one that a cut and a draw
+    within b give."""
+    print(f"sample V={V} T={T} top_p={p} {limits}", flush=True)
+    M = 6
+    x, rng = rows(V, M, V)
+    x[M // 2:] = -np.sort(-x[M // 2:], axis=1)
+    u = np.array([0.0, 0.5, 1 - 2.0 ** -24, 0.3125, 1 - 2.0 ** -20, 1 - 2.0 ** -24])
+    k = np.full(M, V * 3 // 4) if limits != "p" else None
+    q = 1e-7 if limits == "all" else None
+    token, prob = run(x, T, k, p, q, u)
+    b, p32, q32 = V * (2.0 ** -45 + 3.5e-14), float(np.float32(p)), float(np.float32(1e-7))
+    for m in range(M):
+        order = np.argsort(-x[m], kind="stable")[:V if k is None else k[m]]
+        w = np.exp((x[m][order].astype(np.longdouble) - np.longdouble(x[m].max())) / T)
+        w[w < np.exp(np.longdouble(-31))] = 0
+        before = (np.cumsum(w) - w) / w.sum()
+        found = []
+        for cut in (p32 - b, p32 + b):
+            kept = order[:max(1, int((before < cut).sum()))]
+            share = w[:len(kept)].copy()
+            if q is not None:
+                share[1:][share[1:] < q32] = 0
+            by_index = np.argsort(kept)
+            kept, share = kept[by_index], share[by_index]
+            upto = np.cumsum(share) / share.sum()
+            last = np.flatnonzero(share)[-1]
+            for draw in (u[m] - b, u[m] + b):
+                found.append(int(kept[min(int(np.searchsorted(upto, draw, side="right")), last)]))
+            place = int(np.searchsorted(kept, token[m]))
+        assert min(found) <= token[m] <= max(found) and kept[place] == token[m] and share[place] > 0, (m, token[m], found)
+        want = float(share[place] / share.sum())
+        assert abs(prob[m] - want) <= want * (2.0 ** -23 + 4 * b), (m, prob[m], want)
