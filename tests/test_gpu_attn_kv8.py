@@ -478,3 +478,58 @@ def test_every_kind_of_plan(M, P, Hq, Hkv, fmt, plan):
         assert np.isnan(out[sees, :group]).all()
         out[sees, :group] = clean[sees, :group]
         np.testing.assert_array_equal(out.view(np.uint16), clean.view(np.uint16))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,P,Hq,Hkv,tall", [(1, 6000, 8, 8, 0), (16, 6000, 128, 128, 0), (60, 16001, 64, 8, 1), (16, 6000, 1032, 129, 1)])
+def test_probabilities_below_the_normal_range_of_fp16_count(M, P, Hq, Hkv, tall, fmt):
+    """One committed key scores 15.5 binary orders above all others, which weigh w = 2^-15.5 each: its value is 0, theirs is 1, so an output is n w / (1 + n w).
+    Each w is rounded by at most 2^-25."""
+    assert B.tree_verify_attn_kv8_plan_describe(M, P, Hq, Hkv, D, fmt)[4] == tall
+    print(f"attn_kv8 small probabilities M={M} P={P} Hq={Hq} Hkv={Hkv} fmt={fmt}", flush=True)
+    one = 1 if fmt == B.KV8_INT8 else 0x38
+    T = P + M
+    k, v = torch.zeros(T, Hkv, D, dtype=torch.uint8, device=DEV), torch.full((T, Hkv, D), one, dtype=torch.uint8, device=DEV)
+    ks, vs = torch.ones(T, Hkv, dtype=torch.float16, device=DEV), torch.ones(T, Hkv, dtype=torch.float16, device=DEV)
+    q, out = torch.zeros(M, Hq, D, dtype=torch.float16, device=DEV), torch.empty(M, Hq, D, dtype=torch.float16, device=DEV)
+    q[:, :, 5] = 64.0
+    scale = 15.5 * np.log(2.0) / 64.0
+    mask, ws = dev(np.tril(np.ones((M, M), dtype=np.uint8))), B.new_workspace(B.tree_verify_attn_kv8_workspace_bytes(M, P, Hq, Hkv, D))
+    for at in (0, 31, P // 2, P - 1):
+        k[at, :, 5], v[at] = one, 0
+        B.tree_verify_attn_kv8(q, k, v, ks, vs, fmt, mask, out, M, P, Hq, Hkv, D, scale, ws)
+        torch.cuda.synchronize()
+        k[at, :, 5], v[at] = 0, one
+        n = P + np.arange(M)[:, None, None]      # others than `at` that row i sees
+        w = 2.0 ** -15.5
+        want = n * w / (1 + n * w)
+        # a weight's rounding, the scores' (15.5 in fp32, a few steps of 2^-20) and the output's
+        tol = n * 2.0 ** -25 + want * (2.0 ** -11 + 2.0 ** -17)
+        err = np.abs(out.cpu().numpy().astype(np.float64) - want)
+        assert (err <= tol).all(), (at, (err / tol).max())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,P,Hq,Hkv", [(9, 700, 16, 4), (60, 16001, 64, 8)])
+def test_values_and_keys_below_the_normal_range_of_fp16(M, P, Hq, Hkv, fmt):
+    """scales at the formats' lower end: every value, then every key, is a subnormal fp16 number"""
+    c = Call(200 + M, M, P, Hq, Hkv, fmt)
+    rng = np.random.default_rng(M)
+    if fmt == B.KV8_INT8:
+        least = lambda codes: (codes, (rng.integers(1, 4, (P + M, Hkv)) * 2.0 ** -24).astype(np.float16))
+    else:   # codes of up to 1.875 times 2^-15
+        least = lambda codes: ((codes & 0x80) | rng.integers(1, 0x40, codes.shape).astype(np.uint8), np.full((P + M, Hkv), 2.0 ** -15, dtype=np.float16))
+    v, vs = c.v, c.vs
+    c.v, c.vs = least(c.v)
+    out = c.run()
+    k64, v64 = R.kv8_values(c.k, c.ks, fmt), R.kv8_values(c.v, c.vs, fmt)
+    assert np.abs(v64).max() < 2.0 ** -14
+    want, spread = R.tree_verify_attn_seen(c.q, k64, v64, c.mask, c.scale)
+    qk = np.abs(c.q.astype(np.float64)).sum(-1).max() * np.abs(k64).max() * c.scale      # above every sum |q k| scale
+    tol = spread * (2.0 ** -11 * 1.01 + 2 * 128 * 2.0 ** -24 * qk) + (P + M) * 2.0 ** -25 * np.abs(v64).max() + 2.0 ** -25 * 1.01   # the output is a multiple of 2^-24
+    assert (np.abs(out.astype(np.float64) - want) <= tol).all()
+    c.v, c.vs = v, vs
+    c.k, c.ks = least(c.k)
+    c.q = (c.q.astype(np.float32) * 2000).astype(np.float16)
+    assert np.abs(R.kv8_values(c.k, c.ks, fmt)).max() < 2.0 ** -14
+    c.check(c.run())
