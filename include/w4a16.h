@@ -292,7 +292,7 @@ int rope_append_qk_norm(const void *qkv, const void *q_gamma, const void *k_gamm
  *                   up to a power of two, at least 2^-15; code = x / scale rounded to the nearest (ties to even), saturating at
  *                   +-448, at +-240 where the scale is 256
  * Code times scale always is an fp16 number, the value the cache stands for.  A head with an infinity or a NaN in it gets codes 0 and
- * scale NaN: all its values are NaN. */
+ * scale NaN: all its values are NaN.  The cache can hold any D that 8 divides up to 512; tree_verify_attn_kv8 reads D == 128. */
 #define W4A16_KV8_INT8 1
 #define W4A16_KV8_E4M3 2
 

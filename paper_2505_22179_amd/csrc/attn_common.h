@@ -19,7 +19,8 @@ constexpr int kMaxRanges = 32;   // of any plan (the merge keeps one value per r
 constexpr int kChipTiles = 256;  // tiles x ranges of the plans that are picked by predicted time: one workgroup per compute unit
 
 // v_max3_f32 and v_max_f32 as they stand: fmaxf chains are compiled with a canonicalising v_max x, x per
-// operand, which doubles the instruction count of a row maximum; no score here is a NaN.
+// operand, which doubles the instruction count of a row maximum.  They pass over a NaN (the scores that the 8-bit kernels make NaN): it need
+// not be in the maximum to reach the row's sum and outputs, since its exponential is NaN whatever the maximum.
 // The compiler adds no wait states before inline assembly: results of matrix instructions pass through settled() first.
 __device__ __forceinline__ float max_of_three(float a, float b, float c)
 {
@@ -75,7 +76,7 @@ constexpr float kLowest = -1.0e30f;   // "no key seen yet": finite, so differenc
 
 // The rows of a row tile.  The group * M (head, query row) pairs that share a KV head, head by head, are cut into
 // tiles_per_kv tiles of tile_rows rows (the last may have fewer): M for one query head per tile, d * M for d heads, or any
-// other number up to 64, where a tile ends inside a head.  Row rho of tile `unit` is pair first + rho of its KV head.
+// other number up to the kernel's tallest tile, 32, 64 or 128 rows, where a tile ends inside a head.  Row rho of tile `unit` is pair first + rho of its KV head.
 struct RowTile {
     int kvh, group, M, Hq;
     int first;    // pair of tile row 0
@@ -215,7 +216,7 @@ __device__ __forceinline__ void row_to_lds(const uint8_t *src, uint8_t *lds_base
     __builtin_amdgcn_global_load_lds((global_void *)src, (lds_void *)lds_base, 16, 0, 0);
 }
 
-// the whole group cut evenly into as few tiles as 64 rows allow; a tile may end inside a head
+// the whole group cut evenly into as few tiles as `most` rows allow; a tile may end inside a head
 static void even_tiles(int pairs, int most, int &tile_rows, int &tiles_per_kv)
 {
     const int n = (pairs + most - 1) / most;

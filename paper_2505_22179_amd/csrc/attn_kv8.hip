@@ -394,7 +394,8 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kv8_wave_kernel(const K
 // A round is two phases, products (with the next round's conversions in their shadow) and softmax, a barrier behind each.  Half of the wavefronts run a phase
 // behind the others, so that a SIMD's matrix unit and its vector unit are both at work: 50 us at that size, against 54 in step with each other.  A
 // round takes 2400 cycles there, of which the matrix steps need 1030 and LDS reads, at 128 B a cycle, 1250; 13 us go by before the first round, after the last
-// one and in the merge.
+// one and in the merge.  No unit is full: by counters the matrix units work in 35 % of a CU's busy cycles, the vector units in 47, LDS in 46 (18 of them bank
+// conflicts).  The two phases and the barriers behind them keep the three from overlapping.
 constexpr int kTile16 = kKeyBlock * kHeadDim * 2;          // fp16 values of a K or V tile
 constexpr int kStep16 = 2 * kTile16;
 constexpr int kRowGroups = 4;
