@@ -378,7 +378,9 @@ size_t lm_head_sample_workspace_bytes(int M, int V);
  *   token int32 [M], prob fp32 [M]: out; all [M] arrays 4-byte aligned
  * Weights and sums are fp64 or exact whole numbers of 2^-44, so a token depends on nothing but its row; tokens more than e^31 below the row's
  * largest weigh nothing.  A logit of -inf or NaN is no token; +inf shares the row with its equals; a row with no token at all gives token
- * 0x7FFFFFFF and prob 0.  `workspace` holds lm_head_sample_workspace_bytes(M, V) bytes and has been initialised with w4a16_workspace_init. */
+ * 0x7FFFFFFF and prob 0.  A border of top_p or top_k among thousands of nearly equal weights, as for a top_p next to 1 over a large vocabulary, is
+ * searched by one workgroup per row: 0.6 to 2.3 ms where other calls take 10 to 90 us.
+ * `workspace` holds lm_head_sample_workspace_bytes(M, V) bytes and has been initialised with w4a16_workspace_init. */
 int lm_head_sample(const float *logits, int M, int V, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
                    const float *uniform, int32_t *token, float *prob, void *workspace, size_t workspace_bytes, void *stream);
 
