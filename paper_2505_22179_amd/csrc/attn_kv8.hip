@@ -31,8 +31,8 @@ __device__ __forceinline__ void wait_lds_reads(u32x2 &w)
     asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(w) : "n"(N));
 }
 
-// Clears the V codes, in LDS, of the keys of a step that no row of the tile sees.  Such rows of the cache may never have been written: a probability of
-// zero would not keep e4m3's NaN codes, or products beyond fp16, out of the rows' sums.
+// Clears the V codes, in LDS, of some keys of a step: those that no row of the tile sees (such rows of the cache may never have been written) and those that
+// keys_without_numbers finds.  A probability of zero would not keep e4m3's NaN codes, or products beyond fp16, out of the rows' sums.
 __device__ __forceinline__ void clear_codes(uint8_t *tile, uint32_t keys, int lane)
 {
 #pragma unroll
