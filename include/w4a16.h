@@ -325,6 +325,56 @@ int tree_verify_attn_kv8(const void *q, const void *k, const void *v, const void
 int tree_accept_kv8(const int32_t *parent, const int32_t *token, const int32_t *target, int M, int32_t *path, int32_t *result, void *k, void *v,
                     void *k_scale, void *v_scale, int P, int Hkv, int D, void *stream);
 
+/* Tables of the rotary embedding for positions first .. first + n_pos - 1, which rope_append, rope_append_qk_norm, rope_append_kv8, w4a16_gemm_rope,
+ * w4a16_decoder_layer and rope_prompt read, scaled for contexts longer than a model was trained on (paper section 2.1's targets, behind long prompts):
+ *   f_i = theta^(-2 i / R) for the pairs i < R / 2 (R: elements of a head that are turned);  n_i = original f_i / (2 pi): turns of pair i within the original context
+ *   W4A16_ROPE_PLAIN     f_i
+ *   W4A16_ROPE_LINEAR    f_i / factor
+ *   W4A16_ROPE_BY_TURNS  t f_i + (1 - t) f_i / factor,  t = (n_i - low) / (high - low) within [0, 1]
+ *   W4A16_ROPE_BY_INDEX  r f_i / factor + (1 - r) f_i,  r = (i - a) / (b - a) within [0, 1], where a and b are the (fractional) pair indices
+ *                        that turn `high` and `low` times within the original context, a rounded down and at least 0, b rounded up and at most R - 1 (b - a at least 0.001)
+ *   cos_table, sin_table  fp32 [n_pos, R / 2], 16-byte aligned, out: entry [p, i] = amplitude * cos / sin((first + p) f_i)
+ * Evaluated in fp64 and rounded once.  theta > 1; factor > 0 unless W4A16_ROPE_PLAIN; 0 < low < high and original > 0 for the last two (other
+ * kinds ignore what they do not use).  R even, R <= 1024, first + n_pos <= 2^28. */
+#define W4A16_ROPE_PLAIN 0
+#define W4A16_ROPE_LINEAR 1
+#define W4A16_ROPE_BY_TURNS 2
+#define W4A16_ROPE_BY_INDEX 3
+int rope_table(float *cos_table, float *sin_table, int first, int n_pos, int R, double theta, int scaling, double factor, double low, double high,
+               double original, double amplitude, void *stream);
+
+/* rope_append for the packed tokens of one or more prompts (or of a batch's decode steps), whose cache rows need not lie together:
+ *   qkv, pos, tables, q    as for rope_append, with `rows` tokens; tables fp32 [n_pos, R / 2], 16-byte aligned
+ *   R, interleaved         the first R elements of every query and key head are turned, the others copied; pairs are (i, i + R / 2), or (2 i, 2 i + 1) with
+ *                          `interleaved` 1
+ *   slot                   int32 [rows], 4-byte aligned: the cache row that receives the token's keys and values; outside [0, cache_rows) (a padding
+ *                          token): none, q is written all the same.  No two tokens may have the same.  NULL: token r has row r
+ *   k_cache, v_cache       fp16 [cache_rows, Hkv, D]; rows that no slot names are left untouched
+ * The turned values are rope_append's, bit for bit.  A row whose position lies outside [0, n_pos) gets its values stored but its q and k rows
+ * are left untouched.  D % 8 == 0, D <= 512, R even, R <= D, rows <= 2^23. */
+int rope_prompt(const void *qkv, const int32_t *pos, const float *cos_table, const float *sin_table, int n_pos, int R, int interleaved,
+                const int32_t *slot, int cache_rows, void *q, void *k_cache, void *v_cache, int rows, int Hq, int Hkv, int D, void *stream);
+
+/* Scratch of w4a16_prompt_attn for these sizes (partial results where the keys of a row are cut into ranges). */
+size_t w4a16_prompt_attn_workspace_bytes(int rows, int B, int max_q, int max_k, int Hq, int Hkv, int D);
+
+/* Causal attention of B packed sequences of different lengths over their keys in a cache: whole prompts, pieces of long ones behind what the
+ * cache holds, single tokens of a batch, or all of these in one call.  Sequence b has the query rows q_start[b] .. q_start[b + 1] - 1 and the cache rows
+ * k_start[b] .. k_start[b] + k_len[b] - 1; its queries are the last of its keys: query i of n sees keys 0 .. k_len - n + i,
+ *   out[i, h, :] = sum_j softmax_j(scale * q[i, h, :] . k[j, h / (Hq / Hkv), :]) * v[j, h / (Hq / Hkv), :]
+ *   q, out    fp16 [rows, Hq, D];  rows that no sequence names are left untouched
+ *   k, v      fp16 [k_rows, Hkv, D]; rows that a sequence does not see may hold anything
+ *   q_start   int32 [B + 1], ascending;  k_start, k_len int32 [B], both or neither: without them the keys lie as the queries do
+ *             (on the device, 4-byte aligned; a sequence whose rows do not lie in [0, rows) and [0, k_rows) is left out)
+ *   max_q, max_k   most queries and keys of a sequence, by which work is divided: results do not depend on their being right,
+ *                  their roundings do
+ * A row that sees no key (more queries than keys) gets zeros.  Softmax and sums in fp32; probabilities are rounded to fp16 for the product with the values.
+ * A row whose visible scores are all -inf, or among them a NaN or +inf, is NaN; one that sees a value that is not finite is not finite there.  D 64 or 128,
+ * Hq % Hkv == 0, Hq / Hkv <= 64, Hkv <= 1024, B <= 4096, rows <= 2^23, rows * Hq <= 2^29, a finite scale > 0.  `workspace` as for tree_verify_attn. */
+int w4a16_prompt_attn(const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start, const int32_t *k_len, void *out, int B,
+                      int rows, int k_rows, int max_q, int max_k, int Hq, int Hkv, int D, float scale, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
 /* Size in bytes of the packed LM-head weight for a V-token vocabulary and hidden size K (the
  * vocabulary is padded to a multiple of 16 inside the buffer).  0 if the shape is not supported. */
 size_t lm_head_packed_bytes(int V, int K);

@@ -454,3 +454,120 @@ def sample(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, u=0.0):
         margin = min(margin, abs(upto / total - u)) if v != order[-1] else margin
         if upto > u * total or v == order[-1]:
             return v, w[v] / total, margin
+
+
+# ---------------------------------------------------------------------------------------------
+# prompts: rotary tables for long contexts, rotation with scatter, W8A8 linears, causal attention of packed sequences
+
+
+def rope_frequencies(R, theta, scaling=0, factor=1.0, low=0.0, high=0.0, original=0.0):
+    """float64 [R / 2], by the formulas in include/w4a16.h"""
+    out = []
+    for i in range(R // 2):
+        f = float(theta) ** (-2.0 * i / R)
+        if scaling == 1:
+            f /= factor
+        elif scaling == 2:
+            t = min(max((original * f / (2 * math.pi) - low) / (high - low), 0.0), 1.0)
+            f = t * f + (1 - t) * f / factor
+        elif scaling == 3:
+            index = lambda turns: R * math.log(original / (turns * 2 * math.pi)) / (2 * math.log(theta))
+            a, b = max(float(math.floor(index(high))), 0.0), min(float(math.ceil(index(low))), R - 1.0)
+            r = min(max((i - a) / max(b - a, 0.001), 0.0), 1.0)
+            f = r * f / factor + (1 - r) * f
+        out.append(f)
+    return np.array(out)
+
+
+def rope_table(first, n_pos, R, theta, scaling=0, factor=1.0, low=0.0, high=0.0, original=0.0, amplitude=1.0):
+    """(cos, sin) float64 [n_pos, R / 2]"""
+    ang = np.arange(first, first + n_pos, dtype=np.float64)[:, None] * rope_frequencies(R, theta, scaling, factor, low, high, original)
+    return amplitude * np.cos(ang), amplitude * np.sin(ang)
+
+
+def rope_prompt(qkv, pos, cos, sin, R, interleaved, slot, q, k_cache, v_cache):
+    """(q, k_cache, v_cache) float64, exact: copies of the given ones with what rope_prompt writes"""
+    q, k_cache, v_cache = (np.asarray(t, dtype=np.float64).copy() for t in (q, k_cache, v_cache))
+    rows, Hq, D = q.shape
+    Hkv = k_cache.shape[1]
+    x = np.asarray(qkv, dtype=np.float64).reshape(rows, Hq + 2 * Hkv, D)
+    for m in range(rows):
+        to = m if slot is None else int(slot[m])
+        stored = 0 <= to < k_cache.shape[0]
+        if stored:
+            v_cache[to] = x[m, Hq + Hkv:]
+        if not 0 <= pos[m] < cos.shape[0]:
+            continue
+        y = x[m, :Hq + Hkv].copy()
+        for i in range(R // 2):
+            a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + R // 2)
+            c, s = float(cos[pos[m], i]), float(sin[pos[m], i])
+            y[:, a], y[:, b] = x[m, :Hq + Hkv, a] * c - x[m, :Hq + Hkv, b] * s, x[m, :Hq + Hkv, b] * c + x[m, :Hq + Hkv, a] * s
+        q[m] = y[:Hq]
+        if stored:
+            k_cache[to] = y[Hq:]
+    return q, k_cache, v_cache
+
+
+def w8a8_input(x, pre, gamma=None, eps=0.0):
+    """float64: what a W8A8 linear quantises, before its rounding to fp16"""
+    x = np.asarray(x, dtype=np.float64)
+    with np.errstate(over="ignore", invalid="ignore"):
+        if pre == 1:
+            return x * np.asarray(gamma, dtype=np.float64) / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+        if pre == 2:
+            gate, up = np.split(x, 2, axis=-1)
+            return gate / (1 + np.exp(-gate)) * up
+    return x
+
+
+def w8a8_quantise(x16):
+    """(codes int8, scales float32) of fp16 rows; the quotient is rounded exactly (ties to even): x / s in float64 cannot come as near to a half
+    that it is not without being one (x has 11 bits, s 24, the code 8)"""
+    x = np.asarray(x16, dtype=np.float64)
+    top = np.abs(x).max(-1)
+    fine = np.isfinite(x).all(-1)
+    scale = np.where(fine, np.float32(np.where(fine, top, 0.0) / 127), np.float32(np.nan)).astype(np.float32)
+    s = np.where(fine & (top > 0), scale, 1).astype(np.float64)[..., None]
+    codes = np.rint(np.where((fine & (top > 0))[..., None], x, 0.0) / s).astype(np.int8)
+    return codes, scale
+
+
+def w8a8_gemm(codes, scale, w, w_scale, residual=None):
+    """float64 [M, N], exact but for float64's own roundings: integer sums"""
+    acc = np.asarray(codes, dtype=np.int64) @ np.asarray(w, dtype=np.int64).T
+    y = acc * np.asarray(scale, dtype=np.float64)[:, None] * np.asarray(w_scale, dtype=np.float64)
+    return y if residual is None else y + np.asarray(residual, dtype=np.float64)
+
+
+def w8a8_layout(codes, fill=0):
+    """codes [rows, K] in the layout of include/w8a8.h; rows of the padding hold `fill`"""
+    rows, K = codes.shape
+    R, KP = (rows + 15) // 16 * 16, (K + 127) // 128 * 128
+    full = np.zeros((R, KP), dtype=np.int8)
+    full[:rows, :K], full[rows:] = codes, fill
+    return np.ascontiguousarray(full.reshape(R // 16, 16, KP // 64, 4, 16).transpose(0, 2, 3, 1, 4)).reshape(-1)
+
+
+def prompt_attn(q, k, v, q_start, k_start, k_len, scale, out):
+    """(out, spread) float64: `out` with the rows of the sequences replaced; spread = sum_j p_j |v_j| of those rows"""
+    q, k, v = (np.asarray(t, dtype=np.float64) for t in (q, k, v))
+    out, spread = np.asarray(out, dtype=np.float64).copy(), np.zeros(q.shape)
+    group = q.shape[1] // k.shape[1]
+    for b in range(len(q_start) - 1):
+        q0, q1 = int(q_start[b]), int(q_start[b + 1])
+        k0, T = (q0, q1 - q0) if k_len is None else (int(k_start[b]), int(k_len[b]))
+        if q0 < 0 or q1 > q.shape[0] or k0 < 0 or T < 0 or k0 + T > k.shape[0]:
+            continue
+        for i in range(q0, q1):
+            seen = T - (q1 - q0) + (i - q0) + 1
+            out[i], spread[i] = 0.0, 0.0
+            if seen <= 0:
+                continue
+            with np.errstate(invalid="ignore"):
+                for h in range(q.shape[1]):
+                    a = scale * (k[k0:k0 + seen, h // group] @ q[i, h])
+                    p = np.exp(a - a.max())
+                    p /= p.sum()
+                    out[i, h], spread[i, h] = p @ v[k0:k0 + seen, h // group], p @ np.abs(v[k0:k0 + seen, h // group])
+    return out, spread

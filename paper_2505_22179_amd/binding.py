@@ -10,6 +10,7 @@ import os
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
+LIB_W8A8_PATH = os.environ.get("W8A8_LIB") or os.path.join(_HERE, "lib", "libw8a8.so")
 LIB_PATH = os.environ.get("W4A16_LIB") or os.path.join(_HERE, "lib", "libw4a16.so")   # W4A16_LIB: load another build of the same ABI
 
 EXPORTS = (
@@ -20,13 +21,18 @@ EXPORTS = (
     "lm_head_packed_bytes", "lm_head_pack", "w4a16_decoder_layer", "w4a16_plan_describe", "w4a16_gemm_static", "w4a16_weight_is_symmetric",
     "tree_verify_attn_plan_describe", "lm_head_plan_describe", "rope_append_qk_norm", "rope_append_kv8", "w4a16_kv8_read", "tree_accept_kv8",
     "tree_verify_attn_kv8", "tree_verify_attn_kv8_workspace_bytes", "tree_verify_attn_kv8_plan_describe", "lm_head_sample", "lm_head_sample_workspace_bytes",
+    "rope_table", "rope_prompt", "w4a16_prompt_attn", "w4a16_prompt_attn_workspace_bytes",
 )
+EXPORTS_W8A8 = ("w8a8_packed_bytes", "w8a8_pack", "w8a8_unpack", "w8a8_quantize", "w8a8_workspace_bytes", "w8a8_gemm", "w8a8_linear")   # of include/w8a8.h
 
 EPI_NONE, EPI_RESIDUAL, EPI_SILU_MUL = 0, 1, 2
 SYMMETRIC = 0x100   # OR-ed into an epilogue code: every zero-point of the weight is 8
 KV8_INT8, KV8_E4M3 = 1, 2   # formats of an 8-bit attention cache
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BY_TURNS, ROPE_BY_INDEX = 0, 1, 2, 3   # how rope_table stretches its frequencies
+W8A8_PLAIN, W8A8_RMS_NORM, W8A8_SILU_MUL = 0, 1, 2   # what becomes of a W8A8 linear's input before it is quantised
 
 _lib = None
+_lib_w8a8 = None
 
 
 class LayerWeights(ctypes.Structure):
@@ -108,7 +114,31 @@ def load() -> ctypes.CDLL:
     L.lm_head_sample_workspace_bytes.argtypes = [i, i]
     L.lm_head_sample.argtypes = [vp, i, i, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.lm_head_topk.argtypes = [vp, vp, i, i, i, i, vp, vp, vp, vp, sz, vp]
+    L.rope_table.argtypes = [vp, vp, i, i, i] + [ctypes.c_double, i] + [ctypes.c_double] * 5 + [vp]
+    L.rope_prompt.argtypes = [vp, vp, vp, vp, i, i, i, vp, i, vp, vp, vp, i, i, i, i, vp]
+    L.w4a16_prompt_attn_workspace_bytes.restype = sz
+    L.w4a16_prompt_attn_workspace_bytes.argtypes = [i] * 7
+    L.w4a16_prompt_attn.argtypes = [vp] * 7 + [i] * 8 + [ctypes.c_float, vp, sz, vp]
     _lib = L
+    return L
+
+
+def load_w8a8() -> ctypes.CDLL:
+    global _lib_w8a8
+    if _lib_w8a8 is not None:
+        return _lib_w8a8
+    if not os.path.exists(LIB_W8A8_PATH):
+        raise ImportError(f"{LIB_W8A8_PATH} is missing: build it with `python -m paper_2505_22179_amd.build`")
+    L = ctypes.CDLL(LIB_W8A8_PATH)
+    vp, i, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+    L.w8a8_packed_bytes.restype = L.w8a8_workspace_bytes.restype = sz
+    L.w8a8_packed_bytes.argtypes = [i, i]
+    L.w8a8_workspace_bytes.argtypes = [i, i, i]
+    L.w8a8_pack.argtypes = L.w8a8_unpack.argtypes = [vp, vp, i, i, vp]
+    L.w8a8_quantize.argtypes = [vp, i, vp, ctypes.c_float, vp, vp, i, i, vp]
+    L.w8a8_gemm.argtypes = [vp] * 6 + [i, i, i, vp, sz, vp]
+    L.w8a8_linear.argtypes = [vp, i, vp, ctypes.c_float, vp, vp, vp, vp, i, i, i, vp, sz, vp]
+    _lib_w8a8 = L
     return L
 
 
@@ -411,6 +441,77 @@ def tree_verify_attn_kv8_plan_describe(M: int, P: int, Hq: int, Hkv: int, D: int
 def tree_accept_kv8(parent, token, target, M: int, path, result, k, v, k_scale, v_scale, P: int, Hkv: int, D: int) -> None:
     _check(load().tree_accept_kv8(_ptr(parent), _ptr(token), _ptr(target), M, _ptr(path), _ptr(result), _ptr(k), _ptr(v), _ptr(k_scale),
                                   _ptr(v_scale), P, Hkv, D, _stream()), "tree_accept_kv8")
+
+
+def rope_table(cos_table, sin_table, first: int, n_pos: int, R: int, theta: float, scaling: int = ROPE_PLAIN, factor: float = 1.0, low: float = 0.0,
+               high: float = 0.0, original: float = 0.0, amplitude: float = 1.0) -> None:
+    _check(load().rope_table(_ptr(cos_table), _ptr(sin_table), first, n_pos, R, theta, scaling, factor, low, high, original, amplitude, _stream()),
+           "rope_table")
+
+
+def rope_prompt(qkv, pos, cos_table, sin_table, n_pos: int, R: int, interleaved: bool, slot, cache_rows: int, q, k_cache, v_cache, rows: int, Hq: int,
+                Hkv: int, D: int) -> None:
+    _init_cuda()
+    rc = (_lib or load()).rope_prompt(
+        0 if qkv is None else qkv.data_ptr(), 0 if pos is None else pos.data_ptr(), 0 if cos_table is None else cos_table.data_ptr(),
+        0 if sin_table is None else sin_table.data_ptr(), n_pos, R, int(interleaved), 0 if slot is None else slot.data_ptr(), cache_rows,
+        0 if q is None else q.data_ptr(), 0 if k_cache is None else k_cache.data_ptr(), 0 if v_cache is None else v_cache.data_ptr(), rows, Hq, Hkv, D,
+        _raw_stream(_current_device()))
+    if rc:
+        _check(rc, "rope_prompt")
+
+
+def w4a16_prompt_attn_workspace_bytes(rows: int, B: int, max_q: int, max_k: int, Hq: int, Hkv: int, D: int) -> int:
+    return load().w4a16_prompt_attn_workspace_bytes(rows, B, max_q, max_k, Hq, Hkv, D)
+
+
+def w4a16_prompt_attn(q, k, v, q_start, k_start, k_len, out, B: int, rows: int, k_rows: int, max_q: int, max_k: int, Hq: int, Hkv: int, D: int,
+                      scale: float, workspace) -> None:
+    _init_cuda()
+    rc = (_lib or load()).w4a16_prompt_attn(
+        0 if q is None else q.data_ptr(), 0 if k is None else k.data_ptr(), 0 if v is None else v.data_ptr(), 0 if q_start is None else q_start.data_ptr(),
+        0 if k_start is None else k_start.data_ptr(), 0 if k_len is None else k_len.data_ptr(), 0 if out is None else out.data_ptr(), B, rows, k_rows,
+        max_q, max_k, Hq, Hkv, D, float(scale), 0 if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _raw_stream(_current_device()))
+    if rc:
+        _check(rc, "w4a16_prompt_attn")
+
+
+def w8a8_packed_bytes(rows: int, K: int) -> int:
+    return load_w8a8().w8a8_packed_bytes(rows, K)
+
+
+def w8a8_workspace_bytes(M: int, N: int, K: int) -> int:
+    return load_w8a8().w8a8_workspace_bytes(M, N, K)
+
+
+def w8a8_pack(w, packed, rows: int, K: int) -> None:
+    _check(load_w8a8().w8a8_pack(_ptr(w), _ptr(packed), rows, K, _stream()), "w8a8_pack")
+
+
+def w8a8_unpack(packed, w, rows: int, K: int) -> None:
+    _check(load_w8a8().w8a8_unpack(_ptr(packed), _ptr(w), rows, K, _stream()), "w8a8_unpack")
+
+
+def w8a8_quantize(x, pre: int, gamma, eps: float, codes, scale, M: int, K: int) -> None:
+    _check(load_w8a8().w8a8_quantize(_ptr(x), pre, _ptr(gamma), eps, _ptr(codes), _ptr(scale), M, K, _stream()), "w8a8_quantize")
+
+
+def w8a8_gemm(codes, scale, packed, w_scale, residual, y, M: int, N: int, K: int, workspace) -> None:
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load_w8a8().w8a8_gemm(_ptr(codes), _ptr(scale), _ptr(packed), _ptr(w_scale), _ptr(residual), _ptr(y), M, N, K, _ptr(workspace), nbytes,
+                                 _stream()), "w8a8_gemm")
+
+
+def w8a8_linear(x, pre: int, gamma, eps: float, packed, w_scale, residual, y, M: int, N: int, K: int, workspace) -> None:
+    _init_cuda()
+    rc = (_lib_w8a8 or load_w8a8()).w8a8_linear(
+        0 if x is None else x.data_ptr(), pre, 0 if gamma is None else gamma.data_ptr(), eps, 0 if packed is None else packed.data_ptr(),
+        0 if w_scale is None else w_scale.data_ptr(), 0 if residual is None else residual.data_ptr(), 0 if y is None else y.data_ptr(), M, N, K,
+        0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _raw_stream(_current_device()))
+    if rc:
+        _check(rc, "w8a8_linear")
 
 
 # ---- conveniences for tests and the benchmark (still marshalling only) ----

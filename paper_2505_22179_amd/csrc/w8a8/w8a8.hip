@@ -1,0 +1,453 @@
+// W8A8 linear: quantisation of tokens, the product of int8 codes, packing.  Contracts in include/w8a8.h.
+#include "../internal.h"
+#include "../devscope.h"
+#include "../../../include/w8a8.h"
+
+namespace w4 {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef int int4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMostK = 65536;       // 65536 * 128 * 127 < 2^31: no sum of products leaves 32 bits
+constexpr int kMostTokens = 1 << 20;
+__host__ __device__ inline int k_blocks(int K) { return (K + 127) / 128 * 2; }   // tiles of a row of tiles
+// byte of codes (r, 16 chunk .. 16 chunk + 15)
+__host__ __device__ inline size_t chunk_offset(int r, int chunk, int blocks)
+{
+    return ((size_t)(r >> 4) * blocks + (chunk >> 2)) * 1024 + (chunk & 3) * 256 + (r & 15) * 16;
+}
+
+// ---- packing -----------------------------------------------------------------------------------------------
+// A thread moves 16 codes of a row; the sixteen rows of a tile lie in neighbouring threads, so the packed side is contiguous.
+__global__ __launch_bounds__(256) void w8a8_pack_kernel(const int8_t *__restrict__ w, uint8_t *__restrict__ packed, int rows, int K, int blocks)
+{
+    const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;   // 16-byte place in the packed buffer
+    const size_t tile = at >> 6;
+    const int r = (int)(tile / blocks) * 16 + (int)(at & 15), chunk = (int)(tile % blocks) * 4 + (int)((at >> 4) & 3);
+    if (r >= (rows + 15) / 16 * 16) return;
+    u32x4 x = {};
+    if (r < rows && chunk * 16 < K) x = *reinterpret_cast<const u32x4 *>(w + (size_t)r * K + chunk * 16);
+    *reinterpret_cast<u32x4 *>(packed + at * 16) = x;
+}
+__global__ __launch_bounds__(256) void w8a8_unpack_kernel(const uint8_t *__restrict__ packed, int8_t *__restrict__ w, int rows, int K, int blocks)
+{
+    const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const int chunks = K / 16, r = (int)(at / chunks), chunk = (int)(at % chunks);
+    if (r >= rows) return;
+    *reinterpret_cast<u32x4 *>(w + (size_t)r * K + chunk * 16) = *reinterpret_cast<const u32x4 *>(packed + chunk_offset(r, chunk, blocks));
+}
+
+// ---- quantisation --------------------------------------------------------------------------------------------
+// Nearest whole number to x / s, ties to even.  The product with the reciprocal is off by a rounding or two, so the number found may be a neighbour
+// where the quotient lies next to a half: what is left, x - n s, is exact in fp32 (a multiple of the last place of s or of x, no larger than s),
+// and tells.
+__device__ __forceinline__ int nearest_code(float x, float s, float inv)
+{
+    float n = __builtin_rintf(x * inv);
+    const float left = __builtin_fmaf(-n, s, x), half = 0.5f * s;
+    const float over = __builtin_fabsf(left);
+    if (over > half || (over == half && ((int)n & 1))) n += left > 0.f ? 1.f : -1.f;
+    return (int)n;
+}
+
+// One workgroup of T threads per token; a thread keeps PER chunks of sixteen values in registers: one pass over the input.
+template <int PRE, int T, int PER>
+__global__ __launch_bounds__(T) void w8a8_quantize_kernel(const _Float16 *__restrict__ x, const _Float16 *__restrict__ gamma, float eps,
+                                                          uint8_t *__restrict__ codes, float *__restrict__ scale, int K, int blocks)
+{
+    __shared__ float sums[T / 64];
+    __shared__ uint32_t tops[T / 64];
+    const int m = blockIdx.x, chunks = K / 16;
+    const _Float16 *const row = x + (size_t)m * K * (PRE == W8A8_SILU_MUL ? 2 : 1);
+    half8 v[PER][2];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int ch = threadIdx.x + i * T;
+        v[i][0] = v[i][1] = (half8)(_Float16)0;
+        if (ch < chunks) {
+            v[i][0] = *reinterpret_cast<const half8 *>(row + ch * 16);
+            v[i][1] = *reinterpret_cast<const half8 *>(row + ch * 16 + 8);
+        }
+    }
+    if constexpr (PRE == W8A8_SILU_MUL) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int ch = threadIdx.x + i * T;
+            if (ch < chunks) {
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const half8 up = *reinterpret_cast<const half8 *>(row + K + ch * 16 + 8 * p);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float g = (float)v[i][p][e];
+                        v[i][p][e] = (_Float16)keep_f32(g / (1.f + __expf(-g)) * (float)up[e]);
+                    }
+                }
+            }
+        }
+    } else if constexpr (PRE == W8A8_RMS_NORM) {
+        float ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss = __builtin_fmaf((float)v[i][p][e], (float)v[i][p][e], ss);
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) ss += __shfl_xor(ss, off, 64);
+        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = ss;
+        __syncthreads();
+        ss = 0.f;
+#pragma unroll
+        for (int w = 0; w < T / 64; ++w) ss += sums[w];
+        const float inv = 1.f / sqrtf(ss / (float)K + eps);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int ch = threadIdx.x + i * T;
+            if (ch < chunks) {
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const half8 g = *reinterpret_cast<const half8 *>(gamma + ch * 16 + 8 * p);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[i][p][e] = (_Float16)keep_f32((float)v[i][p][e] * inv * (float)g[e]);
+                }
+            }
+        }
+    }
+    // magnitudes of fp16 numbers compare as their bits do, infinities and NaN above all others
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const u32x4 b = __builtin_bit_cast(u32x4, v[i][p]) & 0x7FFF7FFFu;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = max(top, max(b[e] & 0xFFFFu, b[e] >> 16));
+        }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, 64));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = 0;
+#pragma unroll
+    for (int w = 0; w < T / 64; ++w) top = max(top, tops[w]);
+    const bool finite = top < 0x7C00u, some = finite && top > 0;
+    const float s = (float)__builtin_bit_cast(_Float16, (uint16_t)top) / 127.f;   // 0 for a row of zeros
+    const float inv = some ? 1.f / s : 0.f;
+    if (threadIdx.x == 0) scale[m] = finite ? s : __builtin_nanf("");
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int ch = threadIdx.x + i * T;
+        if (ch < blocks * 4) {   // chunks of the padding hold zeros
+            u32x4 packed = {};
+            if (some) {
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) packed[2 * p + (e >> 2)] |= (uint32_t)(nearest_code((float)v[i][p][e], s, inv) & 0xFF) << (8 * (e & 3));
+            }
+            *reinterpret_cast<u32x4 *>(codes + chunk_offset(m, ch, blocks)) = packed;
+        }
+    }
+}
+
+// ---- products ------------------------------------------------------------------------------------------------
+struct GemmArgs {
+    const uint8_t *codes, *packed;
+    const float *scale, *w_scale;
+    const _Float16 *residual;
+    _Float16 *y;
+    int M, N, blocks;
+};
+
+// sums of channels n .. n + 3 of token m become outputs
+__device__ __forceinline__ void finish(const GemmArgs &a, int4v acc, int m, int n)
+{
+    if (m >= a.M || n >= a.N) return;   // N is a multiple of eight: four channels are all there or none
+    const float s = a.scale[m];
+    const float4v t = *reinterpret_cast<const float4v *>(a.w_scale + n);
+    const size_t at = (size_t)m * a.N + n;
+    half4 r = {}, y;
+    if (a.residual) r = *reinterpret_cast<const half4 *>(a.residual + at);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (_Float16)((float)acc[e] * s * t[e] + (float)r[e]);
+    *reinterpret_cast<half4 *>(a.y + at) = y;
+}
+
+// Many tokens: a workgroup of WM x WN wavefronts takes 16 MT WM tokens by 16 NT WN channels, both operands through LDS in steps of 128 values
+// of k, two buffers.  Tiles lie in operand order already, so a transfer is 1 KB in one piece and fragments are read without bank conflicts.
+template <int WM, int WN, int MT, int NT>
+__global__ __launch_bounds__(64 * WM * WN) void w8a8_tile_kernel(GemmArgs a)
+{
+    constexpr int XT = WM * MT, WT = WN * NT, WAVES = WM * WN, STAGE = (XT + WT) * 2048, TRANSFERS = (XT + WT) * 2 / WAVES;
+    static_assert((XT + WT) * 2 % WAVES == 0, "");
+    extern __shared__ u32x4 smem[];
+    uint8_t *const lds = reinterpret_cast<uint8_t *>(smem);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const int x_tiles = (a.M + 15) / 16, w_tiles = (a.N + 15) / 16;
+    const int col_blocks = (w_tiles + WT - 1) / WT;
+    const int bm = blockIdx.x / col_blocks, bn = blockIdx.x % col_blocks;
+    auto request = [&](int step, uint8_t *stage) {
+#pragma unroll
+        for (int i = 0; i < TRANSFERS; ++i) {
+            const int t = wave * TRANSFERS + i, tile = t >> 1, half = t & 1;   // uniform
+            const uint8_t *src = tile < XT ? a.codes + (size_t)min(bm * XT + tile, x_tiles - 1) * a.blocks * 1024
+                                           : a.packed + (size_t)min(bn * WT + tile - XT, w_tiles - 1) * a.blocks * 1024;
+            quad_to_lds(stretch(src, 0x7FFFFFFF), stage + t * 1024, lane * 16, (2 * step + half) * 1024);
+        }
+    };
+    int4v acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
+    const int steps = a.blocks / 2;
+    request(0, lds);
+    for (int step = 0; step < steps; ++step) {
+        const uint8_t *const stage = lds + (step & 1) * STAGE;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this step has landed, the other buffer has been read
+        if (step + 1 < steps) request(step + 1, lds + ((step + 1) & 1) * STAGE);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            int4v xf[MT], wf[NT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) xf[i] = *reinterpret_cast<const int4v *>(stage + ((wm * MT + i) * 2 + half) * 1024 + lane * 16);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) wf[j] = *reinterpret_cast<const int4v *>(stage + ((XT + wn * NT + j) * 2 + half) * 1024 + lane * 16);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[j], xf[i], acc[i][j], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            finish(a, acc[i][j], (bm * XT + wm * MT + i) * 16 + (lane & 15), (bn * WT + wn * NT + j) * 16 + 4 * (lane >> 4));
+}
+
+// Few tokens, bound by the weights: eight wavefronts share TW tiles of channels and take every eighth tile of k; weights go straight to registers.
+template <int MT, int TW>
+__global__ __launch_bounds__(512) void w8a8_stream_kernel(GemmArgs a)
+{
+    constexpr int AHEAD = 4;
+    __shared__ int4v sums[8][MT * TW][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int x_tiles = (a.M + 15) / 16, w_tiles = (a.N + 15) / 16, tile0 = blockIdx.x * TW;
+    int4v acc[MT][TW];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < TW; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
+    const uint8_t *xs[MT], *ws[TW];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xs[i] = a.codes + (size_t)min(i, x_tiles - 1) * a.blocks * 1024 + lane * 16;
+#pragma unroll
+    for (int j = 0; j < TW; ++j) ws[j] = a.packed + (size_t)min(tile0 + j, w_tiles - 1) * a.blocks * 1024 + lane * 16;
+    for (int b = wave; b < a.blocks; b += 8 * AHEAD) {
+        int4v xf[AHEAD][MT], wf[AHEAD][TW];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const size_t at = (size_t)min(b + 8 * u, a.blocks - 1) * 1024;
+#pragma unroll
+            for (int j = 0; j < TW; ++j) wf[u][j] = __builtin_nontemporal_load(reinterpret_cast<const int4v *>(ws[j] + at));
+#pragma unroll
+            for (int i = 0; i < MT; ++i) xf[u][i] = *reinterpret_cast<const int4v *>(xs[i] + at);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (b + 8 * u < a.blocks) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < TW; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[u][j], xf[u][i], acc[i][j], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < TW; ++j) sums[wave][i * TW + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int t = wave; t < MT * TW; t += 8) {
+        int4v all = sums[0][t][lane];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) all += sums[w][t][lane];
+        finish(a, all, t / TW * 16 + (lane & 15), (tile0 + t % TW) * 16 + 4 * (lane >> 4));
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------
+static int check_codes_shape(int rows, int K)
+{
+    if (rows < 1 || K < 1 || K % 16 != 0) return W4A16_EINVAL;
+    if (K > kMostK || rows > (1 << 24)) return W4A16_EUNSUP;
+    return W4A16_OK;
+}
+static size_t codes_bytes(int rows, int K) { return (size_t)((rows + 15) / 16) * k_blocks(K) * 1024; }
+static int check_gemm_shape(int M, int N, int K)
+{
+    if (M < 1 || N < 1 || K < 1 || K % 16 != 0 || N % 8 != 0) return W4A16_EINVAL;
+    if (K > kMostK || N > (1 << 20) || M > kMostTokens) return W4A16_EUNSUP;
+    return W4A16_OK;
+}
+static size_t aligned256(size_t n) { return (n + 255) / 256 * 256; }
+
+static int check_quantize(const void *x, int pre, const void *gamma, float eps, int K)
+{
+    if (pre < W8A8_PLAIN || pre > W8A8_SILU_MUL) return W4A16_EINVAL;
+    if (!x) return W4A16_ENULL;
+    if (pre == W8A8_RMS_NORM) {
+        if (!gamma) return W4A16_ENULL;
+        if (!(eps >= 0.f)) return W4A16_EINVAL;
+    } else if (gamma) return W4A16_EINVAL;
+    if (misaligned(x) || misaligned(gamma)) return W4A16_EALIGN;
+    return W4A16_OK;
+}
+
+static int launch_quantize(const void *x, int pre, const void *gamma, float eps, void *codes, float *scale, int M, int K, hipStream_t stream)
+{
+    const int blocks = k_blocks(K), chunks = blocks * 4;
+#define W8_QUANTIZE(P_, T_, N_)                                                                                                                 \
+    hipLaunchKernelGGL((w8a8_quantize_kernel<P_, T_, N_>), dim3((unsigned)M), dim3(T_), 0, stream, (const _Float16 *)x, (const _Float16 *)gamma, eps, \
+                       (uint8_t *)codes, scale, K, blocks)
+#define W8_QUANTIZE_PRE(P_)                              \
+    do {                                                 \
+        if (chunks <= 256) W8_QUANTIZE(P_, 256, 1);      \
+        else if (chunks <= 512) W8_QUANTIZE(P_, 256, 2); \
+        else if (chunks <= 1024) W8_QUANTIZE(P_, 256, 4);\
+        else if (chunks <= 2048) W8_QUANTIZE(P_, 1024, 2); \
+        else W8_QUANTIZE(P_, 1024, 4);                   \
+    } while (0)
+    if (pre == W8A8_PLAIN) W8_QUANTIZE_PRE(W8A8_PLAIN);
+    else if (pre == W8A8_RMS_NORM) W8_QUANTIZE_PRE(W8A8_RMS_NORM);
+    else W8_QUANTIZE_PRE(W8A8_SILU_MUL);
+#undef W8_QUANTIZE_PRE
+#undef W8_QUANTIZE
+    return launch_status();
+}
+
+template <int WM, int WN, int MT, int NT>
+static int launch_tile(const GemmArgs &a, hipStream_t stream)
+{
+    constexpr int lds = (WM * MT + WN * NT) * 4096;
+    static bool ready = false;   // the LDS size is granted once
+    if (!ready) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(&w8a8_tile_kernel<WM, WN, MT, NT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+            return W4A16_EHIP;
+        ready = true;
+    }
+    const unsigned rows = (unsigned)((a.M + 16 * MT * WM - 1) / (16 * MT * WM)), cols = (unsigned)((a.N + 16 * NT * WN - 1) / (16 * NT * WN));
+    if ((unsigned long long)rows * cols > (1u << 22)) return W4A16_EUNSUP;
+    hipLaunchKernelGGL((w8a8_tile_kernel<WM, WN, MT, NT>), dim3(rows * cols), dim3(64 * WM * WN), lds, stream, a);
+    return launch_status();
+}
+
+static int launch_gemm(const GemmArgs &a, hipStream_t stream)
+{
+    const unsigned tiles = (unsigned)(a.N + 15) / 16;
+    if (a.M <= 16) hipLaunchKernelGGL((w8a8_stream_kernel<1, 1>), dim3(tiles), dim3(512), 0, stream, a);
+    else if (a.M <= 32) hipLaunchKernelGGL((w8a8_stream_kernel<2, 1>), dim3(tiles), dim3(512), 0, stream, a);
+    else if (a.M <= 64) hipLaunchKernelGGL((w8a8_stream_kernel<4, 1>), dim3(tiles), dim3(512), 0, stream, a);
+    else if ((long long)((a.M + 255) / 256) * ((a.N + 255) / 256) >= 256) return launch_tile<2, 4, 8, 4>(a, stream);
+    else return launch_tile<2, 2, 4, 4>(a, stream);
+    return launch_status();
+}
+
+static int check_gemm(const void *packed, const float *w_scale, const void *residual, const void *y)
+{
+    if (!packed || !w_scale || !y) return W4A16_ENULL;
+    if (misaligned(packed) || misaligned(w_scale) || misaligned(residual) || misaligned(y)) return W4A16_EALIGN;
+    return W4A16_OK;
+}
+
+}  // namespace w4
+
+using namespace w4;
+
+extern "C" {
+
+size_t w8a8_packed_bytes(int rows, int K) { return check_codes_shape(rows, K) == W4A16_OK ? codes_bytes(rows, K) : 0; }
+
+int w8a8_pack(const int8_t *w, void *packed, int rows, int K, void *stream)
+{
+    const int rc = check_codes_shape(rows, K);
+    if (rc != W4A16_OK) return rc;
+    if (!w || !packed) return W4A16_ENULL;
+    if (misaligned(w) || misaligned(packed)) return W4A16_EALIGN;
+    const size_t groups = (codes_bytes(rows, K) / 16 + 255) / 256;
+    if (groups >= (1u << 24)) return W4A16_EUNSUP;
+    hipLaunchKernelGGL(w8a8_pack_kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)stream, w, (uint8_t *)packed, rows, K, k_blocks(K));
+    return launch_status();
+}
+
+int w8a8_unpack(const void *packed, int8_t *w, int rows, int K, void *stream)
+{
+    const int rc = check_codes_shape(rows, K);
+    if (rc != W4A16_OK) return rc;
+    if (!w || !packed) return W4A16_ENULL;
+    if (misaligned(w) || misaligned(packed)) return W4A16_EALIGN;
+    const size_t groups = ((size_t)rows * (K / 16) + 255) / 256;
+    if (groups >= (1u << 24)) return W4A16_EUNSUP;
+    hipLaunchKernelGGL(w8a8_unpack_kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)stream, (const uint8_t *)packed, w, rows, K, k_blocks(K));
+    return launch_status();
+}
+
+int w8a8_quantize(const void *x, int pre, const void *gamma, float eps, void *codes, float *scale, int M, int K, void *stream)
+{
+    int rc = check_codes_shape(M, K);
+    if (rc != W4A16_OK) return rc;
+    if (M > kMostTokens) return W4A16_EUNSUP;
+    if (!codes || !scale) return W4A16_ENULL;
+    rc = check_quantize(x, pre, gamma, eps, K);
+    if (rc != W4A16_OK) return rc;
+    if (misaligned(codes) || misaligned(scale)) return W4A16_EALIGN;
+    return launch_quantize(x, pre, gamma, eps, codes, scale, M, K, (hipStream_t)stream);
+}
+
+size_t w8a8_workspace_bytes(int M, int N, int K)
+{
+    if (check_gemm_shape(M, N, K) != W4A16_OK) return 0;
+    return kTicketBytes + codes_bytes(M, K) + aligned256((size_t)M * 4);
+}
+
+int w8a8_gemm(const void *codes, const float *scale, const void *packed, const float *w_scale, const void *residual, void *y, int M, int N, int K,
+              void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_gemm_shape(M, N, K);
+    if (rc != W4A16_OK) return rc;
+    if (!codes || !scale) return W4A16_ENULL;
+    rc = check_gemm(packed, w_scale, residual, y);
+    if (rc != W4A16_OK) return rc;
+    if (misaligned(codes) || misaligned(scale)) return W4A16_EALIGN;
+    if (!workspace || workspace_bytes < w8a8_workspace_bytes(M, N, K)) return W4A16_EWORKSPACE;
+    if (workspace_misaligned(workspace)) return W4A16_EALIGN;
+    const GemmArgs a = {(const uint8_t *)codes, (const uint8_t *)packed, scale, w_scale, (const _Float16 *)residual, (_Float16 *)y, M, N, k_blocks(K)};
+    return launch_gemm(a, (hipStream_t)stream);
+}
+
+int w8a8_linear(const void *x, int pre, const void *gamma, float eps, const void *packed, const float *w_scale, const void *residual, void *y, int M,
+                int N, int K, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_gemm_shape(M, N, K);
+    if (rc != W4A16_OK) return rc;
+    rc = check_quantize(x, pre, gamma, eps, K);
+    if (rc != W4A16_OK) return rc;
+    rc = check_gemm(packed, w_scale, residual, y);
+    if (rc != W4A16_OK) return rc;
+    if (!workspace || workspace_bytes < w8a8_workspace_bytes(M, N, K)) return W4A16_EWORKSPACE;
+    if (workspace_misaligned(workspace)) return W4A16_EALIGN;
+    uint8_t *const codes = static_cast<uint8_t *>(workspace) + kTicketBytes;
+    float *const scale = reinterpret_cast<float *>(codes + codes_bytes(M, K));
+    rc = launch_quantize(x, pre, gamma, eps, codes, scale, M, K, (hipStream_t)stream);
+    if (rc != W4A16_OK) return rc;
+    const GemmArgs a = {codes, (const uint8_t *)packed, scale, w_scale, (const _Float16 *)residual, (_Float16 *)y, M, N, k_blocks(K)};
+    return launch_gemm(a, (hipStream_t)stream);
+}
+
+}  // extern "C"
