@@ -3,102 +3,193 @@
 // The (query, head) pairs that share a KV head are the rows of one problem: query-major, pair = query * group + head in its group, so that a
 // tile of rows spans few queries and the keys it sees end almost together.  S^T = K . Q^T leaves a lane with scores of ONE pair (column
 // lane % 32), which are the operand of O^T += V^T . P^T as they stand; the softmax runs in registers, one pass over the keys.
+//
+// Lengths are known on the device only, so the work is dealt out there: the tiles of all sequences and KV heads, each as long as the keys that
+// it sees, lie end to end, and every workgroup takes an equal stretch of that line.  A tile that a border falls into is cut there, and the
+// last of its workgroups to finish joins the pieces (exchange as in tree_attn_kernel; a border cuts one tile, so the tickets of the
+// workgroups do for the tiles).
 #include "attn_common.h"
 
 namespace w4 {
 
 typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float float2v __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) half4v lds_half4v;
 
-constexpr int kKeyTile = 64;      // keys of a step
-constexpr int kMostSplits = 32;
 constexpr int kMostSequences = 4096;
+constexpr int kMostGroups = 256;   // workgroups of a call: one per compute unit, a ticket each
 
 struct PromptArgs {
     const _Float16 *q, *k, *v;
     const int32_t *q_start, *k_start, *k_len;   // k_start, k_len: both or none
     _Float16 *out;
-    float *part_o, *part_ml;
-    int B, rows, k_rows, Hq, Hkv, group, tiles, splits;   // tiles: most row tiles per KV head
+    float *part_o, *part_ml;   // two pieces per workgroup: the cut tile at the start of its stretch, and the one at its end
+    uint32_t *tickets;
+    int B, rows, k_rows, Hq, Hkv, group;
     float scale_log2e;
 };
 
-// Where a workgroup works.  Row tiles are numbered from the last of the last sequence down: the tiles that see most keys of a sequence are
-// the first to be dealt out.  A sequence whose rows or keys do not lie in the buffers has no tiles.
-struct Place {
-    int kvh, unit, split;   // unit: KV head and tile, of the partial results
-    int n, T, q0, k0;       // queries and keys of the sequence, their first rows
-    int first;              // pair of the tile's first row
-    bool any;
-};
-
-template <int ROWS>
-__device__ __forceinline__ Place find_place(const PromptArgs &a, unsigned block, int lane)
+// a / b for 0 <= a < 2^62, 0 < b < 2^55 and a quotient below 2^40: exact.  The reciprocal (after one Newton step good to 2^-45 and better) makes
+// the quotient off by one at the most.
+__device__ __forceinline__ long long divide(long long a, long long b)
 {
-    Place w;
-    // Workgroups go to the eight XCDs in turn.  Where the KV heads divide evenly, an XCD keeps to its own heads, or to its share of a head's
-    // tiles: its L2 then holds the keys of few heads.
-    const unsigned xcd = block & 7u, turn = block >> 3;
-    unsigned number;   // of tile and split
-    if (a.Hkv % 8 == 0) {
-        const unsigned per = (unsigned)a.Hkv >> 3;
-        w.kvh = (int)(xcd + 8 * (turn % per));
-        number = turn / per;
-    } else if (8 % a.Hkv == 0) {
-        const unsigned share = 8u / (unsigned)a.Hkv;
-        w.kvh = (int)(xcd % (unsigned)a.Hkv);
-        number = turn * share + xcd / (unsigned)a.Hkv;
-    } else {
-        w.kvh = (int)(block % (unsigned)a.Hkv);
-        number = block / (unsigned)a.Hkv;
-    }
-    const int tile = (int)(number / (unsigned)a.splits);
-    w.split = (int)(number - (unsigned)tile * (unsigned)a.splits);
-    w.unit = w.kvh * a.tiles + tile;
-    w.any = false;
-    if (tile >= a.tiles) return w;   // the grid's last round, or offsets that overlap
-    int before = 0;
-    for (int base = 0; base < a.B; base += 64) {   // 64 sequences at a time, the last first
-        const int b = a.B - 1 - base - lane;
-        int n = 0, T = 0, q0 = 0, k0 = 0, count = 0;
-        if (b >= 0) {
-            const int q1 = a.q_start[b + 1];
-            q0 = a.q_start[b];
-            if (a.k_len) {
-                k0 = a.k_start[b];
-                T = a.k_len[b];
-            } else {
-                k0 = q0;
-                T = (int)max(-1ll, min((long long)q1 - q0, 0x7FFFFFFFll));
-            }
-            const bool valid = q0 >= 0 && q1 > q0 && q1 <= a.rows && k0 >= 0 && T >= 0 && (long long)k0 + T <= a.k_rows;
-            if (valid) {
-                n = q1 - q0;
-                count = (int)(((long long)n * a.group + ROWS - 1) / ROWS);
-            }
-        }
-        int upto = count;   // tiles of this sequence and of those after it
+    const double d = (double)b, r0 = __builtin_amdgcn_rcp(d), r = __builtin_fma(__builtin_fma(-d, r0, 1.0), r0, r0);
+    const long long q = (long long)((double)a * r), left = a - q * b;
+    return q + (left >= b) - (left < 0);
+}
+
+// What a piece costs beside its keys (places, first transfers, exchange), in keys: 6 us, in which 32 rows go through 256 keys and more, 256 rows
+// through 320.  Without it a stretch could hold dozens of short sequences: 16 of 1 .. 8192 keys, 32/8 heads, one query each, 179 us.
+constexpr int kPieceKeys = 256;
+
+// A sequence, and its place on the line of work.  Tile t of a KV head reaches from cost(t) to cost(t + 1): the keys that its last query sees, about,
+// and kPieceKeys.
+struct Sequence {
+    int n, T, q0, k0, tiles;
+    int ahead;   // keys ahead of the first query
+};
+template <int ROWS>
+__device__ __forceinline__ long long cost(const Sequence &s, int group, int t)
+{
+    return (long long)t * (s.ahead + kPieceKeys) + (long long)t * (t + 1) * (ROWS / 2) / group;   // t (t + 1) even: no half is lost
+}
+
+// sequence b, no tiles if its rows or keys do not lie in the buffers
+template <int ROWS>
+__device__ __forceinline__ Sequence read_sequence(const PromptArgs &a, int b)
+{
+    Sequence s = {0, 0, 0, 0, 0, 0};
+    if (b < 0 || b >= a.B) return s;
+    const int q0 = a.q_start[b], q1 = a.q_start[b + 1];
+    const bool rows_fit = q0 >= 0 && q1 > q0 && q1 <= a.rows;
+    const int k0 = a.k_len ? a.k_start[b] : q0, T = a.k_len ? a.k_len[b] : rows_fit ? q1 - q0 : 0;
+    if (!rows_fit || k0 < 0 || T < 0 || (long long)k0 + T > a.k_rows) return s;
+    s.n = q1 - q0;
+    s.T = T;
+    s.q0 = q0;
+    s.k0 = k0;
+    s.tiles = (int)(((long long)s.n * a.group + ROWS - 1) / ROWS);
+    s.ahead = max(T - s.n, 0);
+    return s;
+}
+
+__device__ __forceinline__ long long shuffle(long long x, int src)
+{
+    const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)x, src, 64), hi = (uint32_t)__shfl((int)(x >> 32), src, 64);
+    return (long long)((uint64_t)hi << 32 | lo);
+}
+
+__device__ __forceinline__ long long of_lane(long long x, int src)
+{
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, src), hi = __builtin_amdgcn_readlane((int)(x >> 32), src);
+    return (long long)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ long long uniform(long long x) { return of_lane(x, 0); }
+
+constexpr long long kLongestLine = 1ll << 54;   // beyond any sensible call (sequences that share rows); products with a workgroup's number stay in 64 bits
+
+// The line of work, as one wavefront sees it (the same in all of them).  Sequences are read 64 at a time, one per lane.
+template <int ROWS>
+struct Line {
+    long long total;              // its length
+    int tiles;                    // on it (at most 2^30 are counted)
+    long long from, to;           // the sequence at hand reaches from .. to
+    long long per_head;           // of each KV head
+    Sequence seq;
+    long long before;             // length up to the first of the 64 sequences from `base` on, among which the one at hand is
+    int base;
+
+    // sequence base + lane, and the length up to and including it
+    __device__ __forceinline__ long long read(const PromptArgs &a, Sequence &mine, int lane) const
+    {
+        mine = read_sequence<ROWS>(a, base + lane);
+        long long upto = min(cost<ROWS>(mine, a.group, mine.tiles) * a.Hkv, kLongestLine);
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
-            const int other = __shfl_up(upto, off, 64);
-            if (lane >= off) upto += other;
+            const long long other = shuffle(upto, max(lane - off, 0));
+            if (lane >= off) upto = min(upto + other, kLongestLine);
         }
-        const uint64_t hit = __ballot(before + upto > tile);
-        if (hit) {
-            const int src = __builtin_ctzll(hit);
-            const int mine = tile - before - __shfl(upto - count, src, 64);   // tile of the sequence, counted from its last
-            w.n = __builtin_amdgcn_readfirstlane(__shfl(n, src, 64));
-            w.T = __builtin_amdgcn_readfirstlane(__shfl(T, src, 64));
-            w.q0 = __builtin_amdgcn_readfirstlane(__shfl(q0, src, 64));
-            w.k0 = __builtin_amdgcn_readfirstlane(__shfl(k0, src, 64));
-            w.first = __builtin_amdgcn_readfirstlane((__shfl(count, src, 64) - 1 - mine) * ROWS);
-            w.any = true;
-            break;
-        }
-        before += __shfl(upto, 63, 64);
+        return min(upto + before, kLongestLine);
     }
-    return w;
+    __device__ __forceinline__ Line(const PromptArgs &a, int lane, Sequence &mine, long long &upto)
+    {
+        total = from = to = per_head = before = 0;
+        tiles = 0;
+        for (base = 0; base < a.B; base += 64) {
+            upto = read(a, mine, lane);
+            before = of_lane(upto, 63);
+            int here = mine.tiles * a.Hkv;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) here += __shfl_xor(here, off, 64);
+            tiles = (int)min((uint32_t)tiles + (uint32_t)__builtin_amdgcn_readfirstlane(here), 1u << 30);
+        }
+        total = before;
+        before = 0;
+        base = 0;
+    }
+    // brings the sequence that holds place `at` to hand; at < total, and no place before the last one asked for.  mine, upto: what the constructor
+    // read, if `known`
+    __device__ __forceinline__ void find(const PromptArgs &a, long long at, int lane, Sequence mine, long long upto, bool known)
+    {
+        if (at >= from && at < to) return;
+        for (;; base += 64) {
+            if (!known) upto = read(a, mine, lane);
+            known = false;
+            const uint64_t hit = __ballot(upto > at);
+            if (hit) {
+                const int src = __builtin_ctzll(hit);
+                auto take = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
+                seq = {take(mine.n), take(mine.T), take(mine.q0), take(mine.k0), take(mine.tiles), take(mine.ahead)};
+                per_head = cost<ROWS>(seq, a.group, seq.tiles);
+                to = of_lane(upto, src);
+                from = to - per_head * a.Hkv;
+                return;
+            }
+            before = of_lane(upto, 63);
+        }
+    }
+};
+
+// One piece of work: steps s0 .. s1 - 1 of a tile.
+struct Piece {
+    int kvh, first, rows;      // KV head, pair of the first row, rows
+    int steps, s0, s1;         // of the whole tile; of this piece
+    long long begin, end;      // of the tile on the line
+};
+template <int ROWS, int STEP>
+__device__ __forceinline__ void tile_of(const PromptArgs &a, const Line<ROWS> &line, long long at, Piece &p)
+{
+    const Sequence &s = line.seq;
+    long long rel = at - line.from;
+    p.kvh = __builtin_amdgcn_readfirstlane((int)divide(rel, line.per_head));
+    rel -= p.kvh * line.per_head;
+    int lo = 0, hi = s.tiles - 1;   // the last tile that begins at or before rel
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (cost<ROWS>(s, a.group, mid) <= rel) lo = mid;
+        else hi = mid - 1;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    p.begin = uniform(line.from + p.kvh * line.per_head + cost<ROWS>(s, a.group, lo));
+    p.end = uniform(line.from + p.kvh * line.per_head + cost<ROWS>(s, a.group, lo + 1));
+    const int pairs = s.n * a.group;
+    p.first = lo * ROWS;
+    p.rows = min(ROWS, pairs - p.first);
+    const int seen = s.T - s.n + (p.first + p.rows - 1) / a.group + 1;   // keys that the tile's last row sees
+    p.steps = __builtin_amdgcn_readfirstlane(seen > 0 ? (seen + STEP - 1) / STEP : 0);
+}
+// step of a tile at a place on the line
+__device__ __forceinline__ int step_at(const Piece &p, long long at)
+{
+    return at >= p.end ? p.steps : (int)divide((at - p.begin) * p.steps, p.end - p.begin);
+}
+
+// Workgroups go to the eight XCDs in turn; an XCD gets neighbouring stretches, so that its L2 holds the keys of few heads.
+__device__ __forceinline__ unsigned stretch_number(unsigned block, unsigned grid)
+{
+    const unsigned xcd = block & 7u;
+    return xcd * (grid >> 3) + min(xcd, grid & 7u) + (block >> 3);
 }
 
 __device__ __forceinline__ half8v read_chunk(const uint8_t *p) { return *reinterpret_cast<const half8v *>(p); }
@@ -109,242 +200,568 @@ __device__ __forceinline__ half4v read_transposed(const uint8_t *p)
 }
 __device__ __forceinline__ bool not_finite(_Float16 x) { return (__builtin_bit_cast(uint16_t, x) & 0x7C00u) == 0x7C00u; }
 
-// One workgroup of NW wavefronts: NW * 32 * RT rows, keys through LDS in tiles of 64, two buffers, one barrier per tile.
-template <int D, int NW, int RT>
-__global__ __launch_bounds__(64 * NW) void prompt_attn_tile_kernel(PromptArgs a)
+// Chunks of sixteen bytes lie permuted in the LDS tiles, so that fragment reads spread over the banks.
+template <int D>
+struct Tile {
+    static constexpr int ROW = D * 2, CHUNKS = D / 8;
+    __device__ __forceinline__ static uint32_t k_place(int key, int chunk) { return (uint32_t)(key * ROW + ((chunk ^ (key & 7)) << 4)); }
+    __device__ __forceinline__ static uint32_t v_place(int key, int chunk) { return (uint32_t)(key * ROW + ((chunk ^ (2 * key & (CHUNKS - 1))) << 4)); }
+};
+
+// 32 rows (pairs) of a wavefront, lane column c = lane % 32: queries, outputs so far and the running state of the softmax
+template <int D>
+struct Rows {
+    half8v qf[D / 16];
+    float16v o[D / 32];
+    float m_run, l_run;   // l_run: this lane's share (its keys) of the row's sum
+    int pos;              // the row sees keys 0 .. pos
+
+    __device__ __forceinline__ void start(const PromptArgs &a, const Sequence &s, const Piece &p, int row, int h)
+    {
+        const int pair = p.first + min(row, p.rows - 1), query = pair / a.group;
+        pos = s.T - s.n + query;
+        const _Float16 *src = a.q + ((size_t)(s.q0 + query) * a.Hq + p.kvh * a.group + (pair - query * a.group)) * D + 8 * h;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) qf[j] = *reinterpret_cast<const half8v *>(src + 16 * j);
+        m_run = kLowest;
+        l_run = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+    }
+    // Makes the compiler wait for the queries here: left to their first use, in the loop, its wait would count the transfers under way there, too.
+    __device__ __forceinline__ void arrive()
+    {
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) asm volatile("" : "+v"(qf[j]));
+    }
+
+    // scores of 32 keys, in two steps: the fragments of the K tile, and their products
+    __device__ __forceinline__ static void read_keys(half8v (&kf)[D / 16], const uint8_t *ktile, uint32_t kfrag)
+    {
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) kf[j] = read_chunk(ktile + (kfrag ^ (j << 5)));
+    }
+    __device__ __forceinline__ void scores(float16v &s, const half8v (&kf)[D / 16]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[j], qf[j], s, 0, 0, 0);
+    }
+
+    // their probabilities, as operands of the product with the values; what came before is brought to the new maximum
+    template <int KT, bool MASKED>
+    __device__ __forceinline__ void softmax(float16v (&s)[KT], half8v (&pb)[2 * KT], int key0, float scale_log2e, int h)
+    {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) settled(s[kt]);
+        if constexpr (MASKED) {
+            const int room = pos - key0 - 4 * h;   // key 32 kt + 8 (i / 4) + 4 h + i % 4 of the tile is seen up to the position
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[kt][i] = 32 * kt + 8 * (i >> 2) + (i & 3) <= room ? s[kt][i] : -__builtin_inff();
+        }
+        float m[2] = {max_of_two(s[0][0], s[0][1]), max_of_two(s[0][2], s[0][3])};
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int i = kt ? 0 : 4; i < 16; i += 2) m[(i >> 1) & 1] = max_of_three(m[(i >> 1) & 1], s[kt][i], s[kt][i + 1]);
+        // The scale is positive (checked by the host): the largest raw score is the largest scaled one.  The maximum that the exponentials are taken
+        // from moves only where it has grown by 8 (a factor of 2^8, in fp16 probabilities of up to 256): the outputs are seldom scaled, and any
+        // reference that is not far below the largest score serves as well.
+        const float m_seen = half_wave_max(max_of_two(m[0], m[1])) * scale_log2e;
+        const bool moves = !(m_seen <= m_run + 8.f);
+        if (__any(moves)) {
+            const float m_new = moves ? max_of_two(m_run, m_seen) : m_run, alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
+        }
+        const float less = -m_run;
+        float sum[4] = {};
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], scale_log2e, less));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i + 1], scale_log2e, less));
+                sum[i & 3] += p0;
+                sum[(i & 3) + 1] += p1;
+                const half2v both = __builtin_convertvector((float2v){p0, p1}, half2v);
+                pb[2 * kt + (i >> 3)][i & 7] = both[0];
+                pb[2 * kt + (i >> 3)][(i & 7) + 1] = both[1];
+            }
+        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+
+    // fragments u of the V tile: 16 keys, all D values
+    template <bool MASKED>
+    __device__ __forceinline__ static void read_values(half8v (&vf)[D / 32], bool &bad, const uint8_t *vtile, int u, uint32_t vfrag)
+    {
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) {
+            const uint8_t *const p = vtile + u * 16 * Tile<D>::ROW + (vfrag ^ (dt << 6));
+            const half4v lo = read_transposed(p), hi = read_transposed(p + 8 * Tile<D>::ROW);
+            vf[dt] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            if constexpr (MASKED) {   // what a row does not see may be anything: 0 times it need not be 0
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool b = not_finite(vf[dt][e]);
+                    bad |= b;
+                    vf[dt][e] = b ? (_Float16)0 : vf[dt][e];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void add_product(const half8v (&vf)[D / 32], half8v pb)
+    {
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[dt], pb, o[dt], 0, 0, 0);
+    }
+    // rows that do see a value that is not finite: it joins their sums as it is
+    template <int KT>
+    __device__ __forceinline__ void add_not_finite(const uint8_t *vtile, int key0, int h)
+    {
+        for (int key = 0; key < 32 * KT; ++key)
+            for (int chunk = 0; chunk < D / 8; ++chunk) {   // elements 8 chunk + 4 h ..
+                const half4v x = *reinterpret_cast<const half4v *>(vtile + Tile<D>::v_place(key, chunk) + 8 * h);
+                if (!__any(not_finite(x[0]) || not_finite(x[1]) || not_finite(x[2]) || not_finite(x[3])) || key0 + key > pos) continue;
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                    for (int quad = 0; quad < 4; ++quad)
+                        if (4 * dt + quad == chunk)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[dt][4 * quad + e] += not_finite(x[e]) ? (float)x[e] : 0.f;
+            }
+    }
+    template <int KT, bool MASKED>
+    __device__ __forceinline__ void values(const half8v (&pb)[2 * KT], const uint8_t *vtile, int key0, int h, uint32_t vfrag)
+    {
+        bool bad = false;
+        half8v vf[2][D / 32];
+        read_values<MASKED>(vf[0], bad, vtile, 0, vfrag);
+#pragma unroll
+        for (int u = 0; u < 2 * KT; ++u) {
+            if (u + 1 < 2 * KT) read_values<MASKED>(vf[(u + 1) & 1], bad, vtile, u + 1, vfrag);
+            add_product(vf[u & 1], pb[u]);
+        }
+        settled(o[D / 32 - 1]);   // the branches behind this go round too little for the last product
+        if constexpr (MASKED)
+            if (__any(bad)) add_not_finite<KT>(vtile, key0, h);
+    }
+};
+
+// V: lane s of 16-lane block b points at key row 4 (b / 2) + s / 4 (and 8 further on), elements 32 dt + 16 (b % 2) + 4 (s % 4) ..
+template <int D>
+__device__ __forceinline__ uint32_t v_fragment(int lane)
 {
-    constexpr int ROWS = 32 * RT * NW;
-    constexpr int ROW_BYTES = D * 2, CHUNKS = D / 8, TILE = kKeyTile * ROW_BYTES;
-    constexpr int PER = 1024 / ROW_BYTES;                  // rows of a transfer
-    constexpr int TRANSFERS = TILE / 1024 / NW;            // of a wavefront, K and V each
+    const int key = 4 * (lane >> 5) + ((lane & 15) >> 2);
+    return Tile<D>::v_place(key, 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + 8 * (lane & 1);
+}
+
+__device__ __forceinline__ void store_row_quad(const PromptArgs &a, const Sequence &s, const Piece &p, int row, int D, int d, float4v val, float l)
+{
+    const int pair = p.first + row, query = pair / a.group;
+    // a row that sees no key gets zeros; one whose scores are all -inf 0 / 0
+    const float inv = s.T - s.n + query >= 0 ? 1.f / l : 0.f;
+    half4v y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (_Float16)(val[e] * inv);
+    *reinterpret_cast<half4v *>(a.out + ((size_t)(s.q0 + query) * a.Hq + p.kvh * a.group + (pair - query * a.group)) * D + d) = y;
+}
+
+// Where the piece of a cut tile goes: workgroup i keeps the tile that its stretch begins in at 2 i, the one that it ends in at 2 i + 1.
+template <int D, int ROWS>
+struct Pieces {
+    __device__ __forceinline__ static PartialBuffer o(const PromptArgs &a, unsigned slot) { return partial_buffer(a.part_o + (size_t)slot * ROWS * D); }
+    __device__ __forceinline__ static PartialBuffer ml(const PromptArgs &a, unsigned slot) { return partial_buffer(a.part_ml + (size_t)slot * ROWS * 2); }
+};
+
+// Joins `pieces` pieces of a cut tile; called by the last of its workgroups to finish.  Where the rows are few, several groups of threads take
+// every so-manieth piece each and meet in LDS (`shared`, THREADS * 24 bytes): a piece's loads are one trip to memory, eight at a time.
+template <int D, int ROWS, int THREADS>
+__device__ __forceinline__ void join_pieces(const PromptArgs &a, const Sequence &s, const Piece &p, const uint16_t *slots, int pieces, int tid, float *shared)
+{
+    const int items = p.rows * (D / 4);
+    const int parts = items <= THREADS / 4 ? 4 : items <= THREADS / 2 ? 2 : 1, stride = THREADS / parts;   // uniform
+    const int part = tid / stride;
+    for (int item = tid % stride; item < items; item += stride) {
+        const int row = item / (D / 4), d4 = item % (D / 4);
+        float m = kLowest, den = 0.f;
+        float4v num = {0.f, 0.f, 0.f, 0.f};
+        constexpr int AT_ONCE = 8;
+        for (int w = part; w < pieces; w += AT_ONCE * parts) {
+            float ms[AT_ONCE], ls[AT_ONCE];
+            float4v os[AT_ONCE];
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) {
+                const unsigned slot = __builtin_amdgcn_readfirstlane(slots[min(w + e * parts, pieces - 1)]);   // a wavefront is in one part
+                const PartialBuffer po = Pieces<D, ROWS>::o(a, slot), pm = Pieces<D, ROWS>::ml(a, slot);
+                ms[e] = load_partial_f32(pm, 2 * row);
+                ls[e] = load_partial_f32(pm, 2 * row + 1);
+                os[e] = load_partial(po, row * (D / 4) + d4);
+            }
+            float top = m;
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) top = fmaxf(top, ms[e]);
+            const float keep = __builtin_amdgcn_exp2f(m - top);
+            den *= keep;
+            num *= keep;
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) {
+                if (w + e * parts >= pieces) break;
+                const float wgt = __builtin_amdgcn_exp2f(ms[e] - top);
+                den += wgt * ls[e];
+                num += wgt * os[e];
+            }
+            m = top;
+        }
+        if (parts > 1) {   // uniform; there is one round of items then
+            *reinterpret_cast<float4v *>(shared + tid * 4) = num;
+            shared[THREADS * 4 + tid] = m;
+            shared[THREADS * 5 + tid] = den;
+        } else store_row_quad(a, s, p, row, D, 4 * d4, num, den);
+    }
+    if (parts > 1) {
+        __syncthreads();
+        if (tid < items) {
+            float m = kLowest, den = 0.f;
+            float4v num = {0.f, 0.f, 0.f, 0.f};
+            for (int g = 0; g < parts; ++g) m = fmaxf(m, shared[THREADS * 4 + g * stride + tid]);
+            for (int g = 0; g < parts; ++g) {
+                const float wgt = __builtin_amdgcn_exp2f(shared[THREADS * 4 + g * stride + tid] - m);
+                den += wgt * shared[THREADS * 5 + g * stride + tid];
+                num += wgt * *reinterpret_cast<const float4v *>(shared + (g * stride + tid) * 4);
+            }
+            store_row_quad(a, s, p, tid / (D / 4), D, tid % (D / 4) * 4, num, den);
+        }
+    }
+}
+
+// Goes through a workgroup's stretch, piece by piece.  work(sequence, piece, whole, slot) computes steps s0 .. s1 - 1 (s0 < s1) and stores the
+// outputs (whole) or the piece's state.  LEAST: a tile is not cut into pieces shorter than this, in keys.
+template <int D, int ROWS, int STEP, int LEAST, int THREADS, typename Work>
+__device__ __forceinline__ void go_through(const PromptArgs &a, int tid, float *shared, Work work)
+{
+    static_assert(kMostGroups <= THREADS, "");
+    const int lane = tid & 63;
+    __shared__ uint32_t ticket_sh, pieces_sh[THREADS / 64];
+    __shared__ uint16_t slots[kMostGroups];
+    Sequence mine;
+    long long first_upto;
+    Line<ROWS> line(a, lane, mine, first_upto);
+    const unsigned groups = (unsigned)min((long long)gridDim.x, max((long long)max(line.tiles, 1), line.total / LEAST));
+    if (blockIdx.x >= groups) return;
+    const long long stretch_length = uniform(divide(line.total + groups - 1, groups));
+    auto border = [&](unsigned w) { return min(stretch_length * w, line.total); };
+    const unsigned me = stretch_number(blockIdx.x, groups);
+    const long long start = border(me), stop = border(me + 1);
+    long long at = start;
+    if (at < stop) line.find(a, at, lane, mine, first_upto, a.B <= 64);
+    while (at < stop) {   // uniform over the workgroup
+        Piece p;
+        tile_of<ROWS, STEP>(a, line, at, p);
+        const long long upto = stop < p.end ? stop : p.end;
+        p.s0 = __builtin_amdgcn_readfirstlane(step_at(p, at));
+        p.s1 = __builtin_amdgcn_readfirstlane(step_at(p, upto));
+        if (p.steps == 0) {   // none of its rows sees a key
+            if (at == p.begin)
+                for (int item = tid; item < p.rows * (D / 4); item += THREADS)
+                    store_row_quad(a, line.seq, p, item / (D / 4), D, item % (D / 4) * 4, (float4v){0.f, 0.f, 0.f, 0.f}, 1.f);
+        } else if (p.s0 < p.s1) {
+            const bool whole = p.s1 - p.s0 == p.steps;
+            work(line.seq, p, whole, 2 * me + (at > start ? 1u : 0u));
+            if (!whole) {
+                // the workgroups that have a step of the tile, w0 the one where it begins
+                const unsigned w0 = (unsigned)divide(p.begin, stretch_length), w1 = (unsigned)divide(p.end - 1, stretch_length);
+                const unsigned w = w0 + tid;
+                bool has = false, later = false;
+                if (w <= w1) {
+                    const long long b = border(w), e = border(w + 1);
+                    has = step_at(p, max(b, p.begin)) != step_at(p, min(e, p.end));
+                    later = p.begin > b;
+                }
+                const uint64_t all = __ballot(has);
+                if (lane == 0) pieces_sh[tid >> 6] = (uint32_t)__builtin_popcountll(all);
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wavefront's part of the piece has reached memory
+                __syncthreads();
+                uint32_t pieces = 0, ahead = 0;
+#pragma unroll
+                for (int i = 0; i < THREADS / 64; ++i) {
+                    ahead += i < (tid >> 6) ? pieces_sh[i] : 0;
+                    pieces += pieces_sh[i];
+                }
+                if (has) slots[ahead + __builtin_popcountll(all & ((1ull << lane) - 1))] = (uint16_t)(2 * w + later);
+                if (tid == 0) ticket_sh = __hip_atomic_fetch_add(&a.tickets[w0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __syncthreads();
+                if (ticket_sh == pieces - 1) {
+                    if (tid == 0) __hip_atomic_store(&a.tickets[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    join_pieces<D, ROWS, THREADS>(a, line.seq, p, slots, (int)pieces, tid, shared);
+                }
+            }
+            __syncthreads();   // LDS and the ticket are free for the next piece
+        }
+        at = upto;
+        if (at < stop) line.find(a, at, lane, mine, 0, false);
+    }
+}
+
+// Many tiles: one per workgroup, whole.  They are numbered from the last of the last sequence down, so that the tiles that see most keys of a sequence are
+// the first to be dealt out, and an XCD keeps to its own KV heads or to its share of a head's tiles: workgroups that start together read the same keys,
+// which come from memory once for all of them (16384 queries, 32/8 heads: 2449 us, in equal stretches 3000).
+template <int D, int ROWS, int STEP, typename Work>
+__device__ __forceinline__ void take_one(const PromptArgs &a, int lane, Work work)
+{
+    const unsigned xcd = blockIdx.x & 7u, turn = blockIdx.x >> 3, heads = (unsigned)a.Hkv;
+    unsigned kvh, number;
+    if (heads % 8 == 0) {
+        kvh = xcd + 8 * (turn % (heads >> 3));
+        number = turn / (heads >> 3);
+    } else if (8 % heads == 0) {
+        kvh = xcd % heads;
+        number = turn * (8 / heads) + xcd / heads;
+    } else {
+        kvh = blockIdx.x % heads;
+        number = blockIdx.x / heads;
+    }
+    long long before = 0;
+    for (int base = 0; base < a.B; base += 64) {   // 64 sequences at a time, the last first
+        const Sequence mine = read_sequence<ROWS>(a, a.B - 1 - base - lane);
+        int upto = mine.tiles;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int other = __shfl_up(upto, off, 64);
+            if (lane >= off) upto += other;
+        }
+        const uint64_t hit = __ballot(before + upto > (long long)number);
+        if (hit) {
+            const int src = __builtin_ctzll(hit);
+            auto take = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
+            const Sequence s = {take(mine.n), take(mine.T), take(mine.q0), take(mine.k0), take(mine.tiles), take(mine.ahead)};
+            Piece p;
+            p.kvh = (int)kvh;
+            p.first = (take(upto) - 1 - (int)(number - before)) * ROWS;   // its tiles end at `upto`: the first of them is the sequence's last
+            p.rows = min(ROWS, s.n * a.group - p.first);
+            const int seen = s.T - s.n + (p.first + p.rows - 1) / a.group + 1;
+            p.steps = p.s1 = seen > 0 ? (seen + STEP - 1) / STEP : 0;
+            p.s0 = 0;
+            p.begin = p.end = 0;
+            work(s, p, true, 0u);
+            return;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+}
+
+// Many rows: eight wavefronts of 32 rows each, keys through LDS in tiles of 64, one barrier per tile, four buffers: three tiles are under way.
+constexpr int kStages = 4, kTileRows = 256, kTileKeys = 64;
+template <int D, bool CUT>
+__global__ __launch_bounds__(512) void prompt_attn_tile_kernel(PromptArgs a)
+{
+    constexpr int ROWS = kTileRows, KEYS = kTileKeys, NW = 8, KT = KEYS / 32;
+    constexpr int ROW = Tile<D>::ROW, CHUNKS = Tile<D>::CHUNKS, TILE = KEYS * ROW;
+    constexpr int PER = 1024 / ROW;                  // rows of a transfer
+    constexpr int TRANSFERS = TILE / 1024 / NW;      // of a wavefront, K and V each
     static_assert(TRANSFERS >= 1, "");
-    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TILE];   // K, V; K, V
+    extern __shared__ float4v smem4[];
+    uint8_t *const lds = reinterpret_cast<uint8_t *>(smem4);   // kStages times K, V
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, c = lane & 31;
-    const Place at = find_place<ROWS>(a, blockIdx.x, lane);
-    if (!at.any) return;   // uniform over the workgroup
-    const int pairs = at.n * a.group, last = min(at.first + ROWS, pairs) - 1;   // pairs <= 2^31 by the host's checks
-    // position of a row's query among the keys: it sees keys 0 .. position
-    int pair[RT], pos[RT];
-    size_t elem[RT];   // of its (query, head) in q and out
-    half8v qf[RT][D / 16];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        pair[r] = at.first + (wave * RT + r) * 32 + c;
-        const int p = min(pair[r], pairs - 1), query = p / a.group;
-        pos[r] = at.T - at.n + query;
-        elem[r] = ((size_t)(at.q0 + query) * a.Hq + at.kvh * a.group + (p - query * a.group)) * D;
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) qf[r][j] = *reinterpret_cast<const half8v *>(a.q + elem[r] + 16 * j + 8 * h);
-    }
-    const int seen = at.T - at.n + last / a.group + 1;                    // keys that the tile's last row sees
-    const int steps = seen > 0 ? (seen + kKeyTile - 1) / kKeyTile : 0;
-    const int s0 = (int)((long long)steps * at.split / a.splits), s1 = (int)((long long)steps * (at.split + 1) / a.splits);
-    // keys up to which every row of the wavefront sees all
-    const int wave_first = min(at.first + wave * RT * 32, pairs - 1);
-    const int all_see = at.T - at.n + wave_first / a.group + 1;
-    const int wave_seen = at.T - at.n + min(at.first + (wave + 1) * RT * 32 - 1, pairs - 1) / a.group + 1;
-
-    const uint32_t stride = (uint32_t)a.Hkv * ROW_BYTES;
-    const uint8_t *const k_src = reinterpret_cast<const uint8_t *>(a.k) + ((size_t)at.k0 * a.Hkv + at.kvh) * ROW_BYTES;
-    const uint8_t *const v_src = reinterpret_cast<const uint8_t *>(a.v) + ((size_t)at.k0 * a.Hkv + at.kvh) * ROW_BYTES;
+    const uint32_t kfrag = Tile<D>::k_place(c, h), vfrag = v_fragment<D>(lane);
     const int trow = lane / CHUNKS, tchunk = lane % CHUNKS;
-    auto request = [&](int step, uint8_t *buffer) {
-        const int key0 = step * kKeyTile;
-        const Stretch ks = stretch(k_src + (size_t)key0 * stride, 0x7FFFFFFF), vs = stretch(v_src + (size_t)key0 * stride, 0x7FFFFFFF);
-#pragma unroll
-        for (int i = 0; i < TRANSFERS; ++i) {
-            const int t = wave * TRANSFERS + i, row = t * PER + trow;
-            const uint32_t from = (uint32_t)min(row, at.T - 1 - key0) * stride;   // rows beyond the last key repeat it; they are masked
-            quad_to_lds(ks, buffer + t * 1024, from + ((tchunk ^ (row & 7)) << 4), 0);
-            quad_to_lds(vs, buffer + TILE + t * 1024, from + ((tchunk ^ (2 * row & (CHUNKS - 1))) << 4), 0);
-        }
-    };
+    const uint32_t stride = (uint32_t)a.Hkv * ROW;
 
-    float16v o[RT][D / 32];
-    float m_run[RT], l_run[RT];
+    auto work = [&](const Sequence &s, const Piece &p, bool whole, unsigned slot) {
+        const uint8_t *const k_src = reinterpret_cast<const uint8_t *>(a.k) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
+        const uint8_t *const v_src = reinterpret_cast<const uint8_t *>(a.v) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
+        auto stage = [&](int step) { return lds + (step & (kStages - 1)) * 2 * TILE; };
+        auto request = [&](int step) {
+            if (step >= p.s1) return;
+            const int key0 = step * KEYS;
+            uint8_t *const buffer = stage(step);
+            const Stretch ks = stretch(k_src + (size_t)key0 * stride, 0x7FFFFFFF), vs = stretch(v_src + (size_t)key0 * stride, 0x7FFFFFFF);
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        m_run[r] = kLowest;
-        l_run[r] = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[r][dt][i] = 0.f;
-    }
-    const uint32_t kfrag = (uint32_t)(c * ROW_BYTES + ((h ^ (c & 7)) << 4));
-    const int vkey = 4 * h + ((lane & 15) >> 2);
-    const uint32_t vfrag = (uint32_t)(vkey * ROW_BYTES + ((((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ (2 * vkey)) & (CHUNKS - 1)) << 4) + 8 * (lane & 1));
-
-    auto walk = [&](int step, const uint8_t *ktile, auto masked) {
-        constexpr bool MASKED = decltype(masked)::value;
-        const uint8_t *const vtile = ktile + TILE;
-        const int key0 = step * kKeyTile;
-        float16v s[RT][2];
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[r][kt][i] = 0.f;
-#pragma unroll
-            for (int j = 0; j < D / 16; ++j) {
-                const half8v kf = read_chunk(ktile + kt * 32 * ROW_BYTES + (kfrag ^ (j << 5)));
-#pragma unroll
-                for (int r = 0; r < RT; ++r) s[r][kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[r][j], s[r][kt], 0, 0, 0);
+            for (int i = 0; i < TRANSFERS; ++i) {
+                const int t = wave * TRANSFERS + i, row = t * PER + trow;
+                const uint32_t from = (uint32_t)min(row, s.T - 1 - key0) * stride;   // rows beyond the last key repeat it; they are masked
+                quad_to_lds(ks, buffer + t * 1024, from + ((tchunk ^ (row & 7)) << 4), 0);
+                quad_to_lds(vs, buffer + TILE + t * 1024, from + ((tchunk ^ (2 * row & (CHUNKS - 1))) << 4), 0);
             }
-        }
-        half8v pb[RT][4];
+        };
+        Rows<D> rows;
+        rows.start(a, s, p, wave * 32 + c, h);
+        request(p.s0);
+        request(p.s0 + 1);
+        request(p.s0 + 2);
+        rows.arrive();
+        // steps that every row of the workgroup sees whole: they and the others have loops of their own, without branches in them (outputs and scores
+        // that two paths write to cost hundreds of registers in copies)
+        const int all_see = s.T - s.n + p.first / a.group + 1, open = min(all_see / KEYS, p.s1);
+        auto body = [&](int step, auto masked) {
+            constexpr bool MASKED = decltype(masked)::value;
+            // this tile has landed (the two behind it need not have), and the one before it has been read
+            if (step + 2 < p.s1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 * TRANSFERS) : "memory");
+            else if (step + 1 < p.s1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * TRANSFERS) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            request(step + kStages - 1);
+            const uint8_t *const ktile = stage(step);
+            float16v sc[KT];
+            half8v pb[2 * KT];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            settled(s[r][0]);
-            settled(s[r][1]);
-            if constexpr (MASKED) {
-                const int room = pos[r] - key0 - 4 * h;   // key 32 kt + 8 (i / 4) + 4 h + i % 4 of the tile is seen up to the position
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[r][kt][i] = 32 * kt + 8 * (i >> 2) + (i & 3) <= room ? s[r][kt][i] : -__builtin_inff();
+            for (int kt = 0; kt < KT; ++kt) {
+                half8v kf[D / 16];
+                rows.read_keys(kf, ktile + kt * 32 * ROW, kfrag);
+                rows.scores(sc[kt], kf);
             }
-            float m = max_of_two(s[r][0][0], s[r][0][1]);
-#pragma unroll
-            for (int i = 2; i < 16; i += 2) m = max_of_three(m, s[r][0][i], s[r][0][i + 1]);
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) m = max_of_three(m, s[r][1][i], s[r][1][i + 1]);
-            const float m_new = max_of_two(m_run[r], half_wave_max(m) * a.scale_log2e);
-            const float alpha = __builtin_amdgcn_exp2f(m_run[r] - m_new);
-            float sum[4] = {};
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][kt][i], a.scale_log2e, -m_new));
-                    sum[i & 3] += p;
-                    pb[r][2 * kt + (i >> 3)][i & 7] = (_Float16)p;
-                }
-            l_run[r] = l_run[r] * alpha + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
-            m_run[r] = m_new;
-            if (__any(alpha != 1.0f)) {
-#pragma unroll
-                for (int dt = 0; dt < D / 32; ++dt) o[r][dt] *= alpha;
-            }
-        }
-        bool bad = false;
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint8_t *const p = vtile + u * 16 * ROW_BYTES + (vfrag ^ (dt << 6));
-                const half4v lo = read_transposed(p), hi = read_transposed(p + 8 * ROW_BYTES);
-                half8v vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                if constexpr (MASKED) {   // what a row does not see may be anything: 0 times it need not be 0
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool b = not_finite(vf[e]);
-                        bad |= b;
-                        vf[e] = b ? (_Float16)0 : vf[e];
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < RT; ++r) o[r][dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pb[r][u], o[r][dt], 0, 0, 0);
-            }
-        settled(o[RT - 1][D / 32 - 1]);   // the loop's branches go round too little for the last product
-        if constexpr (MASKED) {
-            if (__any(bad)) {   // rows that do see such a value: it joins their sums as it is
-                for (int key = 0; key < kKeyTile; ++key)
-#pragma unroll
-                    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                        for (int quad = 0; quad < 4; ++quad) {   // elements 32 dt + 8 quad + 4 h ..
-                            const half4v x = *reinterpret_cast<const half4v *>(vtile + key * ROW_BYTES + (((4 * dt + quad) ^ (2 * key & (CHUNKS - 1))) << 4) + 8 * h);
-#pragma unroll
-                            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    if (not_finite(x[e]) && key0 + key <= pos[r]) o[r][dt][4 * quad + e] += (float)x[e];
-                        }
-            }
-        }
-    };
-
-    if (s0 < s1) {
-        request(s0, lds);
-        for (int step = s0; step < s1; ++step) {
-            uint8_t *const buffer = lds + ((step - s0) & 1) * 2 * TILE;
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this tile has landed, the other buffer has been read
-            if (step + 1 < s1) request(step + 1, lds + ((step + 1 - s0) & 1) * 2 * TILE);
-            const int key1 = (step + 1) * kKeyTile;
-            if (key1 <= all_see) walk(step, buffer, std::false_type{});        // uniform over the wavefront
-            else if (key1 - kKeyTile < wave_seen) walk(step, buffer, std::true_type{});
-        }
-    }
-
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const float l = l_run[r] + __shfl_xor(l_run[r], 32, 64);
-        if (pair[r] >= pairs) continue;
-        if (a.splits == 1) {
-            const float inv = pos[r] >= 0 ? 1.f / l : 0.f;   // a row that sees no key gets zeros; one whose scores are all -inf 0 / 0
+            rows.template softmax<KT, MASKED>(sc, pb, step * KEYS, a.scale_log2e, h);
+            rows.template values<KT, MASKED>(pb, ktile + TILE, step * KEYS, h, vfrag);
+        };
+        int step = p.s0;
+        for (; step < open; ++step) body(step, std::false_type{});
+        for (; step < p.s1; ++step) body(step, std::true_type{});
+        const PartialBuffer po = Pieces<D, ROWS>::o(a, slot), pm = Pieces<D, ROWS>::ml(a, slot);
+        const float l = rows.l_run + __shfl_xor(rows.l_run, 32, 64);
+        const int row = wave * 32 + c;
+        if (row < p.rows) {
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    half4v y;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = (_Float16)(o[r][dt][4 * g + e] * inv);
-                    *reinterpret_cast<half4v *>(a.out + elem[r] + 32 * dt + 8 * g + 4 * h) = y;
+                    const float4v val = {rows.o[dt][4 * g], rows.o[dt][4 * g + 1], rows.o[dt][4 * g + 2], rows.o[dt][4 * g + 3]};
+                    const int d = 32 * dt + 8 * g + 4 * h;
+                    if (whole) store_row_quad(a, s, p, row, D, d, val, l);
+                    else store_partial(po, (row * D + d) / 4, val);
                 }
-        } else {
-            const size_t row = ((size_t)at.unit * a.splits + at.split) * ROWS + (pair[r] - at.first);
-#pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<float4v *>(a.part_o + row * D + 32 * dt + 8 * g + 4 * h) =
-                        (float4v){o[r][dt][4 * g], o[r][dt][4 * g + 1], o[r][dt][4 * g + 2], o[r][dt][4 * g + 3]};
-            if (h == 0) {
-                a.part_ml[2 * row] = m_run[r];
-                a.part_ml[2 * row + 1] = l;
+            if (!whole && h == 0) {
+                store_partial_f32(pm, 2 * row, rows.m_run);
+                store_partial_f32(pm, 2 * row + 1, l);
             }
         }
-    }
+    };
+    if constexpr (CUT) go_through<D, ROWS, KEYS, 1024, 64 * NW>(a, tid, reinterpret_cast<float *>(lds), work);
+    else take_one<D, ROWS, KEYS>(a, lane, work);
 }
 
-// The ranges of a tile's keys joined: D / 4 threads per row, four outputs each, ranges in order.  Grid as that of the tiles with one split.
-template <int D, int ROWS>
-__global__ __launch_bounds__(256) void prompt_attn_merge_kernel(PromptArgs a)
+// Few rows (single tokens of a batch): 32 rows, and eight wavefronts that each take every eighth step of 32 keys.  A wavefront shares no K or V tile,
+// so it brings them itself and meets the others only at the end of a piece: no barrier in the walk.
+template <int D>
+__global__ __launch_bounds__(512) void prompt_attn_few_kernel(PromptArgs a)
 {
-    const int splits = a.splits;
-    a.splits = 1;   // of the grid
-    const Place at = find_place<ROWS>(a, blockIdx.x, threadIdx.x & 63);
-    if (!at.any) return;
-    const int pairs = at.n * a.group, here = min(ROWS, pairs - at.first);
-    for (int item = blockIdx.y * 256 + threadIdx.x; item < here * (D / 4); item += 256 * gridDim.y) {
-        const int r = item / (D / 4), d4 = item % (D / 4), p = at.first + r, query = p / a.group;
-        const size_t row = (size_t)at.unit * splits * ROWS + r;
-        float m = kLowest;
-        for (int s = 0; s < splits; ++s) m = fmaxf(m, a.part_ml[2 * (row + (size_t)s * ROWS)]);
-        float den = 0.f;
-        float4v num = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < splits; ++s) {
-            const float ms = a.part_ml[2 * (row + (size_t)s * ROWS)], ls = a.part_ml[2 * (row + (size_t)s * ROWS) + 1];
-            const float w = __builtin_amdgcn_exp2f(ms - m);
-            den += w * ls;
-            num += w * *reinterpret_cast<const float4v *>(a.part_o + (row + (size_t)s * ROWS) * D + 4 * d4);
-        }
-        const float inv = at.T - at.n + query >= 0 ? 1.f / den : 0.f;
-        half4v y;
+    constexpr int ROWS = 32, KEYS = 32, NW = 8;
+    constexpr int ROW = Tile<D>::ROW, CHUNKS = Tile<D>::CHUNKS, TILE = KEYS * ROW, PER = 1024 / ROW, TRANSFERS = TILE / 1024;
+    constexpr int EX_ROW = D * 4 + 16, EX_WAVE = ROWS * EX_ROW;        // after the walk: outputs of a wavefront, rows 16 bytes apart from the banks of the last
+    constexpr int STATE = NW * EX_WAVE;                                // [row][wavefront] (max, sum)
+    constexpr int LDS = STATE + ROWS * NW * 8 > NW * 2 * TILE ? STATE + ROWS * NW * 8 : NW * 2 * TILE;
+    extern __shared__ float4v smem4[];
+    uint8_t *const lds = reinterpret_cast<uint8_t *>(smem4);
+    static_assert(LDS <= 160 * 1024 - 64, "");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int h = lane >> 5, c = lane & 31;
+    const uint32_t kfrag = Tile<D>::k_place(c, h), vfrag = v_fragment<D>(lane);
+    const int trow = lane / CHUNKS, tchunk = lane % CHUNKS;
+    const uint32_t stride = (uint32_t)a.Hkv * ROW;
+    uint8_t *const ktile = lds + wave * 2 * TILE, *const vtile = ktile + TILE;
+
+    go_through<D, ROWS, KEYS, 512, 64 * NW>(a, tid, reinterpret_cast<float *>(lds), [&](const Sequence &s, const Piece &p, bool whole, unsigned slot) {
+        const uint8_t *const k_src = reinterpret_cast<const uint8_t *>(a.k) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
+        const uint8_t *const v_src = reinterpret_cast<const uint8_t *>(a.v) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
+        auto request = [&](int step, const uint8_t *src, uint8_t *tile, bool values) {
+            const int key0 = step * KEYS;
+            const Stretch from = stretch(src + (size_t)key0 * stride, 0x7FFFFFFF);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = (_Float16)(num[e] * inv);
-        *reinterpret_cast<half4v *>(a.out + ((size_t)(at.q0 + query) * a.Hq + at.kvh * a.group + (p - query * a.group)) * D + 4 * d4) = y;
-    }
+            for (int i = 0; i < TRANSFERS; ++i) {
+                const int row = i * PER + trow, chunk = values ? tchunk ^ (2 * row & (CHUNKS - 1)) : tchunk ^ (row & 7);
+                quad_to_lds(from, tile + i * 1024, (uint32_t)min(row, s.T - 1 - key0) * stride + (chunk << 4), 0);   // rows beyond the last key repeat it; they are masked
+            }
+        };
+        Rows<D> rows;
+        rows.start(a, s, p, c, h);
+        __builtin_amdgcn_sched_barrier(0);   // Q before K before V: the waits count on it
+        int step = p.s0 + wave;
+        if (step < p.s1) {
+            request(step, k_src, ktile, false);
+            __builtin_amdgcn_sched_barrier(0);
+            request(step, v_src, vtile, true);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        rows.arrive();
+        const int all_see = s.T - s.n + p.first / a.group + 1;
+        while (step < p.s1) {   // uniform over the wavefront
+            const int next = step + NW;
+            const bool more = next < p.s1;
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TRANSFERS) : "memory");   // K of this step; its V is newer
+            const int key0 = step * KEYS;
+            const bool all = key0 + KEYS <= all_see;
+            float16v sc[1];
+            half8v pb[2];
+            half8v kf[D / 16];
+            rows.read_keys(kf, ktile, kfrag);
+            rows.scores(sc[0], kf);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the K tile has been read
+            if (more) request(next, k_src, ktile, false);
+            if (all) rows.template softmax<1, false>(sc, pb, key0, a.scale_log2e, h);
+            else rows.template softmax<1, true>(sc, pb, key0, a.scale_log2e, h);
+            if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TRANSFERS) : "memory");   // V of this step; the next K is newer
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (all) rows.template values<1, false>(pb, vtile, key0, h, vfrag);
+            else rows.template values<1, true>(pb, vtile, key0, h, vfrag);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the V tile has been read
+            if (more) request(next, v_src, vtile, true);
+            step = next;
+        }
+        // the states of the wavefronts meet in LDS
+        const float l_run = rows.l_run + __shfl_xor(rows.l_run, 32, 64);
+        __syncthreads();   // every wavefront has left its tiles
+        float *const state = reinterpret_cast<float *>(lds + STATE);
+        if (h == 0) {
+            state[(c * NW + wave) * 2] = rows.m_run;
+            state[(c * NW + wave) * 2 + 1] = l_run;
+        }
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4v *>(lds + wave * EX_WAVE + c * EX_ROW + (32 * dt + 8 * g + 4 * h) * 4) =
+                    (float4v){rows.o[dt][4 * g], rows.o[dt][4 * g + 1], rows.o[dt][4 * g + 2], rows.o[dt][4 * g + 3]};
+        __syncthreads();
+        const PartialBuffer po = Pieces<D, ROWS>::o(a, slot), pm = Pieces<D, ROWS>::ml(a, slot);
+        for (int item = tid; item < p.rows * (D / 4); item += 64 * NW) {
+            const int row = item / (D / 4), d4 = item % (D / 4);
+            float m = kLowest, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) m = fmaxf(m, state[(row * NW + w) * 2]);
+            float4v val = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float wgt = __builtin_amdgcn_exp2f(state[(row * NW + w) * 2] - m);
+                l += wgt * state[(row * NW + w) * 2 + 1];
+                val += wgt * *reinterpret_cast<const float4v *>(lds + w * EX_WAVE + row * EX_ROW + d4 * 16);
+            }
+            if (whole) store_row_quad(a, s, p, row, D, 4 * d4, val, l);
+            else {
+                store_partial(po, row * (D / 4) + d4, val);
+                if (d4 == 0) {
+                    store_partial_f32(pm, 2 * row, m);
+                    store_partial_f32(pm, 2 * row + 1, l);
+                }
+            }
+        }
+    });
 }
+template <int D>
+constexpr int few_lds() { return 8 * 32 * (D * 4 + 16) + 32 * 8 * 8 > 8 * 2 * 32 * D * 2 ? 8 * 32 * (D * 4 + 16) + 32 * 8 * 8 : 8 * 2 * 32 * D * 2; }
 
 // ---- host ------------------------------------------------------------------------------------------------------
-constexpr int kTileRows = 256;
+constexpr int kFewRows = 32;
 
 struct PromptPlan {
-    int tiles, splits;
+    bool few, cut;
+    int rows, grid;   // of a tile; workgroups
     size_t o_bytes, ml_bytes;
 };
 
@@ -352,7 +769,8 @@ static int check_prompt_sizes(int rows, int B, int max_q, int max_k, int Hq, int
 {
     if (rows < 1 || B < 1 || max_q < 1 || max_k < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || D < 1) return W4A16_EINVAL;
     if (D != 64 && D != 128) return W4A16_EUNSUP;
-    if (B > kMostSequences || (long long)rows * Hq > (1 << 29) || rows > (1 << 23) || Hkv > 1024 || Hq / Hkv > 64 || max_q > (1 << 23) || max_k > (1 << 30)) return W4A16_EUNSUP;
+    if (B > kMostSequences || (long long)rows * Hq > (1 << 29) || rows > (1 << 23) || Hkv > 1024 || Hq / Hkv > 64 || max_q > (1 << 23) || max_k > (1 << 30))
+        return W4A16_EUNSUP;
     return W4A16_OK;
 }
 
@@ -360,24 +778,39 @@ static PromptPlan prompt_plan(int rows, int B, int max_q, int max_k, int Hq, int
 {
     PromptPlan p;
     const int group = Hq / Hkv;
-    p.tiles = (int)((long long)rows * group / kTileRows) + B;
-    const long long work = (long long)p.tiles * Hkv;
-    // too few tiles for the compute units: their keys are cut, eight steps a range at least
-    p.splits = 1;
-    if (work < 256) p.splits = (int)min(min((512 + work - 1) / work, (long long)(max_k + 8 * kKeyTile - 1) / (8 * kKeyTile)), (long long)kMostSplits);
-    const size_t rows_kept = p.splits > 1 ? (size_t)work * p.splits * kTileRows : 0;
-    p.o_bytes = rows_kept * D * 4;
-    p.ml_bytes = rows_kept * 8;
+    p.few = (long long)max_q * group <= 2 * kFewRows;
+    p.rows = p.few ? kFewRows : kTileRows;
+    const long long tiles = (long long)rows * group / p.rows + B;   // most of a KV head
+    p.cut = p.few || (max_k > 4096 && (long long)rows * group / p.rows * Hkv < 2 * kMostGroups);
+    if (p.cut) {   // no more workgroups than there can be work for, were every sequence as long as the longest
+        p.grid = (int)min(tiles * Hkv * (((long long)max_k + 255) / 256), (long long)kMostGroups);
+        p.o_bytes = (size_t)p.grid * 2 * p.rows * D * 4;
+        p.ml_bytes = (size_t)p.grid * 2 * p.rows * 8;
+    } else {       // whole tiles, as take_one() deals them out
+        p.grid = (int)(8 % Hkv == 0 ? (tiles + 8 / Hkv - 1) / (8 / Hkv) * 8 : tiles * Hkv);
+        p.o_bytes = p.ml_bytes = 0;
+    }
     return p;
 }
 
-// blocks of a grid that find_place() deals out
-static unsigned prompt_grid(int tiles, int splits, int Hkv)
+template <int WHICH, typename Kernel>
+static int launch_with_lds(Kernel kernel, int lds, int threads, const PromptArgs &a, const PromptPlan &p, hipStream_t stream)
 {
-    const unsigned n = (unsigned)tiles * (unsigned)splits;
-    if (Hkv % 8 == 0) return n * (unsigned)Hkv;
-    if (8 % Hkv == 0) return (n + 8u / Hkv - 1) / (8u / Hkv) * 8u;
-    return n * (unsigned)Hkv;
+    static bool ready = false;   // the LDS size is granted once for each of them
+    if (!ready) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return W4A16_EHIP;
+        ready = true;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(threads), lds, stream, a);
+    return launch_status();
+}
+template <int D>
+static int launch_prompt(const PromptArgs &a, const PromptPlan &p, hipStream_t stream)
+{
+    constexpr int tile_lds = kStages * 2 * kTileKeys * D * 2;
+    if (p.few) return launch_with_lds<D>(&prompt_attn_few_kernel<D>, few_lds<D>(), 512, a, p, stream);
+    if (p.cut) return launch_with_lds<D + 1>(&prompt_attn_tile_kernel<D, true>, tile_lds, 512, a, p, stream);
+    return launch_with_lds<D + 2>(&prompt_attn_tile_kernel<D, false>, tile_lds, 512, a, p, stream);
 }
 
 }  // namespace w4
@@ -408,16 +841,8 @@ int w4a16_prompt_attn(const void *q, const void *k, const void *v, const int32_t
     if (workspace_misaligned(workspace)) return W4A16_EALIGN;
     float *const part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + kTicketBytes);
     const PromptArgs a = {(const _Float16 *)q, (const _Float16 *)k, (const _Float16 *)v, q_start, k_start, k_len, (_Float16 *)out, part_o,
-                          part_o + p.o_bytes / 4, B, rows, k_rows, Hq, Hkv, Hq / Hkv, p.tiles, p.splits, scale * 1.44269504088896340736f};
-    const unsigned grid = prompt_grid(p.tiles, p.splits, Hkv);
-    if (D == 128) hipLaunchKernelGGL((prompt_attn_tile_kernel<128, 8, 1>), dim3(grid), dim3(512), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL((prompt_attn_tile_kernel<64, 8, 1>), dim3(grid), dim3(512), 0, (hipStream_t)stream, a);
-    if (p.splits > 1) {
-        const dim3 merge(prompt_grid(p.tiles, 1, Hkv), 8);
-        if (D == 128) hipLaunchKernelGGL((prompt_attn_merge_kernel<128, kTileRows>), merge, dim3(256), 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL((prompt_attn_merge_kernel<64, kTileRows>), merge, dim3(256), 0, (hipStream_t)stream, a);
-    }
-    return launch_status();
+                          part_o + p.o_bytes / 4, (uint32_t *)workspace, B, rows, k_rows, Hq, Hkv, Hq / Hkv, scale * 1.44269504088896340736f};
+    return D == 128 ? launch_prompt<128>(a, p, (hipStream_t)stream) : launch_prompt<64>(a, p, (hipStream_t)stream);
 }
 
 }  // extern "C"
