@@ -160,7 +160,9 @@ struct GemmArgs {
     const float *scale, *w_scale;
     const _Float16 *residual;
     _Float16 *y;
-    int M, N, blocks;
+    float *partials;
+    uint32_t *tickets;
+    int M, N, blocks, splits;
 };
 
 // sums of channels n .. n + 3 of token m become outputs
@@ -177,51 +179,119 @@ __device__ __forceinline__ void finish(const GemmArgs &a, int4v acc, int m, int 
     *reinterpret_cast<half4 *>(a.y + at) = y;
 }
 
-// Many tokens: a workgroup of WM x WN wavefronts takes 16 MT WM tokens by 16 NT WN channels, both operands through LDS in steps of 128 values
-// of k, two buffers.  Tiles lie in operand order already, so a transfer is 1 KB in one piece and fragments are read without bank conflicts.
-template <int WM, int WN, int MT, int NT>
+// More than 16 tokens: a workgroup of WM x WN wavefronts takes 16 MT WM tokens by 16 NT WN channels, a wavefront MT x NT tiles of them, in steps of 128
+// values of k.  The activations, which WN wavefronts read, go through LDS (three buffers: two steps under way); the weights go straight to
+// registers, AHEAD steps ahead: with both operands in LDS its bandwidth was as scarce as the matrix pipe (256 x 256: 2048 clocks a step each).  Tiles lie in
+// operand order already, so a load or transfer is 1 KB in one piece and fragments are read without bank conflicts.
+// Where the tiles are few, `splits` workgroups share the walk along k; the last of them to finish adds the others' sums (whole numbers: in any order)
+// to its own.
+template <int WM, int WN, int MT, int NT, int AHEAD>
 __global__ __launch_bounds__(64 * WM * WN) void w8a8_tile_kernel(GemmArgs a)
 {
-    constexpr int XT = WM * MT, WT = WN * NT, WAVES = WM * WN, STAGE = (XT + WT) * 2048, TRANSFERS = (XT + WT) * 2 / WAVES;
-    static_assert((XT + WT) * 2 % WAVES == 0, "");
+    constexpr int XT = WM * MT, WT = WN * NT, WAVES = WM * WN, STAGE = XT * 2048, TRANSFERS = (XT * 2 + WAVES - 1) / WAVES, STAGES = 3;
+    constexpr int RING = AHEAD + 1, UNROLL = RING % 2 ? 2 * RING : RING;   // in halves of a step
     extern __shared__ u32x4 smem[];
     uint8_t *const lds = reinterpret_cast<uint8_t *>(smem);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int x_tiles = (a.M + 15) / 16, w_tiles = (a.N + 15) / 16;
-    const int col_blocks = (w_tiles + WT - 1) / WT;
-    const int bm = blockIdx.x / col_blocks, bn = blockIdx.x % col_blocks;
-    auto request = [&](int step, uint8_t *stage) {
+    // An XCD gets neighbouring places; bands of eight blocks of tokens, so that workgroups that run together share both operands.
+    const unsigned xcd = blockIdx.x & 7u, grid = gridDim.x;
+    const unsigned number = xcd * (grid >> 3) + min(xcd, grid & 7u) + (blockIdx.x >> 3);
+    const unsigned split = number % (unsigned)a.splits, place = number / (unsigned)a.splits;
+    const unsigned rows = (unsigned)(x_tiles + XT - 1) / XT, cols = (unsigned)(w_tiles + WT - 1) / WT;
+    const unsigned band = place / (8 * cols), in_band = place - band * 8 * cols, high = min(8u, rows - 8 * band);
+    const int bm = (int)(8 * band + in_band % high), bn = (int)(in_band / high);
+    const int all = a.blocks / 2, first = (int)((long long)all * split / a.splits), steps = (int)((long long)all * (split + 1) / a.splits) - first;
+
+    const uint8_t *xs[TRANSFERS];
 #pragma unroll
-        for (int i = 0; i < TRANSFERS; ++i) {
-            const int t = wave * TRANSFERS + i, tile = t >> 1, half = t & 1;   // uniform
-            const uint8_t *src = tile < XT ? a.codes + (size_t)min(bm * XT + tile, x_tiles - 1) * a.blocks * 1024
-                                           : a.packed + (size_t)min(bn * WT + tile - XT, w_tiles - 1) * a.blocks * 1024;
-            quad_to_lds(stretch(src, 0x7FFFFFFF), stage + t * 1024, lane * 16, (2 * step + half) * 1024);
-        }
+    for (int i = 0; i < TRANSFERS; ++i)
+        xs[i] = a.codes + ((size_t)min(bm * XT + (wave * TRANSFERS + i) / 2, x_tiles - 1) * a.blocks + 2 * first + (wave * TRANSFERS + i) % 2) * 1024;
+    auto transfer = [&](int step, int i) {
+        if (step < steps && (XT * 2 % WAVES == 0 || wave * TRANSFERS + i < XT * 2))   // uniform
+            quad_to_lds(stretch(xs[i], 0x7FFFFFFF), lds + step % STAGES * STAGE + (wave * TRANSFERS + i) * 1024, lane * 16, step * 2048);
+    };
+    Stretch ws[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+        ws[j] = stretch(a.packed + ((size_t)min(bn * WT + wn * NT + j, w_tiles - 1) * a.blocks + 2 * first) * 1024, 0x7FFFFFFF);
+    int4v wf[RING][NT];
+    auto fetch = [&](int half, int j) {
+        return __builtin_bit_cast(int4v, __builtin_amdgcn_raw_buffer_load_b128(ws[j], lane * 16, min(half, 2 * steps - 1) * 1024, WM == 1 ? kStreamed : 0));
     };
     int4v acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
-    const int steps = a.blocks / 2;
-    request(0, lds);
-    for (int step = 0; step < steps; ++step) {
-        const uint8_t *const stage = lds + (step & 1) * STAGE;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this step has landed, the other buffer has been read
-        if (step + 1 < steps) request(step + 1, lds + ((step + 1) & 1) * STAGE);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            int4v xf[MT], wf[NT];
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int i = 0; i < MT; ++i) xf[i] = *reinterpret_cast<const int4v *>(stage + ((wm * MT + i) * 2 + half) * 1024 + lane * 16);
+        for (int i = 0; i < TRANSFERS; ++i) transfer(s, i);
+    __builtin_amdgcn_sched_barrier(0);   // the waits below count on this order
 #pragma unroll
-            for (int j = 0; j < NT; ++j) wf[j] = *reinterpret_cast<const int4v *>(stage + ((XT + wn * NT + j) * 2 + half) * 1024 + lane * 16);
+    for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) wf[u][j] = fetch(u, j);
+    for (int step0 = 0; step0 < steps; step0 += UNROLL / 2) {
+#pragma unroll
+        for (int u = 0; u < UNROLL; u += 2) {
+            const int step = step0 + u / 2;
+            if (step >= steps) break;   // uniform
+            // This step's activations have landed and the step before this one has been read.  Newer than they are the weights asked for in three
+            // halves and the next step's activations (which are not there behind the last).
+            if (step + 1 < steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(TRANSFERS + NT * (AHEAD > 2 ? 3 : AHEAD)) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            const uint8_t *const stage = lds + step % STAGES * STAGE;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                int4v xf[MT];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) xf[i] = *reinterpret_cast<const int4v *>(stage + ((wm * MT + i) * 2 + half) * 1024 + lane * 16);
+                // Loads go out between the products: a compute unit takes 64 bytes a clock, and a wavefront that asks for all at once stands still meanwhile.
+                // Activations first (the wait above counts on it).
+                constexpr int HERE = (TRANSFERS + 1) / 2, LOADS = HERE + NT, GAP = MT * NT / LOADS > 0 ? MT * NT / LOADS : 1;
+                auto load = [&](int n) {
+                    if (n < HERE) {
+                        if (half * HERE + n < TRANSFERS) transfer(step + 2, half * HERE + n);
+                    } else if (n < LOADS) wf[(u + half + AHEAD) % RING][n - HERE] = fetch(2 * step + half + AHEAD, n - HERE);
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        const int at = i * NT + j;
+                        if (at % GAP == 0 && at / GAP < LOADS) load(at / GAP);
+                        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[(u + half) % RING][j], xf[i], acc[i][j], 0, 0, 0);
+                    }
+#pragma unroll
+                for (int n = (MT * NT + GAP - 1) / GAP; n < LOADS; ++n) load(n);
+            }
+        }
+    }
+    if (a.splits > 1) {
+        constexpr int QUADS = WAVES * MT * NT * 64;   // of a workgroup's sums
+        const PartialBuffer mine = partial_buffer(a.partials + ((size_t)place * a.splits + split) * QUADS * 4);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) store_partial(mine, ((wave * MT + i) * NT + j) * 64 + lane, __builtin_bit_cast(float4v, acc[i][j]));
+        uint32_t *const ticket_sh = reinterpret_cast<uint32_t *>(lds);   // exchange as in the linears of 4 bits
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) *ticket_sh = __hip_atomic_fetch_add(&a.tickets[place], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (*ticket_sh != (uint32_t)(a.splits - 1)) return;
+        if (threadIdx.x == 0) __hip_atomic_store(&a.tickets[place], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (unsigned s = 0; s < (unsigned)a.splits; ++s) {
+            if (s == split) continue;
+            const PartialBuffer other = partial_buffer(a.partials + ((size_t)place * a.splits + s) * QUADS * 4);
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[j], xf[i], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < NT; ++j) acc[i][j] += __builtin_bit_cast(int4v, load_partial(other, ((wave * MT + i) * NT + j) * 64 + lane));
         }
     }
 #pragma unroll
@@ -332,31 +402,59 @@ static int launch_quantize(const void *x, int pre, const void *gamma, float eps,
     return launch_status();
 }
 
-template <int WM, int WN, int MT, int NT>
-static int launch_tile(const GemmArgs &a, hipStream_t stream)
+// How a product is cut: the kernel, its tile and the number of workgroups that share a tile's walk along k.
+struct GemmPlan {
+    int kind;   // 0: w8a8_stream_kernel; else the tile kernels below
+    int rows, cols, splits;
+};
+
+template <int WM, int WN, int MT, int NT, int AHEAD>
+static int launch_tile(GemmArgs a, const GemmPlan &p, hipStream_t stream)
 {
-    constexpr int lds = (WM * MT + WN * NT) * 4096;
+    constexpr int lds = WM * MT * 2048 * 3;
     static bool ready = false;   // the LDS size is granted once
     if (!ready) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void *>(&w8a8_tile_kernel<WM, WN, MT, NT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(&w8a8_tile_kernel<WM, WN, MT, NT, AHEAD>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
             return W4A16_EHIP;
         ready = true;
     }
-    const unsigned rows = (unsigned)((a.M + 16 * MT * WM - 1) / (16 * MT * WM)), cols = (unsigned)((a.N + 16 * NT * WN - 1) / (16 * NT * WN));
-    if ((unsigned long long)rows * cols > (1u << 22)) return W4A16_EUNSUP;
-    hipLaunchKernelGGL((w8a8_tile_kernel<WM, WN, MT, NT>), dim3(rows * cols), dim3(64 * WM * WN), lds, stream, a);
+    a.splits = p.splits;
+    const unsigned grid = (unsigned)((a.M + p.rows - 1) / p.rows) * (unsigned)((a.N + p.cols - 1) / p.cols) * (unsigned)p.splits;
+    hipLaunchKernelGGL((w8a8_tile_kernel<WM, WN, MT, NT, AHEAD>), dim3(grid), dim3(64 * WM * WN), lds, stream, a);
     return launch_status();
 }
 
-static int launch_gemm(const GemmArgs &a, hipStream_t stream)
+static GemmPlan gemm_plan(int M, int N, int K)
 {
-    const unsigned tiles = (unsigned)(a.N + 15) / 16;
-    if (a.M <= 16) hipLaunchKernelGGL((w8a8_stream_kernel<1, 1>), dim3(tiles), dim3(512), 0, stream, a);
-    else if (a.M <= 32) hipLaunchKernelGGL((w8a8_stream_kernel<2, 1>), dim3(tiles), dim3(512), 0, stream, a);
-    else if (a.M <= 64) hipLaunchKernelGGL((w8a8_stream_kernel<4, 1>), dim3(tiles), dim3(512), 0, stream, a);
-    else if ((long long)((a.M + 255) / 256) * ((a.N + 255) / 256) >= 256) return launch_tile<2, 4, 8, 4>(a, stream);
-    else return launch_tile<2, 2, 4, 4>(a, stream);
-    return launch_status();
+    GemmPlan p = {0, 0, 0, 1};
+    if (M <= 16) return p;
+    const int steps = k_blocks(K) / 2;
+    auto tiles = [&](int rows, int cols) { return (long long)((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
+    if (M <= 32) p.kind = 1, p.rows = 32, p.cols = 128;
+    else if (M <= 64) p.kind = 2, p.rows = 64, p.cols = 128;
+    else if (M <= 128) p.kind = 3, p.rows = 128, p.cols = 256;
+    else if (tiles(256, 256) >= 192) p.kind = 5, p.rows = 256, p.cols = 256;
+    else p.kind = 4, p.rows = 128, p.cols = 256;
+    const long long n = tiles(p.rows, p.cols);
+    if (n < 256 && p.kind < 5) p.splits = (int)max(1ll, min(min(256 / n, (long long)steps / 4), 16ll));
+    return p;
+}
+
+// of any number of tokens up to M: tiles times splits are 256 at most where a walk is split
+static size_t most_partials(int M) { return M <= 16 ? 0 : (size_t)256 * 4 * (M <= 32 ? 32 * 128 : M <= 64 ? 64 * 128 : 128 * 256); }
+
+static int launch_gemm(const GemmArgs &a, const GemmPlan &p, hipStream_t stream)
+{
+    switch (p.kind) {
+    case 0:
+        hipLaunchKernelGGL((w8a8_stream_kernel<1, 1>), dim3((unsigned)(a.N + 15) / 16), dim3(512), 0, stream, a);
+        return launch_status();
+    case 1: return launch_tile<1, 8, 2, 1, 13>(a, p, stream);
+    case 2: return launch_tile<1, 8, 4, 1, 13>(a, p, stream);
+    case 3: return launch_tile<1, 8, 8, 2, 7>(a, p, stream);
+    case 4: return launch_tile<2, 4, 4, 4, 3>(a, p, stream);
+    default: return launch_tile<2, 4, 8, 4, 2>(a, p, stream);
+    }
 }
 
 static int check_gemm(const void *packed, const float *w_scale, const void *residual, const void *y)
@@ -413,7 +511,7 @@ int w8a8_quantize(const void *x, int pre, const void *gamma, float eps, void *co
 size_t w8a8_workspace_bytes(int M, int N, int K)
 {
     if (check_gemm_shape(M, N, K) != W4A16_OK) return 0;
-    return kTicketBytes + codes_bytes(M, K) + aligned256((size_t)M * 4);
+    return kTicketBytes + codes_bytes(M, K) + aligned256((size_t)M * 4) + most_partials(M);
 }
 
 int w8a8_gemm(const void *codes, const float *scale, const void *packed, const float *w_scale, const void *residual, void *y, int M, int N, int K,
@@ -427,8 +525,10 @@ int w8a8_gemm(const void *codes, const float *scale, const void *packed, const f
     if (misaligned(codes) || misaligned(scale)) return W4A16_EALIGN;
     if (!workspace || workspace_bytes < w8a8_workspace_bytes(M, N, K)) return W4A16_EWORKSPACE;
     if (workspace_misaligned(workspace)) return W4A16_EALIGN;
-    const GemmArgs a = {(const uint8_t *)codes, (const uint8_t *)packed, scale, w_scale, (const _Float16 *)residual, (_Float16 *)y, M, N, k_blocks(K)};
-    return launch_gemm(a, (hipStream_t)stream);
+    uint8_t *const partials = static_cast<uint8_t *>(workspace) + kTicketBytes + codes_bytes(M, K) + aligned256((size_t)M * 4);
+    const GemmArgs a = {(const uint8_t *)codes, (const uint8_t *)packed, scale, w_scale, (const _Float16 *)residual, (_Float16 *)y,
+                        (float *)partials, (uint32_t *)workspace, M, N, k_blocks(K), 1};
+    return launch_gemm(a, gemm_plan(M, N, K), (hipStream_t)stream);
 }
 
 int w8a8_linear(const void *x, int pre, const void *gamma, float eps, const void *packed, const float *w_scale, const void *residual, void *y, int M,
@@ -446,8 +546,9 @@ int w8a8_linear(const void *x, int pre, const void *gamma, float eps, const void
     float *const scale = reinterpret_cast<float *>(codes + codes_bytes(M, K));
     rc = launch_quantize(x, pre, gamma, eps, codes, scale, M, K, (hipStream_t)stream);
     if (rc != W4A16_OK) return rc;
-    const GemmArgs a = {codes, (const uint8_t *)packed, scale, w_scale, (const _Float16 *)residual, (_Float16 *)y, M, N, k_blocks(K)};
-    return launch_gemm(a, (hipStream_t)stream);
+    const GemmArgs a = {codes, (const uint8_t *)packed, scale, w_scale, (const _Float16 *)residual, (_Float16 *)y,
+                        reinterpret_cast<float *>(codes + codes_bytes(M, K) + aligned256((size_t)M * 4)), (uint32_t *)workspace, M, N, k_blocks(K), 1};
+    return launch_gemm(a, gemm_plan(M, N, K), (hipStream_t)stream);
 }
 
 }  // extern "C"
