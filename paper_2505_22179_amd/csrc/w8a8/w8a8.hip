@@ -56,11 +56,14 @@ __device__ __forceinline__ int nearest_code(float x, float s, float inv)
 // One workgroup of T threads per token; a thread keeps PER chunks of sixteen values in registers: one pass over the input.
 template <int PRE, int T, int PER>
 __global__ __launch_bounds__(T) void w8a8_quantize_kernel(const _Float16 *__restrict__ x, const _Float16 *__restrict__ gamma, float eps,
-                                                          uint8_t *__restrict__ codes, float *__restrict__ scale, int K, int blocks)
+                                                          uint8_t *__restrict__ codes, float *__restrict__ scale, int M, int K, int blocks)
 {
     __shared__ float sums[T / 64];
     __shared__ uint32_t tops[T / 64];
-    const int m = blockIdx.x, chunks = K / 16;
+    // The sixteen tokens of a tile share the cache lines of its codes: workgroups go to the eight XCDs in turn, and a tile's go to one, whose L2
+    // puts the lines together (8192 tokens of 4096: 33 us in the order of launch)
+    const int m = (int)(((blockIdx.x >> 7) * 8 + (blockIdx.x & 7)) * 16 + ((blockIdx.x >> 3) & 15)), chunks = K / 16;
+    if (m >= M) return;
     const _Float16 *const row = x + (size_t)m * K * (PRE == W8A8_SILU_MUL ? 2 : 1);
     half8 v[PER][2];
 #pragma unroll
@@ -383,9 +386,10 @@ static int check_quantize(const void *x, int pre, const void *gamma, float eps, 
 static int launch_quantize(const void *x, int pre, const void *gamma, float eps, void *codes, float *scale, int M, int K, hipStream_t stream)
 {
     const int blocks = k_blocks(K), chunks = blocks * 4;
+    const unsigned grid = M <= 16 ? 1u + 8u * (unsigned)(M - 1) : ((unsigned)M + 127u) / 128u * 128u;   // one tile: its tokens are those at 8 m
 #define W8_QUANTIZE(P_, T_, N_)                                                                                                                 \
-    hipLaunchKernelGGL((w8a8_quantize_kernel<P_, T_, N_>), dim3((unsigned)M), dim3(T_), 0, stream, (const _Float16 *)x, (const _Float16 *)gamma, eps, \
-                       (uint8_t *)codes, scale, K, blocks)
+    hipLaunchKernelGGL((w8a8_quantize_kernel<P_, T_, N_>), dim3(grid), dim3(T_), 0, stream, (const _Float16 *)x, (const _Float16 *)gamma, eps, \
+                       (uint8_t *)codes, scale, M, K, blocks)
 #define W8_QUANTIZE_PRE(P_)                              \
     do {                                                 \
         if (chunks <= 256) W8_QUANTIZE(P_, 256, 1);      \
@@ -404,8 +408,7 @@ static int launch_quantize(const void *x, int pre, const void *gamma, float eps,
 
 // How a product is cut: the kernel, its tile and the number of workgroups that share a tile's walk along k.
 struct GemmPlan {
-    int kind;   // 0: w8a8_stream_kernel; else the tile kernels below
-    int rows, cols, splits;
+    int kind, rows, cols, splits;
 };
 
 template <int WM, int WN, int MT, int NT, int AHEAD>
@@ -424,37 +427,58 @@ static int launch_tile(GemmArgs a, const GemmPlan &p, hipStream_t stream)
     return launch_status();
 }
 
+// The kernels, by measurement over 28 shapes (M 1 .. 4096, N 1024 .. 28672, K 4096 .. 14336), us:
+//   up to 16 tokens, and up to 64 where k is short, the stream kernel: 60 tokens 4096 -> 4096 8.6 (tiles of 64 x 128, walk shared by four, 13.6), 8192 -> 8192 18.5
+//   (22.1); with many channels or a long k its wavefronts' own copies of the activations cost more than an exchange: 60 tokens 4096 -> 28672 30.8 (24.7),
+//   14336 -> 4096 21.9 (19.6).  Two tiles of channels to a wavefront where that still fills the chip: 60 tokens 8192 -> 8192 21.9 with one
+//   up to 128 tokens tiles of 64 x 128 with a shared walk unless 128 x 128 fill the chip: 100 tokens 4096 -> 4096 12.5 (13.8)
+//   more: of 256 x 256, 128 x 256 and 128 x 128 the one that takes the shortest time by its rounds over 256 compute units, a step of 128 values of k in
+//   1.66, 1.02 and 0.54 us: 4096 tokens 4096 -> 4096 59, 74 and 74; 777 tokens 8192 -> 8192 73, 61 and 74; 1024 tokens 4096 -> 4096 -, 29 and 23
+enum { kStream = 0, kTile64x128, kTile128x128, kTile128x256, kTile256x256 };
+
 static GemmPlan gemm_plan(int M, int N, int K)
 {
-    GemmPlan p = {0, 0, 0, 1};
-    if (M <= 16) return p;
-    const int steps = k_blocks(K) / 2;
+    const long long steps = k_blocks(K) / 2;
     auto tiles = [&](int rows, int cols) { return (long long)((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
-    if (M <= 32) p.kind = 1, p.rows = 32, p.cols = 128;
-    else if (M <= 64) p.kind = 2, p.rows = 64, p.cols = 128;
-    else if (M <= 128) p.kind = 3, p.rows = 128, p.cols = 256;
-    else if (tiles(256, 256) >= 192) p.kind = 5, p.rows = 256, p.cols = 256;
-    else p.kind = 4, p.rows = 128, p.cols = 256;
-    const long long n = tiles(p.rows, p.cols);
-    if (n < 256 && p.kind < 5) p.splits = (int)max(1ll, min(min(256 / n, (long long)steps / 4), 16ll));
-    return p;
+    auto shared = [&](int kind, int rows, int cols) {   // the walks shared by as many workgroups as fill the chip, four steps each at least
+        const long long n = tiles(rows, cols);
+        return GemmPlan{kind, rows, cols, n < 256 ? (int)max(1ll, min(min(256 / n, steps / 4), 16ll)) : 1};
+    };
+    if (M <= 16 || (M <= 64 && K <= 8192 && tiles(64, 128) < 192)) return {kStream, 16 * (M <= 16 ? 1 : M <= 32 ? 2 : 4), M > 16 && N >= 6144 ? 32 : 16, 1};
+    if (M <= 64 || (M <= 128 && tiles(128, 128) < 160)) return shared(kTile64x128, 64, 128);
+    const GemmPlan whole[3] = {{kTile256x256, 256, 256, 1}, {kTile128x256, 128, 256, 1}, {kTile128x128, 128, 128, 1}};
+    const int step_ns[3] = {1660, 1020, 540};
+    GemmPlan best = shared(kTile128x128, 128, 128);
+    long long least = best.splits > 1 ? (steps + best.splits - 1) / best.splits * step_ns[2] + 6000 : 1ll << 62;   // the exchange takes 6 us
+    for (int i = 0; i < 3; ++i) {
+        const long long ns = (tiles(whole[i].rows, whole[i].cols) + 255) / 256 * steps * step_ns[i];
+        if (ns < least) least = ns, best = whole[i];
+    }
+    return best;
 }
 
 // of any number of tokens up to M: tiles times splits are 256 at most where a walk is split
-static size_t most_partials(int M) { return M <= 16 ? 0 : (size_t)256 * 4 * (M <= 32 ? 32 * 128 : M <= 64 ? 64 * 128 : 128 * 256); }
+static size_t most_partials(int M) { return M <= 16 ? 0 : (size_t)256 * 4 * (M <= 64 ? 64 * 128 : 128 * 128); }
 
 static int launch_gemm(const GemmArgs &a, const GemmPlan &p, hipStream_t stream)
 {
+#define W8_STREAM(MT_, TW_) \
+    hipLaunchKernelGGL((w8a8_stream_kernel<MT_, TW_>), dim3((unsigned)((a.N + 16 * TW_ - 1) / (16 * TW_))), dim3(512), 0, stream, a)
     switch (p.kind) {
-    case 0:
-        hipLaunchKernelGGL((w8a8_stream_kernel<1, 1>), dim3((unsigned)(a.N + 15) / 16), dim3(512), 0, stream, a);
+    case kStream:
+        if (p.rows == 16) W8_STREAM(1, 1);
+        else if (p.rows == 32) {
+            if (p.cols == 16) W8_STREAM(2, 1);
+            else W8_STREAM(2, 2);
+        } else if (p.cols == 16) W8_STREAM(4, 1);
+        else W8_STREAM(4, 2);
         return launch_status();
-    case 1: return launch_tile<1, 8, 2, 1, 13>(a, p, stream);
-    case 2: return launch_tile<1, 8, 4, 1, 13>(a, p, stream);
-    case 3: return launch_tile<1, 8, 8, 2, 7>(a, p, stream);
-    case 4: return launch_tile<2, 4, 4, 4, 3>(a, p, stream);
+    case kTile64x128: return launch_tile<1, 8, 4, 1, 13>(a, p, stream);
+    case kTile128x128: return launch_tile<2, 4, 4, 2, 7>(a, p, stream);
+    case kTile128x256: return launch_tile<1, 8, 8, 2, 7>(a, p, stream);
     default: return launch_tile<2, 4, 8, 4, 2>(a, p, stream);
     }
+#undef W8_STREAM
 }
 
 static int check_gemm(const void *packed, const float *w_scale, const void *residual, const void *y)
