@@ -53,24 +53,20 @@ __device__ __forceinline__ int nearest_code(float x, float s, float inv)
     return (int)n;
 }
 
-// One workgroup of T threads per token; a thread keeps PER chunks of sixteen values in registers: one pass over the input.
-template <int PRE, int T, int PER>
-__global__ __launch_bounds__(T) void w8a8_quantize_kernel(const _Float16 *__restrict__ x, const _Float16 *__restrict__ gamma, float eps,
-                                                          uint8_t *__restrict__ codes, float *__restrict__ scale, int M, int K, int blocks)
+// One token by the first T threads of a workgroup; a thread keeps PER chunks of sixteen values in registers: one pass over the input.
+// store(chunk, codes) receives the chunks, those of the padding too (zeros).  Returns the scale (in the first T threads).  Two barriers, for all threads.
+template <int PRE, int T, int PER, typename Store>
+__device__ __forceinline__ float quantize_row(const _Float16 *__restrict__ row, const _Float16 *__restrict__ gamma, float eps, int K, int padded,
+                                              int tid, float *sums, uint32_t *tops, Store store)
 {
-    __shared__ float sums[T / 64];
-    __shared__ uint32_t tops[T / 64];
-    // The sixteen tokens of a tile share the cache lines of its codes: workgroups go to the eight XCDs in turn, and a tile's go to one, whose L2
-    // puts the lines together (8192 tokens of 4096: 33 us in the order of launch)
-    const int m = (int)(((blockIdx.x >> 7) * 8 + (blockIdx.x & 7)) * 16 + ((blockIdx.x >> 3) & 15)), chunks = K / 16;
-    if (m >= M) return;
-    const _Float16 *const row = x + (size_t)m * K * (PRE == W8A8_SILU_MUL ? 2 : 1);
+    const int chunks = K / 16;
+    const bool works = tid < T;
     half8 v[PER][2];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int ch = threadIdx.x + i * T;
+        const int ch = tid + i * T;
         v[i][0] = v[i][1] = (half8)(_Float16)0;
-        if (ch < chunks) {
+        if (works && ch < chunks) {
             v[i][0] = *reinterpret_cast<const half8 *>(row + ch * 16);
             v[i][1] = *reinterpret_cast<const half8 *>(row + ch * 16 + 8);
         }
@@ -78,8 +74,8 @@ __global__ __launch_bounds__(T) void w8a8_quantize_kernel(const _Float16 *__rest
     if constexpr (PRE == W8A8_SILU_MUL) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int ch = threadIdx.x + i * T;
-            if (ch < chunks) {
+            const int ch = tid + i * T;
+            if (works && ch < chunks) {
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
                     const half8 up = *reinterpret_cast<const half8 *>(row + K + ch * 16 + 8 * p);
@@ -101,7 +97,7 @@ __global__ __launch_bounds__(T) void w8a8_quantize_kernel(const _Float16 *__rest
                 for (int e = 0; e < 8; ++e) ss = __builtin_fmaf((float)v[i][p][e], (float)v[i][p][e], ss);
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) ss += __shfl_xor(ss, off, 64);
-        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = ss;
+        if (works && (tid & 63) == 0) sums[tid >> 6] = ss;
         __syncthreads();
         ss = 0.f;
 #pragma unroll
@@ -109,8 +105,8 @@ __global__ __launch_bounds__(T) void w8a8_quantize_kernel(const _Float16 *__rest
         const float inv = 1.f / sqrtf(ss / (float)K + eps);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int ch = threadIdx.x + i * T;
-            if (ch < chunks) {
+            const int ch = tid + i * T;
+            if (works && ch < chunks) {
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
                     const half8 g = *reinterpret_cast<const half8 *>(gamma + ch * 16 + 8 * p);
@@ -132,7 +128,7 @@ __global__ __launch_bounds__(T) void w8a8_quantize_kernel(const _Float16 *__rest
         }
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, 64));
-    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    if (works && (tid & 63) == 0) tops[tid >> 6] = top;
     __syncthreads();
     top = 0;
 #pragma unroll
@@ -140,11 +136,10 @@ __global__ __launch_bounds__(T) void w8a8_quantize_kernel(const _Float16 *__rest
     const bool finite = top < 0x7C00u, some = finite && top > 0;
     const float s = (float)__builtin_bit_cast(_Float16, (uint16_t)top) / 127.f;   // 0 for a row of zeros
     const float inv = some ? 1.f / s : 0.f;
-    if (threadIdx.x == 0) scale[m] = finite ? s : __builtin_nanf("");
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int ch = threadIdx.x + i * T;
-        if (ch < blocks * 4) {   // chunks of the padding hold zeros
+        const int ch = tid + i * T;
+        if (works && ch < padded) {
             u32x4 packed = {};
             if (some) {
 #pragma unroll
@@ -152,9 +147,25 @@ __global__ __launch_bounds__(T) void w8a8_quantize_kernel(const _Float16 *__rest
 #pragma unroll
                     for (int e = 0; e < 8; ++e) packed[2 * p + (e >> 2)] |= (uint32_t)(nearest_code((float)v[i][p][e], s, inv) & 0xFF) << (8 * (e & 3));
             }
-            *reinterpret_cast<u32x4 *>(codes + chunk_offset(m, ch, blocks)) = packed;
+            store(ch, packed);
         }
     }
+    return finite ? s : __builtin_nanf("");
+}
+
+template <int PRE, int T, int PER>
+__global__ __launch_bounds__(T) void w8a8_quantize_kernel(const _Float16 *__restrict__ x, const _Float16 *__restrict__ gamma, float eps,
+                                                          uint8_t *__restrict__ codes, float *__restrict__ scale, int M, int K, int blocks)
+{
+    __shared__ float sums[T / 64];
+    __shared__ uint32_t tops[T / 64];
+    // The sixteen tokens of a tile share the cache lines of its codes: workgroups go to the eight XCDs in turn, and a tile's go to one, whose L2
+    // puts the lines together (8192 tokens of 8192: 67 us in the order of launch, 34 like this)
+    const int m = (int)(((blockIdx.x >> 7) * 8 + (blockIdx.x & 7)) * 16 + ((blockIdx.x >> 3) & 15));
+    if (m >= M) return;
+    const float s = quantize_row<PRE, T, PER>(x + (size_t)m * K * (PRE == W8A8_SILU_MUL ? 2 : 1), gamma, eps, K, blocks * 4, threadIdx.x, sums, tops,
+                                              [&](int chunk, u32x4 packed) { *reinterpret_cast<u32x4 *>(codes + chunk_offset(m, chunk, blocks)) = packed; });
+    if (threadIdx.x == 0) scale[m] = s;
 }
 
 // ---- products ------------------------------------------------------------------------------------------------
@@ -166,13 +177,17 @@ struct GemmArgs {
     float *partials;
     uint32_t *tickets;
     int M, N, blocks, splits;
+    // of a kernel that quantises by itself
+    const _Float16 *x, *gamma;
+    float eps;
+    int K;
 };
 
 // sums of channels n .. n + 3 of token m become outputs
-__device__ __forceinline__ void finish(const GemmArgs &a, int4v acc, int m, int n)
+__device__ __forceinline__ void finish(const GemmArgs &a, const float *scale, int4v acc, int m, int n)
 {
     if (m >= a.M || n >= a.N) return;   // N is a multiple of eight: four channels are all there or none
-    const float s = a.scale[m];
+    const float s = scale[m];
     const float4v t = *reinterpret_cast<const float4v *>(a.w_scale + n);
     const size_t at = (size_t)m * a.N + n;
     half4 r = {}, y;
@@ -301,15 +316,22 @@ __global__ __launch_bounds__(64 * WM * WN) void w8a8_tile_kernel(GemmArgs a)
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j)
-            finish(a, acc[i][j], (bm * XT + wm * MT + i) * 16 + (lane & 15), (bn * WT + wn * NT + j) * 16 + 4 * (lane >> 4));
+            finish(a, a.scale, acc[i][j], (bm * XT + wm * MT + i) * 16 + (lane & 15), (bn * WT + wn * NT + j) * 16 + 4 * (lane >> 4));
 }
 
 // Few tokens, bound by the weights: eight wavefronts share TW tiles of channels and take every eighth tile of k; weights go straight to registers.
-template <int MT, int TW>
+// FUSED: one token of up to kFusedK values, quantised by every workgroup for itself into LDS while its first weights are on the way: a launch less, in the
+// other kernel's arrangement and so with its bits.  A normed token 4096 -> 28672 25.1 -> 22.1 us, 4096 -> 6144 10.9 -> 8.1.  Longer rows or more
+// tokens cost every workgroup more than the launch: 8192 -> 57344 82 -> 84, two tokens 4096 -> 28672 25 -> 29.
+constexpr int kFusedK = 4096;
+template <int MT, int TW, int PRE = W8A8_PLAIN, bool FUSED = false>
 __global__ __launch_bounds__(512) void w8a8_stream_kernel(GemmArgs a)
 {
     constexpr int AHEAD = 4;
     __shared__ int4v sums[8][MT * TW][64];
+    __shared__ u32x4 row_codes[FUSED ? kFusedK / 16 : 1];
+    __shared__ float row_scale, norm_sums[4];
+    __shared__ uint32_t tops[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int x_tiles = (a.M + 15) / 16, w_tiles = (a.N + 15) / 16, tile0 = blockIdx.x * TW;
     int4v acc[MT][TW];
@@ -322,15 +344,33 @@ __global__ __launch_bounds__(512) void w8a8_stream_kernel(GemmArgs a)
     for (int i = 0; i < MT; ++i) xs[i] = a.codes + (size_t)min(i, x_tiles - 1) * a.blocks * 1024 + lane * 16;
 #pragma unroll
     for (int j = 0; j < TW; ++j) ws[j] = a.packed + (size_t)min(tile0 + j, w_tiles - 1) * a.blocks * 1024 + lane * 16;
+    auto weights = [&](int4v (&wf)[AHEAD][TW], int b) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int j = 0; j < TW; ++j)
+                wf[u][j] = __builtin_nontemporal_load(reinterpret_cast<const int4v *>(ws[j] + (size_t)min(b + 8 * u, a.blocks - 1) * 1024));
+    };
+    int4v wf[AHEAD][TW];
+    if constexpr (FUSED) {
+        weights(wf, wave);
+        __builtin_amdgcn_sched_barrier(0);
+        const float s = quantize_row<PRE, 256, 1>(a.x, a.gamma, a.eps, a.K, a.blocks * 4, threadIdx.x, norm_sums, tops,
+                                                  [&](int chunk, u32x4 packed) { row_codes[chunk] = packed; });
+        if (threadIdx.x == 0) row_scale = s;
+        __syncthreads();
+    }
     for (int b = wave; b < a.blocks; b += 8 * AHEAD) {
-        int4v xf[AHEAD][MT], wf[AHEAD][TW];
+        int4v xf[AHEAD][MT];
+        if (!FUSED || b != wave) weights(wf, b);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const size_t at = (size_t)min(b + 8 * u, a.blocks - 1) * 1024;
+            const int at = min(b + 8 * u, a.blocks - 1);
 #pragma unroll
-            for (int j = 0; j < TW; ++j) wf[u][j] = __builtin_nontemporal_load(reinterpret_cast<const int4v *>(ws[j] + at));
-#pragma unroll
-            for (int i = 0; i < MT; ++i) xf[u][i] = *reinterpret_cast<const int4v *>(xs[i] + at);
+            for (int i = 0; i < MT; ++i) {
+                if constexpr (FUSED) xf[u][i] = __builtin_bit_cast(int4v, row_codes[at * 4 + (lane >> 4)]);   // the token's, for all sixteen rows
+                else xf[u][i] = *reinterpret_cast<const int4v *>(xs[i] + (size_t)at * 1024);
+            }
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
@@ -351,7 +391,7 @@ __global__ __launch_bounds__(512) void w8a8_stream_kernel(GemmArgs a)
         int4v all = sums[0][t][lane];
 #pragma unroll
         for (int w = 1; w < 8; ++w) all += sums[w][t][lane];
-        finish(a, all, t / TW * 16 + (lane & 15), (tile0 + t % TW) * 16 + 4 * (lane >> 4));
+        finish(a, FUSED ? &row_scale : a.scale, all, t / TW * 16 + (lane & 15), (tile0 + t % TW) * 16 + 4 * (lane >> 4));
     }
 }
 
@@ -551,7 +591,7 @@ int w8a8_gemm(const void *codes, const float *scale, const void *packed, const f
     if (workspace_misaligned(workspace)) return W4A16_EALIGN;
     uint8_t *const partials = static_cast<uint8_t *>(workspace) + kTicketBytes + codes_bytes(M, K) + aligned256((size_t)M * 4);
     const GemmArgs a = {(const uint8_t *)codes, (const uint8_t *)packed, scale, w_scale, (const _Float16 *)residual, (_Float16 *)y,
-                        (float *)partials, (uint32_t *)workspace, M, N, k_blocks(K), 1};
+                        (float *)partials, (uint32_t *)workspace, M, N, k_blocks(K), 1, nullptr, nullptr, 0.f, K};
     return launch_gemm(a, gemm_plan(M, N, K), (hipStream_t)stream);
 }
 
@@ -568,11 +608,18 @@ int w8a8_linear(const void *x, int pre, const void *gamma, float eps, const void
     if (workspace_misaligned(workspace)) return W4A16_EALIGN;
     uint8_t *const codes = static_cast<uint8_t *>(workspace) + kTicketBytes;
     float *const scale = reinterpret_cast<float *>(codes + codes_bytes(M, K));
-    rc = launch_quantize(x, pre, gamma, eps, codes, scale, M, K, (hipStream_t)stream);
-    if (rc != W4A16_OK) return rc;
     const GemmArgs a = {codes, (const uint8_t *)packed, scale, w_scale, (const _Float16 *)residual, (_Float16 *)y,
-                        reinterpret_cast<float *>(codes + codes_bytes(M, K) + aligned256((size_t)M * 4)), (uint32_t *)workspace, M, N, k_blocks(K), 1};
-    return launch_gemm(a, gemm_plan(M, N, K), (hipStream_t)stream);
+                        reinterpret_cast<float *>(codes + codes_bytes(M, K) + aligned256((size_t)M * 4)), (uint32_t *)workspace, M, N, k_blocks(K), 1,
+                        (const _Float16 *)x, (const _Float16 *)gamma, eps, K};
+    if (M == 1 && K <= kFusedK) {
+        auto *const kernel = pre == W8A8_PLAIN      ? &w8a8_stream_kernel<1, 1, W8A8_PLAIN, true>
+                             : pre == W8A8_RMS_NORM ? &w8a8_stream_kernel<1, 1, W8A8_RMS_NORM, true>
+                                                    : &w8a8_stream_kernel<1, 1, W8A8_SILU_MUL, true>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((N + 15) / 16)), dim3(512), 0, (hipStream_t)stream, a);
+        return launch_status();
+    }
+    rc = launch_quantize(x, pre, gamma, eps, codes, scale, M, K, (hipStream_t)stream);
+    return rc != W4A16_OK ? rc : launch_gemm(a, gemm_plan(M, N, K), (hipStream_t)stream);
 }
 
 }  // extern "C"
