@@ -433,8 +433,8 @@ static int launch_quantize(const void *x, int pre, const void *gamma, float eps,
 #define W8_QUANTIZE_PRE(P_)                              \
     do {                                                 \
         if (chunks <= 256) W8_QUANTIZE(P_, 256, 1);      \
-        else if (chunks <= 512) W8_QUANTIZE(P_, 256, 2); \
-        else if (chunks <= 1024) W8_QUANTIZE(P_, 256, 4);\
+        else if (chunks <= 512) W8_QUANTIZE(P_, 512, 1); \
+        else if (chunks <= 1024) W8_QUANTIZE(P_, 1024, 1); \
         else if (chunks <= 2048) W8_QUANTIZE(P_, 1024, 2); \
         else W8_QUANTIZE(P_, 1024, 4);                   \
     } while (0)
