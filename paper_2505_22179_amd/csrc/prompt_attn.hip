@@ -251,19 +251,10 @@ struct Rows {
         for (int j = 0; j < D / 16; ++j) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[j], qf[j], s, 0, 0, 0);
     }
 
-    // their probabilities, as operands of the product with the values; what came before is brought to the new maximum
-    template <int KT, bool MASKED>
-    __device__ __forceinline__ void softmax(float16v (&s)[KT], half8v (&pb)[2 * KT], int key0, float scale_log2e, int h)
+    // their probabilities, as operands of the product with the values, and the running sum; returns the factor that the outputs are still to be scaled by
+    template <int KT>
+    __device__ __forceinline__ float probabilities(float16v (&s)[KT], half8v (&pb)[2 * KT], float scale_log2e)
     {
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) settled(s[kt]);
-        if constexpr (MASKED) {
-            const int room = pos - key0 - 4 * h;   // key 32 kt + 8 (i / 4) + 4 h + i % 4 of the tile is seen up to the position
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[kt][i] = 32 * kt + 8 * (i >> 2) + (i & 3) <= room ? s[kt][i] : -__builtin_inff();
-        }
         float m[2] = {max_of_two(s[0][0], s[0][1]), max_of_two(s[0][2], s[0][3])};
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
@@ -273,29 +264,43 @@ struct Rows {
         // from moves only where it has grown by 8 (a factor of 2^8, in fp16 probabilities of up to 256): the outputs are seldom scaled, and any
         // reference that is not far below the largest score serves as well.
         const float m_seen = half_wave_max(max_of_two(m[0], m[1])) * scale_log2e;
-        const bool moves = !(m_seen <= m_run + 8.f);
-        if (__any(moves)) {
-            const float m_new = moves ? max_of_two(m_run, m_seen) : m_run, alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-            m_run = m_new;
-            l_run *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
-        }
-        const float less = -m_run;
-        float sum[4] = {};
+        const float m_larger = max_of_two(m_run, m_seen), m_new = m_seen <= m_run + 8.f ? m_run : m_larger, alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        m_run = m_new;
+        const float less = -m_new;
+        float sum[2] = {};
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], scale_log2e, less));
                 const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i + 1], scale_log2e, less));
-                sum[i & 3] += p0;
-                sum[(i & 3) + 1] += p1;
                 const half2v both = __builtin_convertvector((float2v){p0, p1}, half2v);
+                sum[(i >> 1) & 1] = __builtin_amdgcn_fdot2(both, (half2v){1, 1}, sum[(i >> 1) & 1], false);   // of what multiplies the values; one instruction for two
                 pb[2 * kt + (i >> 3)][i & 7] = both[0];
                 pb[2 * kt + (i >> 3)][(i & 7) + 1] = both[1];
             }
-        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        l_run = l_run * alpha + (sum[0] + sum[1]);
+        return alpha;
+    }
+
+    // the same with the mask, and the outputs scaled
+    template <int KT, bool MASKED>
+    __device__ __forceinline__ void softmax(float16v (&s)[KT], half8v (&pb)[2 * KT], int key0, float scale_log2e, int h)
+    {
+        if constexpr (KT == 2) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1]));   // settled() for both
+        else settled(s[0]);
+        if constexpr (MASKED) {
+            const int room = pos - key0 - 4 * h;   // key 32 kt + 8 (i / 4) + 4 h + i % 4 of the tile is seen up to the position
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[kt][i] = 32 * kt + 8 * (i >> 2) + (i & 3) <= room ? s[kt][i] : -__builtin_inff();
+        }
+        const float alpha = probabilities<KT>(s, pb, scale_log2e);
+        if (__any(alpha != 1.f)) {
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
+        }
     }
 
     // fragments u of the V tile: 16 keys, all D values
@@ -575,29 +580,40 @@ __global__ __launch_bounds__(512) void prompt_attn_tile_kernel(PromptArgs a)
     const uint32_t kfrag = Tile<D>::k_place(c, h), vfrag = v_fragment<D>(lane);
     const int trow = lane / CHUNKS, tchunk = lane % CHUNKS;
     const uint32_t stride = (uint32_t)a.Hkv * ROW;
+    static_assert(2 * PER % 8 == 0, "rows of transfers two apart lie alike");
+    uint32_t k_lane[2], v_lane[2];
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) {
+        const int row = odd * PER + trow;
+        k_lane[odd] = trow * stride + ((tchunk ^ (row & 7)) << 4);
+        v_lane[odd] = trow * stride + ((tchunk ^ (2 * row & (CHUNKS - 1))) << 4);
+    }
 
     auto work = [&](const Sequence &s, const Piece &p, bool whole, unsigned slot) {
         const uint8_t *const k_src = reinterpret_cast<const uint8_t *>(a.k) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
         const uint8_t *const v_src = reinterpret_cast<const uint8_t *>(a.v) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
         auto stage = [&](int step) { return lds + (step & (kStages - 1)) * 2 * TILE; };
+        // Transfer i of a wavefront brings PER rows; the descriptor ends with the sequence's last key: what lies behind it, whole tiles too, is not
+        // read (it is masked wherever it could count).
         auto request = [&](int step) {
-            if (step >= p.s1) return;
-            const int key0 = step * KEYS;
-            uint8_t *const buffer = stage(step);
-            const Stretch ks = stretch(k_src + (size_t)key0 * stride, 0x7FFFFFFF), vs = stretch(v_src + (size_t)key0 * stride, 0x7FFFFFFF);
+            const long long key0 = (long long)step * KEYS;
+            const uint32_t bytes = (uint32_t)max(0ll, min((s.T - 1 - key0) * stride + ROW, 0x7FFFFFFFll));
+            uint8_t *const tile = stage(step);
+            const Stretch ks = stretch(k_src + (size_t)key0 * stride, bytes), vs = stretch(v_src + (size_t)key0 * stride, bytes);
 #pragma unroll
             for (int i = 0; i < TRANSFERS; ++i) {
-                const int t = wave * TRANSFERS + i, row = t * PER + trow;
-                const uint32_t from = (uint32_t)min(row, s.T - 1 - key0) * stride;   // rows beyond the last key repeat it; they are masked
-                quad_to_lds(ks, buffer + t * 1024, from + ((tchunk ^ (row & 7)) << 4), 0);
-                quad_to_lds(vs, buffer + TILE + t * 1024, from + ((tchunk ^ (2 * row & (CHUNKS - 1))) << 4), 0);
+                const int t = wave * TRANSFERS + i;
+                quad_to_lds(ks, tile + t * 1024, k_lane[t & 1], (uint32_t)(t * PER) * stride);
+                quad_to_lds(vs, tile + TILE + t * 1024, v_lane[t & 1], (uint32_t)(t * PER) * stride);
             }
         };
         Rows<D> rows;
         rows.start(a, s, p, wave * 32 + c, h);
-        request(p.s0);
-        request(p.s0 + 1);
-        request(p.s0 + 2);
+        if (p.s0 < p.s1) {
+            request(p.s0);
+            request(p.s0 + 1);
+            request(p.s0 + 2);
+        }
         rows.arrive();
         // steps that every row of the workgroup sees whole: they and the others have loops of their own, without branches in them (outputs and scores
         // that two paths write to cost hundreds of registers in copies)
@@ -605,9 +621,7 @@ __global__ __launch_bounds__(512) void prompt_attn_tile_kernel(PromptArgs a)
         auto body = [&](int step, auto masked) {
             constexpr bool MASKED = decltype(masked)::value;
             // this tile has landed (the two behind it need not have), and the one before it has been read
-            if (step + 2 < p.s1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 * TRANSFERS) : "memory");
-            else if (step + 1 < p.s1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * TRANSFERS) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 * TRANSFERS) : "memory");
             request(step + kStages - 1);
             const uint8_t *const ktile = stage(step);
             float16v sc[KT];
@@ -624,6 +638,7 @@ __global__ __launch_bounds__(512) void prompt_attn_tile_kernel(PromptArgs a)
         int step = p.s0;
         for (; step < open; ++step) body(step, std::false_type{});
         for (; step < p.s1; ++step) body(step, std::true_type{});
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is under way into the buffers behind this
         const PartialBuffer po = Pieces<D, ROWS>::o(a, slot), pm = Pieces<D, ROWS>::ml(a, slot);
         const float l = rows.l_run + __shfl_xor(rows.l_run, 32, 64);
         const int row = wave * 32 + c;
