@@ -18,6 +18,7 @@ typedef float float2v __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) half4v lds_half4v;
 
 constexpr int kMostSequences = 4096;
+constexpr int kMostTiles = 1 << 20;   // that are counted; more than workgroups anyhow
 constexpr int kMostGroups = 256;   // workgroups of a call: one per compute unit, a ticket each
 
 struct PromptArgs {
@@ -44,7 +45,7 @@ __device__ __forceinline__ long long divide(long long a, long long b)
 constexpr int kPieceKeys = 256;
 
 // A sequence, and its place on the line of work.  Tile t of a KV head reaches from cost(t) to cost(t + 1): the keys that its last query sees, about,
-// and kPieceKeys.
+// and kPieceKeys, each counted `group` times: nothing is divided.
 struct Sequence {
     int n, T, q0, k0, tiles;
     int ahead;   // keys ahead of the first query
@@ -52,7 +53,7 @@ struct Sequence {
 template <int ROWS>
 __device__ __forceinline__ long long cost(const Sequence &s, int group, int t)
 {
-    return (long long)t * (s.ahead + kPieceKeys) + (long long)t * (t + 1) * (ROWS / 2) / group;   // t (t + 1) even: no half is lost
+    return (long long)t * (s.ahead + kPieceKeys) * group + (long long)t * (t + 1) * (ROWS / 2);
 }
 
 // sequence b, no tiles if its rows or keys do not lie in the buffers
@@ -87,28 +88,33 @@ __device__ __forceinline__ long long of_lane(long long x, int src)
 }
 __device__ __forceinline__ long long uniform(long long x) { return of_lane(x, 0); }
 
-constexpr long long kLongestLine = 1ll << 54;   // beyond any sensible call (sequences that share rows); products with a workgroup's number stay in 64 bits
+constexpr long long kLongestLine = 1ll << 60;   // beyond any sensible call (sequences that share rows); sums stay in 64 bits
 
 // The line of work, as one wavefront sees it (the same in all of them).  Sequences are read 64 at a time, one per lane.
 template <int ROWS>
 struct Line {
     long long total;              // its length
-    int tiles;                    // on it (at most 2^30 are counted)
+    int tiles;                    // on it (at most kMostTiles are counted)
     long long from, to;           // the sequence at hand reaches from .. to
     long long per_head;           // of each KV head
     Sequence seq;
     long long before;             // length up to the first of the 64 sequences from `base` on, among which the one at hand is
     int base;
 
-    // sequence base + lane, and the length up to and including it
-    __device__ __forceinline__ long long read(const PromptArgs &a, Sequence &mine, int lane) const
+    // sequence base + lane, and the length up to and including it (and tiles)
+    __device__ __forceinline__ long long read(const PromptArgs &a, Sequence &mine, int &upto_tiles, int lane) const
     {
         mine = read_sequence<ROWS>(a, base + lane);
         long long upto = min(cost<ROWS>(mine, a.group, mine.tiles) * a.Hkv, kLongestLine);
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
+        upto_tiles = min(mine.tiles * a.Hkv, kMostTiles);
+        const int here = min(64, a.B - base);
+        for (int off = 1; off < here; off <<= 1) {
             const long long other = shuffle(upto, max(lane - off, 0));
-            if (lane >= off) upto = min(upto + other, kLongestLine);
+            const int other_tiles = __shfl(upto_tiles, max(lane - off, 0), 64);
+            if (lane >= off) {
+                upto = min(upto + other, kLongestLine);
+                upto_tiles = min(upto_tiles + other_tiles, kMostTiles);
+            }
         }
         return min(upto + before, kLongestLine);
     }
@@ -117,12 +123,10 @@ struct Line {
         total = from = to = per_head = before = 0;
         tiles = 0;
         for (base = 0; base < a.B; base += 64) {
-            upto = read(a, mine, lane);
-            before = of_lane(upto, 63);
-            int here = mine.tiles * a.Hkv;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) here += __shfl_xor(here, off, 64);
-            tiles = (int)min((uint32_t)tiles + (uint32_t)__builtin_amdgcn_readfirstlane(here), 1u << 30);
+            int upto_tiles;
+            upto = read(a, mine, upto_tiles, lane);
+            before = of_lane(upto, min(63, a.B - base - 1));
+            tiles = min(tiles + __builtin_amdgcn_readlane(upto_tiles, min(63, a.B - base - 1)), kMostTiles);
         }
         total = before;
         before = 0;
@@ -134,9 +138,10 @@ struct Line {
     {
         if (at >= from && at < to) return;
         for (;; base += 64) {
-            if (!known) upto = read(a, mine, lane);
+            int upto_tiles;
+            if (!known) upto = read(a, mine, upto_tiles, lane);
             known = false;
-            const uint64_t hit = __ballot(upto > at);
+            const uint64_t hit = __ballot(upto > at && base + lane < a.B);
             if (hit) {
                 const int src = __builtin_ctzll(hit);
                 auto take = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
@@ -387,16 +392,17 @@ struct Pieces {
     __device__ __forceinline__ static PartialBuffer ml(const PromptArgs &a, unsigned slot) { return partial_buffer(a.part_ml + (size_t)slot * ROWS * 2); }
 };
 
-// Joins `pieces` pieces of a cut tile; called by the last of its workgroups to finish.  Where the rows are few, several groups of threads take
+// Joins `pieces` pieces of rows row0 .. row1 - 1 of a cut tile.  Where the rows are few, several groups of threads take
 // every so-manieth piece each and meet in LDS (`shared`, THREADS * 24 bytes): a piece's loads are one trip to memory, eight at a time.
-template <int D, int ROWS, int THREADS>
-__device__ __forceinline__ void join_pieces(const PromptArgs &a, const Sequence &s, const Piece &p, const uint16_t *slots, int pieces, int tid, float *shared)
+// SAME: written by other workgroups of the same kernel.
+template <int D, int ROWS, int THREADS, bool SAME>
+__device__ __forceinline__ void join_pieces(const PromptArgs &a, const Sequence &s, const Piece &p, const uint16_t *slots, int pieces, int row0, int row1, int tid, float *shared)
 {
-    const int items = p.rows * (D / 4);
+    const int items = (row1 - row0) * (D / 4);
     const int parts = items <= THREADS / 4 ? 4 : items <= THREADS / 2 ? 2 : 1, stride = THREADS / parts;   // uniform
     const int part = tid / stride;
     for (int item = tid % stride; item < items; item += stride) {
-        const int row = item / (D / 4), d4 = item % (D / 4);
+        const int row = row0 + item / (D / 4), d4 = item % (D / 4);
         float m = kLowest, den = 0.f;
         float4v num = {0.f, 0.f, 0.f, 0.f};
         constexpr int AT_ONCE = 8;
@@ -406,10 +412,17 @@ __device__ __forceinline__ void join_pieces(const PromptArgs &a, const Sequence 
 #pragma unroll
             for (int e = 0; e < AT_ONCE; ++e) {
                 const unsigned slot = __builtin_amdgcn_readfirstlane(slots[min(w + e * parts, pieces - 1)]);   // a wavefront is in one part
-                const PartialBuffer po = Pieces<D, ROWS>::o(a, slot), pm = Pieces<D, ROWS>::ml(a, slot);
-                ms[e] = load_partial_f32(pm, 2 * row);
-                ls[e] = load_partial_f32(pm, 2 * row + 1);
-                os[e] = load_partial(po, row * (D / 4) + d4);
+                if constexpr (SAME) {
+                    const PartialBuffer po = Pieces<D, ROWS>::o(a, slot), pm = Pieces<D, ROWS>::ml(a, slot);
+                    ms[e] = load_partial_f32(pm, 2 * row);
+                    ls[e] = load_partial_f32(pm, 2 * row + 1);
+                    os[e] = load_partial(po, row * (D / 4) + d4);
+                } else {
+                    const float *const ml = a.part_ml + (size_t)slot * ROWS * 2 + 2 * row;
+                    ms[e] = ml[0];
+                    ls[e] = ml[1];
+                    os[e] = *reinterpret_cast<const float4v *>(a.part_o + (size_t)slot * ROWS * D + row * D + 4 * d4);
+                }
             }
             float top = m;
 #pragma unroll
@@ -443,14 +456,63 @@ __device__ __forceinline__ void join_pieces(const PromptArgs &a, const Sequence 
                 den += wgt * shared[THREADS * 5 + g * stride + tid];
                 num += wgt * *reinterpret_cast<const float4v *>(shared + (g * stride + tid) * 4);
             }
-            store_row_quad(a, s, p, tid / (D / 4), D, tid % (D / 4) * 4, num, den);
+            store_row_quad(a, s, p, row0 + tid / (D / 4), D, tid % (D / 4) * 4, num, den);
         }
     }
 }
 
+// The cut of a line into stretches.
+template <int ROWS>
+struct Cut {
+    unsigned groups;
+    long long length, total;
+    // grid: workgroups at most; least: a tile is not cut into pieces shorter than this, in keys
+    __device__ __forceinline__ Cut(const Line<ROWS> &line, int group, unsigned grid, int least)
+    {
+        // as many workgroups as tiles, or as stretches of a length that is worth one; a multiple of the tiles, so that those of one length are cut alike
+        total = line.total;
+        groups = (unsigned)min((long long)grid, max((long long)max(line.tiles, 1), divide(total, (long long)least * group)));
+        if (line.tiles > 0 && (unsigned)line.tiles < groups) groups -= groups % (unsigned)line.tiles;
+        length = uniform(divide(total + groups - 1, groups));
+    }
+    __device__ __forceinline__ long long border(unsigned w) const { return min(length * w, total); }
+    // Collects the pieces of a cut tile: where each is kept, in the order of their keys.  w0 .. : the workgroups among which it lies.  All threads; `slots` and
+    // the count are there behind the caller's next barrier.  Returns this thread's part of the work that is left: see finish().
+    struct Found {
+        bool has;
+        unsigned slot;
+        uint64_t all;
+    };
+    __device__ __forceinline__ Found look(const Piece &p, unsigned w0, int tid, int lane, uint32_t *pieces_sh) const
+    {
+        const unsigned w1 = (unsigned)divide(p.end - 1, length), w = w0 + tid;
+        Found f = {false, 0, 0};
+        if (w <= w1) {
+            const long long b = border(w), e = border(w + 1);
+            f.has = step_at(p, max(b, p.begin)) != step_at(p, min(e, p.end));
+            f.slot = 2 * w + (p.begin > b ? 1 : 0);
+        }
+        f.all = __ballot(f.has);
+        if (lane == 0) pieces_sh[tid >> 6] = (uint32_t)__builtin_popcountll(f.all);
+        return f;
+    }
+    template <int WAVES>
+    __device__ __forceinline__ uint32_t finish(const Found &f, int tid, int lane, const uint32_t *pieces_sh, uint16_t *slots) const
+    {
+        uint32_t pieces = 0, ahead = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            ahead += i < (tid >> 6) ? pieces_sh[i] : 0;
+            pieces += pieces_sh[i];
+        }
+        if (f.has) slots[ahead + __builtin_popcountll(f.all & ((1ull << lane) - 1))] = (uint16_t)f.slot;
+        return pieces;
+    }
+};
+
 // Goes through a workgroup's stretch, piece by piece.  work(sequence, piece, whole, slot) computes steps s0 .. s1 - 1 (s0 < s1) and stores the
-// outputs (whole) or the piece's state.  LEAST: a tile is not cut into pieces shorter than this, in keys.
-template <int D, int ROWS, int STEP, int LEAST, int THREADS, typename Work>
+// outputs (whole) or the piece's state.  JOIN: the last workgroup of a cut tile to finish joins its pieces; else prompt_attn_join_kernel does.
+template <int D, int ROWS, int STEP, int LEAST, int THREADS, bool JOIN, typename Work>
 __device__ __forceinline__ void go_through(const PromptArgs &a, int tid, float *shared, Work work)
 {
     static_assert(kMostGroups <= THREADS, "");
@@ -460,12 +522,10 @@ __device__ __forceinline__ void go_through(const PromptArgs &a, int tid, float *
     Sequence mine;
     long long first_upto;
     Line<ROWS> line(a, lane, mine, first_upto);
-    const unsigned groups = (unsigned)min((long long)gridDim.x, max((long long)max(line.tiles, 1), line.total / LEAST));
-    if (blockIdx.x >= groups) return;
-    const long long stretch_length = uniform(divide(line.total + groups - 1, groups));
-    auto border = [&](unsigned w) { return min(stretch_length * w, line.total); };
-    const unsigned me = stretch_number(blockIdx.x, groups);
-    const long long start = border(me), stop = border(me + 1);
+    const Cut<ROWS> cut(line, a.group, gridDim.x, LEAST);
+    if (blockIdx.x >= cut.groups) return;
+    const unsigned me = stretch_number(blockIdx.x, cut.groups);
+    const long long start = cut.border(me), stop = cut.border(me + 1);
     long long at = start;
     if (at < stop) line.find(a, at, lane, mine, first_upto, a.B <= 64);
     while (at < stop) {   // uniform over the workgroup
@@ -481,32 +541,17 @@ __device__ __forceinline__ void go_through(const PromptArgs &a, int tid, float *
         } else if (p.s0 < p.s1) {
             const bool whole = p.s1 - p.s0 == p.steps;
             work(line.seq, p, whole, 2 * me + (at > start ? 1u : 0u));
-            if (!whole) {
-                // the workgroups that have a step of the tile, w0 the one where it begins
-                const unsigned w0 = (unsigned)divide(p.begin, stretch_length), w1 = (unsigned)divide(p.end - 1, stretch_length);
-                const unsigned w = w0 + tid;
-                bool has = false, later = false;
-                if (w <= w1) {
-                    const long long b = border(w), e = border(w + 1);
-                    has = step_at(p, max(b, p.begin)) != step_at(p, min(e, p.end));
-                    later = p.begin > b;
-                }
-                const uint64_t all = __ballot(has);
-                if (lane == 0) pieces_sh[tid >> 6] = (uint32_t)__builtin_popcountll(all);
+            if (JOIN && !whole) {
+                const unsigned w0 = (unsigned)divide(p.begin, cut.length);   // the workgroup that the tile begins in: its ticket
+                const auto found = cut.look(p, w0, tid, lane, pieces_sh);
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wavefront's part of the piece has reached memory
                 __syncthreads();
-                uint32_t pieces = 0, ahead = 0;
-#pragma unroll
-                for (int i = 0; i < THREADS / 64; ++i) {
-                    ahead += i < (tid >> 6) ? pieces_sh[i] : 0;
-                    pieces += pieces_sh[i];
-                }
-                if (has) slots[ahead + __builtin_popcountll(all & ((1ull << lane) - 1))] = (uint16_t)(2 * w + later);
+                const uint32_t pieces = cut.template finish<THREADS / 64>(found, tid, lane, pieces_sh, slots);
                 if (tid == 0) ticket_sh = __hip_atomic_fetch_add(&a.tickets[w0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 __syncthreads();
                 if (ticket_sh == pieces - 1) {
                     if (tid == 0) __hip_atomic_store(&a.tickets[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    join_pieces<D, ROWS, THREADS>(a, line.seq, p, slots, (int)pieces, tid, shared);
+                    join_pieces<D, ROWS, THREADS, true>(a, line.seq, p, slots, (int)pieces, 0, p.rows, tid, shared);
                 }
             }
             __syncthreads();   // LDS and the ticket are free for the next piece
@@ -514,6 +559,39 @@ __device__ __forceinline__ void go_through(const PromptArgs &a, int tid, float *
         at = upto;
         if (at < stop) line.find(a, at, lane, mine, 0, false);
     }
+}
+
+// Joins the pieces of the tiles that the tile kernel's stretches cut, kJoinRows rows to a workgroup: a tile of 256 rows is 128 KB a piece, of which one
+// workgroup alone reads 20 KB in a microsecond (4 x 64 queries behind 7936 keys, 32/8 heads: 103 us joined by the last to finish, 72 like this).
+// blockIdx.x: rows (next to each other on all XCDs: cut tiles begin at every eighth stretch, say); blockIdx.y: the stretch whose end cuts the tile
+// that begins in it.
+constexpr int kJoinRows = 8;
+template <int D, int ROWS, int STEP, int LEAST>
+__global__ __launch_bounds__(256) void prompt_attn_join_kernel(PromptArgs a)
+{
+    static_assert(kMostGroups <= 256, "");
+    const int tid = threadIdx.x, lane = tid & 63;
+    __shared__ uint32_t pieces_sh[4];
+    __shared__ uint16_t slots[kMostGroups];
+    __shared__ __attribute__((aligned(16))) float shared[256 * 6];
+    Sequence mine;
+    long long first_upto;
+    Line<ROWS> line(a, lane, mine, first_upto);
+    const Cut<ROWS> cut(line, a.group, gridDim.y, LEAST);
+    const unsigned me = blockIdx.y;
+    const long long at = cut.border(me + 1);
+    if (me + 1 >= cut.groups || at >= line.total) return;
+    line.find(a, at, lane, mine, first_upto, a.B <= 64);
+    Piece p;
+    tile_of<ROWS, STEP>(a, line, at, p);
+    const int row0 = blockIdx.x * kJoinRows;
+    if (p.begin >= at || p.begin < cut.border(me) || p.steps == 0 || row0 >= p.rows) return;   // not cut here, or not first here
+    const auto found = cut.look(p, me, tid, lane, pieces_sh);
+    __syncthreads();
+    const uint32_t pieces = cut.template finish<4>(found, tid, lane, pieces_sh, slots);
+    __syncthreads();
+    if (pieces < 2) return;   // one workgroup has all its steps and has stored the outputs
+    join_pieces<D, ROWS, 256, false>(a, line.seq, p, slots, (int)pieces, row0, min(row0 + kJoinRows, p.rows), tid, shared);
 }
 
 // Many tiles: one per workgroup, whole.  They are numbered from the last of the last sequence down, so that the tiles that see most keys of a sequence are
@@ -564,17 +642,17 @@ __device__ __forceinline__ void take_one(const PromptArgs &a, int lane, Work wor
 }
 
 // Many rows: eight wavefronts of 32 rows each, keys through LDS in tiles of 64, one barrier per tile, four buffers: three tiles are under way.
-constexpr int kStages = 4, kTileRows = 256, kTileKeys = 64;
-template <int D, bool CUT>
-__global__ __launch_bounds__(512) void prompt_attn_tile_kernel(PromptArgs a)
+constexpr int kTileKeys = 64, kTileLeast = 1024;
+template <int D, int NW, int STAGES, bool CUT>
+__global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs a)
 {
-    constexpr int ROWS = kTileRows, KEYS = kTileKeys, NW = 8, KT = KEYS / 32;
+    constexpr int ROWS = 32 * NW, KEYS = kTileKeys, KT = KEYS / 32;
     constexpr int ROW = Tile<D>::ROW, CHUNKS = Tile<D>::CHUNKS, TILE = KEYS * ROW;
     constexpr int PER = 1024 / ROW;                  // rows of a transfer
     constexpr int TRANSFERS = TILE / 1024 / NW;      // of a wavefront, K and V each
     static_assert(TRANSFERS >= 1, "");
     extern __shared__ float4v smem4[];
-    uint8_t *const lds = reinterpret_cast<uint8_t *>(smem4);   // kStages times K, V
+    uint8_t *const lds = reinterpret_cast<uint8_t *>(smem4);   // STAGES times K, V
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, c = lane & 31;
     const uint32_t kfrag = Tile<D>::k_place(c, h), vfrag = v_fragment<D>(lane);
@@ -592,7 +670,7 @@ __global__ __launch_bounds__(512) void prompt_attn_tile_kernel(PromptArgs a)
     auto work = [&](const Sequence &s, const Piece &p, bool whole, unsigned slot) {
         const uint8_t *const k_src = reinterpret_cast<const uint8_t *>(a.k) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
         const uint8_t *const v_src = reinterpret_cast<const uint8_t *>(a.v) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
-        auto stage = [&](int step) { return lds + (step & (kStages - 1)) * 2 * TILE; };
+        auto stage = [&](int step) { return lds + (step & (STAGES - 1)) * 2 * TILE; };
         // Transfer i of a wavefront brings PER rows; the descriptor ends with the sequence's last key: what lies behind it, whole tiles too, is not
         // read (it is masked wherever it could count).
         auto request = [&](int step) {
@@ -610,9 +688,8 @@ __global__ __launch_bounds__(512) void prompt_attn_tile_kernel(PromptArgs a)
         Rows<D> rows;
         rows.start(a, s, p, wave * 32 + c, h);
         if (p.s0 < p.s1) {
-            request(p.s0);
-            request(p.s0 + 1);
-            request(p.s0 + 2);
+#pragma unroll
+            for (int i = 0; i < STAGES - 1; ++i) request(p.s0 + i);
         }
         rows.arrive();
         // steps that every row of the workgroup sees whole: they and the others have loops of their own, without branches in them (outputs and scores
@@ -620,9 +697,9 @@ __global__ __launch_bounds__(512) void prompt_attn_tile_kernel(PromptArgs a)
         const int all_see = s.T - s.n + p.first / a.group + 1, open = min(all_see / KEYS, p.s1);
         auto body = [&](int step, auto masked) {
             constexpr bool MASKED = decltype(masked)::value;
-            // this tile has landed (the two behind it need not have), and the one before it has been read
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 * TRANSFERS) : "memory");
-            request(step + kStages - 1);
+            // this tile has landed (those asked for after it need not have), and the one before it has been read
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * TRANSFERS * (STAGES - 2)) : "memory");
+            request(step + STAGES - 1);
             const uint8_t *const ktile = stage(step);
             float16v sc[KT];
             half8v pb[2 * KT];
@@ -639,7 +716,8 @@ __global__ __launch_bounds__(512) void prompt_attn_tile_kernel(PromptArgs a)
         for (; step < open; ++step) body(step, std::false_type{});
         for (; step < p.s1; ++step) body(step, std::true_type{});
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is under way into the buffers behind this
-        const PartialBuffer po = Pieces<D, ROWS>::o(a, slot), pm = Pieces<D, ROWS>::ml(a, slot);
+        // a piece is read by another kernel: plain stores, whose lines the L2 puts together (written through, 32 bytes at a time, 128 KB took 20 us and more)
+        float *const po = a.part_o + (size_t)slot * ROWS * D, *const pm = a.part_ml + (size_t)slot * ROWS * 2;
         const float l = rows.l_run + __shfl_xor(rows.l_run, 32, 64);
         const int row = wave * 32 + c;
         if (row < p.rows) {
@@ -650,15 +728,15 @@ __global__ __launch_bounds__(512) void prompt_attn_tile_kernel(PromptArgs a)
                     const float4v val = {rows.o[dt][4 * g], rows.o[dt][4 * g + 1], rows.o[dt][4 * g + 2], rows.o[dt][4 * g + 3]};
                     const int d = 32 * dt + 8 * g + 4 * h;
                     if (whole) store_row_quad(a, s, p, row, D, d, val, l);
-                    else store_partial(po, (row * D + d) / 4, val);
+                    else *reinterpret_cast<float4v *>(po + row * D + d) = val;
                 }
             if (!whole && h == 0) {
-                store_partial_f32(pm, 2 * row, rows.m_run);
-                store_partial_f32(pm, 2 * row + 1, l);
+                pm[2 * row] = rows.m_run;
+                pm[2 * row + 1] = l;
             }
         }
     };
-    if constexpr (CUT) go_through<D, ROWS, KEYS, 1024, 64 * NW>(a, tid, reinterpret_cast<float *>(lds), work);
+    if constexpr (CUT) go_through<D, ROWS, KEYS, kTileLeast, 64 * NW, false>(a, tid, reinterpret_cast<float *>(lds), work);
     else take_one<D, ROWS, KEYS>(a, lane, work);
 }
 
@@ -682,7 +760,7 @@ __global__ __launch_bounds__(512) void prompt_attn_few_kernel(PromptArgs a)
     const uint32_t stride = (uint32_t)a.Hkv * ROW;
     uint8_t *const ktile = lds + wave * 2 * TILE, *const vtile = ktile + TILE;
 
-    go_through<D, ROWS, KEYS, 512, 64 * NW>(a, tid, reinterpret_cast<float *>(lds), [&](const Sequence &s, const Piece &p, bool whole, unsigned slot) {
+    go_through<D, ROWS, KEYS, 512, 64 * NW, true>(a, tid, reinterpret_cast<float *>(lds), [&](const Sequence &s, const Piece &p, bool whole, unsigned slot) {
         const uint8_t *const k_src = reinterpret_cast<const uint8_t *>(a.k) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
         const uint8_t *const v_src = reinterpret_cast<const uint8_t *>(a.v) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
         auto request = [&](int step, const uint8_t *src, uint8_t *tile, bool values) {
@@ -733,10 +811,11 @@ __global__ __launch_bounds__(512) void prompt_attn_few_kernel(PromptArgs a)
         const float l_run = rows.l_run + __shfl_xor(rows.l_run, 32, 64);
         __syncthreads();   // every wavefront has left its tiles
         float *const state = reinterpret_cast<float *>(lds + STATE);
-        if (h == 0) {
+        if (c < p.rows && h == 0) {
             state[(c * NW + wave) * 2] = rows.m_run;
             state[(c * NW + wave) * 2 + 1] = l_run;
         }
+        if (c < p.rows)
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -793,10 +872,23 @@ static PromptPlan prompt_plan(int rows, int B, int max_q, int max_k, int Hq, int
 {
     PromptPlan p;
     const int group = Hq / Hkv;
+    auto tiles_of = [&](int height) { return ((long long)rows * group + (long long)(height - 1) * B) / height; };   // most of a KV head
     p.few = (long long)max_q * group <= 2 * kFewRows;
-    p.rows = p.few ? kFewRows : kTileRows;
-    const long long tiles = (long long)rows * group / p.rows + B;   // most of a KV head
-    p.cut = p.few || (max_k > 4096 && (long long)rows * group / p.rows * Hkv < 2 * kMostGroups);
+    p.rows = kFewRows;
+    p.cut = true;
+    if (!p.few) {
+        // Whole tiles of 256 rows (a step of 64 keys takes 2.15 us), of 128, two to a compute unit (1.35 us alone, 2.15 with a neighbour), or tiles of 256 cut
+        // into equal stretches (40 us more for pieces written, read and joined): the shortest by these times, were all sequences as long as the longest.
+        // 32/8 heads: 1024 queries 38, 31 us and - ; 2048 queries -, 61 and 90; 4 x 64 queries behind 2936 keys -, 69 and 58; 4096 queries 156, 166 and -.
+        const long long steps = (max_k + 63) / 64, part = max_q >= max_k ? 1 : 2;   // a whole prompt's rows see half of its keys on average
+        const long long high = tiles_of(256) * Hkv, low = tiles_of(128) * Hkv;
+        const long long whole = high <= 256 ? steps * 2150 : (high + 255) / 256 * steps * part * 1075;
+        const long long halves = low <= 256 ? steps * 1350 : low <= 512 ? steps * 2150 : (low + 511) / 512 * steps * part * 1075;
+        const long long cut = high * steps * part * 1075 / 256 + 40000;
+        p.cut = cut < whole && cut < halves;
+        p.rows = !p.cut && halves < whole ? 128 : 256;
+    }
+    const long long tiles = tiles_of(p.rows);
     if (p.cut) {   // no more workgroups than there can be work for, were every sequence as long as the longest
         p.grid = (int)min(tiles * Hkv * (((long long)max_k + 255) / 256), (long long)kMostGroups);
         p.o_bytes = (size_t)p.grid * 2 * p.rows * D * 4;
@@ -822,10 +914,16 @@ static int launch_with_lds(Kernel kernel, int lds, int threads, const PromptArgs
 template <int D>
 static int launch_prompt(const PromptArgs &a, const PromptPlan &p, hipStream_t stream)
 {
-    constexpr int tile_lds = kStages * 2 * kTileKeys * D * 2;
+    constexpr int stage = 2 * kTileKeys * D * 2;
     if (p.few) return launch_with_lds<D>(&prompt_attn_few_kernel<D>, few_lds<D>(), 512, a, p, stream);
-    if (p.cut) return launch_with_lds<D + 1>(&prompt_attn_tile_kernel<D, true>, tile_lds, 512, a, p, stream);
-    return launch_with_lds<D + 2>(&prompt_attn_tile_kernel<D, false>, tile_lds, 512, a, p, stream);
+    if (p.cut) {
+        const int rc = launch_with_lds<D + 1>(&prompt_attn_tile_kernel<D, 8, 4, true>, 4 * stage, 512, a, p, stream);
+        if (rc != W4A16_OK) return rc;
+        hipLaunchKernelGGL((prompt_attn_join_kernel<D, 256, kTileKeys, kTileLeast>), dim3(256 / kJoinRows, (unsigned)p.grid), dim3(256), 0, stream, a);
+        return launch_status();
+    }
+    if (p.rows == 128) return launch_with_lds<D + 2>(&prompt_attn_tile_kernel<D, 4, 2, false>, 2 * stage, 256, a, p, stream);
+    return launch_with_lds<D + 3>(&prompt_attn_tile_kernel<D, 8, 4, false>, 4 * stage, 512, a, p, stream);
 }
 
 }  // namespace w4
