@@ -133,11 +133,11 @@ struct Line {
         base = 0;
     }
     // brings the sequence that holds place `at` to hand; at < total, and no place before the last one asked for.  mine, upto: what the constructor
-    // read, if `known`
-    __device__ __forceinline__ void find(const PromptArgs &a, long long at, int lane, Sequence mine, long long upto, bool known)
+    // read, if `known`.  False if there is none: lengths that were changed under the running kernel
+    __device__ __forceinline__ bool find(const PromptArgs &a, long long at, int lane, Sequence mine, long long upto, bool known)
     {
-        if (at >= from && at < to) return;
-        for (;; base += 64) {
+        if (at >= from && at < to) return true;
+        for (; base < a.B; base += 64) {
             int upto_tiles;
             if (!known) upto = read(a, mine, upto_tiles, lane);
             known = false;
@@ -149,10 +149,11 @@ struct Line {
                 per_head = cost<ROWS>(seq, a.group, seq.tiles);
                 to = of_lane(upto, src);
                 from = to - per_head * a.Hkv;
-                return;
+                return true;
             }
             before = of_lane(upto, 63);
         }
+        return false;
     }
 };
 
@@ -471,7 +472,7 @@ struct Cut {
     {
         // as many workgroups as tiles, or as stretches of a length that is worth one; a multiple of the tiles, so that those of one length are cut alike
         total = line.total;
-        groups = (unsigned)min((long long)grid, max((long long)max(line.tiles, 1), divide(total, (long long)least * group)));
+        groups = (unsigned)__builtin_amdgcn_readfirstlane((int)min((long long)grid, max((long long)max(line.tiles, 1), divide(total, (long long)least * group))));
         if (line.tiles > 0 && (unsigned)line.tiles < groups) groups -= groups % (unsigned)line.tiles;
         length = uniform(divide(total + groups - 1, groups));
     }
@@ -527,7 +528,7 @@ __device__ __forceinline__ void go_through(const PromptArgs &a, int tid, float *
     const unsigned me = stretch_number(blockIdx.x, cut.groups);
     const long long start = cut.border(me), stop = cut.border(me + 1);
     long long at = start;
-    if (at < stop) line.find(a, at, lane, mine, first_upto, a.B <= 64);
+    if (at < stop && !line.find(a, at, lane, mine, first_upto, a.B <= 64)) return;
     while (at < stop) {   // uniform over the workgroup
         Piece p;
         tile_of<ROWS, STEP>(a, line, at, p);
@@ -542,7 +543,7 @@ __device__ __forceinline__ void go_through(const PromptArgs &a, int tid, float *
             const bool whole = p.s1 - p.s0 == p.steps;
             work(line.seq, p, whole, 2 * me + (at > start ? 1u : 0u));
             if (JOIN && !whole) {
-                const unsigned w0 = (unsigned)divide(p.begin, cut.length);   // the workgroup that the tile begins in: its ticket
+                const unsigned w0 = (unsigned)__builtin_amdgcn_readfirstlane((int)divide(p.begin, cut.length));   // the workgroup that the tile begins in: its ticket
                 const auto found = cut.look(p, w0, tid, lane, pieces_sh);
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wavefront's part of the piece has reached memory
                 __syncthreads();
@@ -557,7 +558,7 @@ __device__ __forceinline__ void go_through(const PromptArgs &a, int tid, float *
             __syncthreads();   // LDS and the ticket are free for the next piece
         }
         at = upto;
-        if (at < stop) line.find(a, at, lane, mine, 0, false);
+        if (at < stop && !line.find(a, at, lane, mine, 0, false)) return;
     }
 }
 
@@ -581,7 +582,7 @@ __global__ __launch_bounds__(256) void prompt_attn_join_kernel(PromptArgs a)
     const unsigned me = blockIdx.y;
     const long long at = cut.border(me + 1);
     if (me + 1 >= cut.groups || at >= line.total) return;
-    line.find(a, at, lane, mine, first_upto, a.B <= 64);
+    if (!line.find(a, at, lane, mine, first_upto, a.B <= 64)) return;
     Piece p;
     tile_of<ROWS, STEP>(a, line, at, p);
     const int row0 = blockIdx.x * kJoinRows;
