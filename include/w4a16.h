@@ -334,7 +334,7 @@ int tree_accept_kv8(const int32_t *parent, const int32_t *token, const int32_t *
  *   W4A16_ROPE_BY_INDEX  r f_i / factor + (1 - r) f_i,  r = (i - a) / (b - a) within [0, 1], where a and b are the (fractional) pair indices
  *                        that turn `high` and `low` times within the original context, a rounded down and at least 0, b rounded up and at most R - 1 (b - a at least 0.001)
  *   cos_table, sin_table  fp32 [n_pos, R / 2], 16-byte aligned, out: entry [p, i] = amplitude * cos / sin((first + p) f_i)
- * Evaluated in fp64 and rounded once.  theta > 1; factor > 0 unless W4A16_ROPE_PLAIN; 0 < low < high and original > 0 for the last two (other
+ * Evaluated in fp64 and rounded once.  theta > 1; factor >= 1/8 unless W4A16_ROPE_PLAIN; 0 < low < high and original > 0 for the last two (other
  * kinds ignore what they do not use).  R even, R <= 1024, first + n_pos <= 2^28. */
 #define W4A16_ROPE_PLAIN 0
 #define W4A16_ROPE_LINEAR 1
@@ -355,7 +355,8 @@ int rope_table(float *cos_table, float *sin_table, int first, int n_pos, int R, 
 int rope_prompt(const void *qkv, const int32_t *pos, const float *cos_table, const float *sin_table, int n_pos, int R, int interleaved,
                 const int32_t *slot, int cache_rows, void *q, void *k_cache, void *v_cache, int rows, int Hq, int Hkv, int D, void *stream);
 
-/* Scratch of w4a16_prompt_attn for these sizes (partial results where the keys of a row are cut into ranges). */
+/* Scratch of w4a16_prompt_attn for these sizes (partial results where the keys of a row are cut into ranges).  Few or single queries can need more than
+ * many: a workspace that serves calls of different sizes has the largest of theirs. */
 size_t w4a16_prompt_attn_workspace_bytes(int rows, int B, int max_q, int max_k, int Hq, int Hkv, int D);
 
 /* Causal attention of B packed sequences of different lengths over their keys in a cache: whole prompts, pieces of long ones behind what the

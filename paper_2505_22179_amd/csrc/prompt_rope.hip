@@ -190,6 +190,7 @@ int rope_table(float *cos_table, float *sin_table, int first, int n_pos, int R, 
     if (scaling >= W4A16_ROPE_BY_TURNS && (!(low > 0.0) || !(high > low) || !(high < INFINITY) || !(original > 0.0) || !(original < INFINITY)))
         return W4A16_EINVAL;
     if (R > 2 * kTableMostPairs || (long long)first + n_pos > (1ll << 28)) return W4A16_EUNSUP;
+    if (scaling != W4A16_ROPE_PLAIN && factor < 0.125) return W4A16_EUNSUP;   // angles stay below 2^31
     if (!cos_table || !sin_table) return W4A16_ENULL;
     if (misaligned(cos_table) || misaligned(sin_table)) return W4A16_EALIGN;
     TableArgs a = {cos_table, sin_table, -log2(theta) * 2.0 / R, 1.0, 0.0, low, 0.0, amplitude, first, n_pos, R / 2, scaling};

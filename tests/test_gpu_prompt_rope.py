@@ -140,3 +140,16 @@ def test_graph_replays():
         assert torch.equal(cos, first)
         for x, w in zip(bufs, want):
             np.testing.assert_array_equal(x.cpu().numpy().view(np.uint16), w.view(np.uint16))
+
+
+@pytest.mark.parametrize("kind, low, high, original", [(B.ROPE_LINEAR, 0.0, 0.0, 0.0), (B.ROPE_BY_TURNS, 1.0, 4.0, 8.0), (B.ROPE_BY_INDEX, 1.0, 32.0, 64.0)])
+def test_tables_of_the_largest_angles(kind, low, high, original):
+    first, n, R_, factor = 2 ** 28 - 20, 20, 64, 0.125
+    cos, sin = (torch.zeros(n, R_ // 2, device=DEV) for _ in range(2))
+    print(f"rope_table kind {kind} from {first}", flush=True)
+    B.rope_table(cos, sin, first, n, R_, 10000.0, kind, factor, low, high, original, 1.0)
+    torch.cuda.synchronize()
+    for got, ref in zip((cos, sin), R.rope_table(first, n, R_, 10000.0, kind, factor, low, high, original, 1.0)):
+        # as above, of angles that are 1 / factor times as large
+        tol = 2.0 ** -24 * np.abs(ref) + 2.0 ** 31 * 2.0 ** -48 + 2.0 ** -35
+        assert (np.abs(got.cpu().numpy().astype(np.float64) - ref) <= tol).all()

@@ -117,3 +117,8 @@ def test_no_result_of_a_matrix_instruction_is_touched_too_early(library, kernels
         bad += [b for b in found if kernels in b.split(":")[0]]
         matrix += sum(n.startswith("v_mfma") and kernels in k for n, k in zip(code.name, code.kernel))
     assert matrix > 50 and not bad, "\n".join(bad[:40])
+
+
+def test_rope_table_refuses_factors_that_lead_out_of_its_range():
+    call = caller(B.load(), "rope_table", cos=A, sin=A, first=0, n=64, R=128, theta=1e4, scaling=B.ROPE_LINEAR, factor=0.1249, low=1.0, high=4.0, original=8192.0, amplitude=1.0)
+    refusals(call, {EUNSUP: [dict(), dict(scaling=B.ROPE_BY_TURNS), dict(scaling=B.ROPE_BY_INDEX), dict(factor=1e-300)]})
