@@ -320,8 +320,11 @@ __global__ __launch_bounds__(64 * WM * WN) void w8a8_tile_kernel(GemmArgs a)
 }
 
 // Few tokens, bound by the weights: eight wavefronts share TW tiles of channels and take every eighth tile of k; weights go straight to registers.
+// One tile of channels: AHEAD tiles of k are always under way, each asked for as soon as its registers are free (one token 14336 -> 4096 11.3 us, asked for
+// four at a time 12.6: 5.2 TB/s; 28672 -> 8192 39.4, 43).  Two, of which fewer workgroups come to a compute unit: four at a time (60 tokens 8192 -> 8192
+// 17.2, always under way 19.7).
 // FUSED: one token of up to kFusedK values, quantised by every workgroup for itself into LDS while its first weights are on the way: a launch less, in the
-// other kernel's arrangement and so with its bits.  A normed token 4096 -> 28672 25.1 -> 22.1 us, 4096 -> 6144 10.9 -> 8.1.  Longer rows or more
+// other kernel's arrangement and so with its bits.  A normed token 4096 -> 28672 25.1 -> 21.8 us, 4096 -> 6144 10.9 -> 8.0.  Longer rows or more
 // tokens cost every workgroup more than the launch: 8192 -> 57344 82 -> 84, two tokens 4096 -> 28672 25 -> 29.
 constexpr int kFusedK = 4096;
 template <int MT, int TW, int PRE = W8A8_PLAIN, bool FUSED = false>
@@ -339,47 +342,55 @@ __global__ __launch_bounds__(512) void w8a8_stream_kernel(GemmArgs a)
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < TW; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
-    const uint8_t *xs[MT], *ws[TW];
+    Stretch xs[MT], ws[TW];   // a row of tiles each: what is asked for behind its end is zero, and adds nothing
 #pragma unroll
-    for (int i = 0; i < MT; ++i) xs[i] = a.codes + (size_t)min(i, x_tiles - 1) * a.blocks * 1024 + lane * 16;
+    for (int i = 0; i < MT; ++i) xs[i] = stretch(a.codes + (size_t)min(i, x_tiles - 1) * a.blocks * 1024, a.blocks * 1024);
 #pragma unroll
-    for (int j = 0; j < TW; ++j) ws[j] = a.packed + (size_t)min(tile0 + j, w_tiles - 1) * a.blocks * 1024 + lane * 16;
-    auto weights = [&](int4v (&wf)[AHEAD][TW], int b) {
+    for (int j = 0; j < TW; ++j) ws[j] = stretch(a.packed + (size_t)min(tile0 + j, w_tiles - 1) * a.blocks * 1024, a.blocks * 1024);
+    int4v wf[AHEAD][TW], xf[AHEAD][MT];
+    auto load = [&](int u, int at) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
+        for (int j = 0; j < TW; ++j) wf[u][j] = __builtin_bit_cast(int4v, __builtin_amdgcn_raw_buffer_load_b128(ws[j], at * 1024 + lane * 16, 0, kStreamed));
+        if constexpr (!FUSED)
 #pragma unroll
-            for (int j = 0; j < TW; ++j)
-                wf[u][j] = __builtin_nontemporal_load(reinterpret_cast<const int4v *>(ws[j] + (size_t)min(b + 8 * u, a.blocks - 1) * 1024));
+            for (int i = 0; i < MT; ++i) xf[u][i] = __builtin_bit_cast(int4v, __builtin_amdgcn_raw_buffer_load_b128(xs[i], at * 1024 + lane * 16, 0, 0));
     };
-    int4v wf[AHEAD][TW];
+    if constexpr (TW == 1)
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) load(u, wave + 8 * u);
     if constexpr (FUSED) {
-        weights(wf, wave);
         __builtin_amdgcn_sched_barrier(0);
         const float s = quantize_row<PRE, 256, 1>(a.x, a.gamma, a.eps, a.K, a.blocks * 4, threadIdx.x, norm_sums, tops,
                                                   [&](int chunk, u32x4 packed) { row_codes[chunk] = packed; });
         if (threadIdx.x == 0) row_scale = s;
         __syncthreads();
     }
-    for (int b = wave; b < a.blocks; b += 8 * AHEAD) {
-        int4v xf[AHEAD][MT];
-        if (!FUSED || b != wave) weights(wf, b);
+    auto add = [&](int u, int at) {
+        if constexpr (FUSED) xf[u][0] = __builtin_bit_cast(int4v, row_codes[min(at, a.blocks - 1) * 4 + (lane >> 4)]);   // the token's, for all sixteen rows
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int at = min(b + 8 * u, a.blocks - 1);
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                if constexpr (FUSED) xf[u][i] = __builtin_bit_cast(int4v, row_codes[at * 4 + (lane >> 4)]);   // the token's, for all sixteen rows
-                else xf[u][i] = *reinterpret_cast<const int4v *>(xs[i] + (size_t)at * 1024);
+            for (int j = 0; j < TW; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[u][j], xf[u][i], acc[i][j], 0, 0, 0);
+    };
+    int b = wave;
+    if constexpr (TW == 1) {
+        for (; b + 8 * AHEAD < a.blocks; b += 8 * AHEAD) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                add(u, b + 8 * u);
+                load(u, b + 8 * (u + AHEAD));
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            if (b + 8 * u < a.blocks) {
+        for (int u = 0; u < AHEAD; ++u) add(u, b + 8 * u);
+    } else {
+        for (; b < a.blocks; b += 8 * AHEAD) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+            for (int u = 0; u < AHEAD; ++u) load(u, b + 8 * u);
+            if constexpr (MT == 2) __builtin_amdgcn_sched_barrier(0);   // left to itself the compiler puts the loads next to their products: 32 tokens 4096 -> 6144 7.5 us, 8.4
 #pragma unroll
-                    for (int j = 0; j < TW; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[u][j], xf[u][i], acc[i][j], 0, 0, 0);
-            }
+            for (int u = 0; u < AHEAD; ++u) add(u, b + 8 * u);
         }
     }
 #pragma unroll
@@ -468,9 +479,9 @@ static int launch_tile(GemmArgs a, const GemmPlan &p, hipStream_t stream)
 }
 
 // The kernels, by measurement over 28 shapes (M 1 .. 4096, N 1024 .. 28672, K 4096 .. 14336), us:
-//   up to 16 tokens, and up to 64 where k is short, the stream kernel: 60 tokens 4096 -> 4096 8.6 (tiles of 64 x 128, walk shared by four, 13.6), 8192 -> 8192 18.5
+//   up to 16 tokens, and up to 64 where k is short, the stream kernel: 60 tokens 4096 -> 4096 7.5 (tiles of 64 x 128, walk shared by four, 13.6), 8192 -> 8192 17.2
 //   (22.1); with many channels or a long k its wavefronts' own copies of the activations cost more than an exchange: 60 tokens 4096 -> 28672 30.8 (24.7),
-//   14336 -> 4096 21.9 (19.6).  Two tiles of channels to a wavefront where that still fills the chip: 60 tokens 8192 -> 8192 21.9 with one
+//   14336 -> 4096 21.9 (19.6).  Two tiles of channels to a wavefront where that still fills the chip: 60 tokens 8192 -> 8192 23.8 with one
 //   up to 128 tokens tiles of 64 x 128 with a shared walk unless 128 x 128 fill the chip: 100 tokens 4096 -> 4096 12.5 (13.8)
 //   more: of 256 x 256, 128 x 256 and 128 x 128 the one that takes the shortest time by its rounds over 256 compute units, a step of 128 values of k in
 //   1.66, 1.02 and 0.54 us: 4096 tokens 4096 -> 4096 59, 74 and 74; 777 tokens 8192 -> 8192 73, 61 and 74; 1024 tokens 4096 -> 4096 -, 29 and 23
