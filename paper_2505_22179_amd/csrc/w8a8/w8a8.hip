@@ -227,16 +227,16 @@ __global__ __launch_bounds__(64 * WM * WN) void w8a8_tile_kernel(GemmArgs a)
     for (int i = 0; i < TRANSFERS; ++i)
         xs[i] = a.codes + ((size_t)min(bm * XT + (wave * TRANSFERS + i) / 2, x_tiles - 1) * a.blocks + 2 * first + (wave * TRANSFERS + i) % 2) * 1024;
     auto transfer = [&](int step, int i) {
-        if (step < steps && (XT * 2 % WAVES == 0 || wave * TRANSFERS + i < XT * 2))   // uniform
-            quad_to_lds(stretch(xs[i], 0x7FFFFFFF), lds + step % STAGES * STAGE + (wave * TRANSFERS + i) * 1024, lane * 16, step * 2048);
+        if (XT * 2 % WAVES == 0 || wave * TRANSFERS + i < XT * 2)   // uniform; what is asked for behind the last step is not there, so no load needs a branch
+            quad_to_lds(stretch(xs[i], 2048 * steps - 1024), lds + step % STAGES * STAGE + (wave * TRANSFERS + i) * 1024, lane * 16, step * 2048);
     };
     Stretch ws[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
-        ws[j] = stretch(a.packed + ((size_t)min(bn * WT + wn * NT + j, w_tiles - 1) * a.blocks + 2 * first) * 1024, 0x7FFFFFFF);
+        ws[j] = stretch(a.packed + ((size_t)min(bn * WT + wn * NT + j, w_tiles - 1) * a.blocks + 2 * first) * 1024, 2048 * steps);
     int4v wf[RING][NT];
     auto fetch = [&](int half, int j) {
-        return __builtin_bit_cast(int4v, __builtin_amdgcn_raw_buffer_load_b128(ws[j], lane * 16, min(half, 2 * steps - 1) * 1024, WM == 1 ? kStreamed : 0));
+        return __builtin_bit_cast(int4v, __builtin_amdgcn_raw_buffer_load_b128(ws[j], lane * 16, half * 1024, WM == 1 ? kStreamed : 0));
     };
     int4v acc[MT][NT];
 #pragma unroll
@@ -252,43 +252,48 @@ __global__ __launch_bounds__(64 * WM * WN) void w8a8_tile_kernel(GemmArgs a)
     for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
         for (int j = 0; j < NT; ++j) wf[u][j] = fetch(u, j);
-    for (int step0 = 0; step0 < steps; step0 += UNROLL / 2) {
+    auto body = [&](int u, int step, auto last) __attribute__((always_inline)) {
+        // This step's activations have landed and the step before this one has been read.  Newer than they are the next step's activations and the
+        // weights asked for in three halves; those that the last steps would ask for the compiler leaves out.
+        constexpr int NEWER = TRANSFERS + (decltype(last)::value ? 0 : NT * (AHEAD > 2 ? 3 : AHEAD));
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NEWER) : "memory");
+        const uint8_t *const stage = lds + step % STAGES * STAGE;
 #pragma unroll
-        for (int u = 0; u < UNROLL; u += 2) {
-            const int step = step0 + u / 2;
-            if (step >= steps) break;   // uniform
-            // This step's activations have landed and the step before this one has been read.  Newer than they are the weights asked for in three
-            // halves and the next step's activations (which are not there behind the last).
-            if (step + 1 < steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(TRANSFERS + NT * (AHEAD > 2 ? 3 : AHEAD)) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            const uint8_t *const stage = lds + step % STAGES * STAGE;
+        for (int half = 0; half < 2; ++half) {
+            int4v xf[MT];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                int4v xf[MT];
+            for (int i = 0; i < MT; ++i) xf[i] = *reinterpret_cast<const int4v *>(stage + ((wm * MT + i) * 2 + half) * 1024 + lane * 16);
+            // Loads go out between the products: a compute unit takes 64 bytes a clock, and a wavefront that asks for all at once stands still meanwhile.
+            // Activations first (the wait above counts on it).
+            constexpr int HERE = (TRANSFERS + 1) / 2, LOADS = HERE + NT, GAP = MT * NT / LOADS > 0 ? MT * NT / LOADS : 1;
+            auto load = [&](int n) {
+                if (n < HERE) {
+                    if (half * HERE + n < TRANSFERS) transfer(step + 2, half * HERE + n);
+                } else if (n < LOADS) wf[(u + half + AHEAD) % RING][n - HERE] = fetch(2 * step + half + AHEAD, n - HERE);
+                __builtin_amdgcn_sched_barrier(0);
+            };
 #pragma unroll
-                for (int i = 0; i < MT; ++i) xf[i] = *reinterpret_cast<const int4v *>(stage + ((wm * MT + i) * 2 + half) * 1024 + lane * 16);
-                // Loads go out between the products: a compute unit takes 64 bytes a clock, and a wavefront that asks for all at once stands still meanwhile.
-                // Activations first (the wait above counts on it).
-                constexpr int HERE = (TRANSFERS + 1) / 2, LOADS = HERE + NT, GAP = MT * NT / LOADS > 0 ? MT * NT / LOADS : 1;
-                auto load = [&](int n) {
-                    if (n < HERE) {
-                        if (half * HERE + n < TRANSFERS) transfer(step + 2, half * HERE + n);
-                    } else if (n < LOADS) wf[(u + half + AHEAD) % RING][n - HERE] = fetch(2 * step + half + AHEAD, n - HERE);
-                    __builtin_amdgcn_sched_barrier(0);
-                };
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int j = 0; j < NT; ++j) {
+                    const int at = i * NT + j;
+                    if (at % GAP == 0 && at / GAP < LOADS) load(at / GAP);
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[(u + half) % RING][j], xf[i], acc[i][j], 0, 0, 0);
+                }
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) {
-                        const int at = i * NT + j;
-                        if (at % GAP == 0 && at / GAP < LOADS) load(at / GAP);
-                        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[(u + half) % RING][j], xf[i], acc[i][j], 0, 0, 0);
-                    }
-#pragma unroll
-                for (int n = (MT * NT + GAP - 1) / GAP; n < LOADS; ++n) load(n);
-            }
+            for (int n = (MT * NT + GAP - 1) / GAP; n < LOADS; ++n) load(n);
         }
+    };
+    int step0 = 0;
+    for (; step0 + UNROLL / 2 <= steps; step0 += UNROLL / 2)
+#pragma unroll
+        for (int u = 0; u < UNROLL; u += 2) body(u, step0 + u / 2, std::false_type{});
+#pragma unroll
+    for (int u = 0; u < UNROLL - 2; u += 2) {
+        if (step0 + u / 2 >= steps) break;   // uniform
+        body(u, step0 + u / 2, std::true_type{});
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is under way into LDS behind this
     if (a.splits > 1) {
         constexpr int QUADS = WAVES * MT * NT * 64;   // of a workgroup's sums
         const PartialBuffer mine = partial_buffer(a.partials + ((size_t)place * a.splits + split) * QUADS * 4);
@@ -479,12 +484,13 @@ static int launch_tile(GemmArgs a, const GemmPlan &p, hipStream_t stream)
 }
 
 // The kernels, by measurement over 28 shapes (M 1 .. 4096, N 1024 .. 28672, K 4096 .. 14336), us:
-//   up to 16 tokens, and up to 64 where k is short, the stream kernel: 60 tokens 4096 -> 4096 7.5 (tiles of 64 x 128, walk shared by four, 13.6), 8192 -> 8192 17.2
-//   (22.1); with many channels or a long k its wavefronts' own copies of the activations cost more than an exchange: 60 tokens 4096 -> 28672 30.8 (24.7),
-//   14336 -> 4096 21.9 (19.6).  Two tiles of channels to a wavefront where that still fills the chip: 60 tokens 8192 -> 8192 23.8 with one
-//   up to 128 tokens tiles of 64 x 128 with a shared walk unless 128 x 128 fill the chip: 100 tokens 4096 -> 4096 12.5 (13.8)
+//   up to 16 tokens, and up to 64 where k is short, the stream kernel: 60 tokens 4096 -> 4096 7.1 (tiles of 64 x 128, walk shared by four, 10.6), 8192 -> 8192 16.8
+//   (20.6); with many channels or a long k its wavefronts' own copies of the activations cost more than an exchange: 60 tokens 4096 -> 28672 30.1 (21.7),
+//   14336 -> 4096 20.0 (18.4).  Two tiles of channels to a wavefront where that still fills the chip: 60 tokens 8192 -> 8192 23.8 with one
+//   up to 128 tokens tiles of 64 x 128 with a shared walk unless 128 x 128 fill the chip: 100 tokens 4096 -> 4096 11.3 (16.5), 128 tokens 4096 -> 28672 35.9 (33.8)
 //   more: of 256 x 256, 128 x 256 and 128 x 128 the one that takes the shortest time by its rounds over 256 compute units, a step of 128 values of k in
-//   1.66, 1.02 and 0.54 us: 4096 tokens 4096 -> 4096 59, 74 and 74; 777 tokens 8192 -> 8192 73, 61 and 74; 1024 tokens 4096 -> 4096 -, 29 and 23
+//   1.64, 0.91 and 0.5 us and 4 us to begin and end a round: 4096 tokens 4096 -> 4096 61, 77 and 84; 777 tokens 8192 -> 8192 85, 59 and 69; 1024 tokens
+//   4096 -> 4096 -, 33 and 22
 enum { kStream = 0, kTile64x128, kTile128x128, kTile128x256, kTile256x256 };
 
 static GemmPlan gemm_plan(int M, int N, int K)
@@ -498,11 +504,11 @@ static GemmPlan gemm_plan(int M, int N, int K)
     if (M <= 16 || (M <= 64 && K <= 8192 && tiles(64, 128) < 192)) return {kStream, 16 * (M <= 16 ? 1 : M <= 32 ? 2 : 4), M > 16 && N >= 6144 ? 32 : 16, 1};
     if (M <= 64 || (M <= 128 && tiles(128, 128) < 160)) return shared(kTile64x128, 64, 128);
     const GemmPlan whole[3] = {{kTile256x256, 256, 256, 1}, {kTile128x256, 128, 256, 1}, {kTile128x128, 128, 128, 1}};
-    const int step_ns[3] = {1660, 1020, 540};
+    const int step_ns[3] = {1640, 910, 500}, round_ns = 4000;
     GemmPlan best = shared(kTile128x128, 128, 128);
-    long long least = best.splits > 1 ? (steps + best.splits - 1) / best.splits * step_ns[2] + 6000 : 1ll << 62;   // the exchange takes 6 us
+    long long least = best.splits > 1 ? (steps + best.splits - 1) / best.splits * step_ns[2] + round_ns + 6000 : 1ll << 62;   // the exchange takes 6 us
     for (int i = 0; i < 3; ++i) {
-        const long long ns = (tiles(whole[i].rows, whole[i].cols) + 255) / 256 * steps * step_ns[i];
+        const long long ns = (tiles(whole[i].rows, whole[i].cols) + 255) / 256 * (steps * step_ns[i] + round_ns);
         if (ns < least) least = ns, best = whole[i];
     }
     return best;
