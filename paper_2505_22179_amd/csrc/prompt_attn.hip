@@ -764,50 +764,52 @@ __global__ __launch_bounds__(512) void prompt_attn_few_kernel(PromptArgs a)
     go_through<D, ROWS, KEYS, 512, 64 * NW, true>(a, tid, reinterpret_cast<float *>(lds), [&](const Sequence &s, const Piece &p, bool whole, unsigned slot) {
         const uint8_t *const k_src = reinterpret_cast<const uint8_t *>(a.k) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
         const uint8_t *const v_src = reinterpret_cast<const uint8_t *>(a.v) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
-        auto request = [&](int step, const uint8_t *src, uint8_t *tile, bool values) {
-            const int key0 = step * KEYS;
-            const Stretch from = stretch(src + (size_t)key0 * stride, 0x7FFFFFFF);
+        // what lies behind the sequence's last key or behind the piece is not read (the former is masked wherever it could count)
+        uint32_t k_lane[2], v_lane[2];
 #pragma unroll
-            for (int i = 0; i < TRANSFERS; ++i) {
-                const int row = i * PER + trow, chunk = values ? tchunk ^ (2 * row & (CHUNKS - 1)) : tchunk ^ (row & 7);
-                quad_to_lds(from, tile + i * 1024, (uint32_t)min(row, s.T - 1 - key0) * stride + (chunk << 4), 0);   // rows beyond the last key repeat it; they are masked
-            }
+        for (int odd = 0; odd < 2; ++odd) {
+            const int row = odd * PER + trow;
+            k_lane[odd] = trow * stride + ((tchunk ^ (row & 7)) << 4);
+            v_lane[odd] = trow * stride + ((tchunk ^ (2 * row & (CHUNKS - 1))) << 4);
+        }
+        auto request = [&](int step, const uint8_t *src, uint8_t *tile, const uint32_t (&at)[2]) {
+            const long long key0 = (long long)step * KEYS;
+            const uint32_t bytes = step < p.s1 ? (uint32_t)min((s.T - 1 - key0) * stride + ROW, 0x7FFFFFFFll) : 0;
+            const Stretch from = stretch(src + (size_t)key0 * stride, bytes);
+#pragma unroll
+            for (int i = 0; i < TRANSFERS; ++i) quad_to_lds(from, tile + i * 1024, at[i & 1], (uint32_t)(i * PER) * stride);
         };
         Rows<D> rows;
         rows.start(a, s, p, c, h);
         __builtin_amdgcn_sched_barrier(0);   // Q before K before V: the waits count on it
         int step = p.s0 + wave;
-        if (step < p.s1) {
-            request(step, k_src, ktile, false);
-            __builtin_amdgcn_sched_barrier(0);
-            request(step, v_src, vtile, true);
-        }
+        request(step, k_src, ktile, k_lane);
+        __builtin_amdgcn_sched_barrier(0);
+        request(step, v_src, vtile, v_lane);
         __builtin_amdgcn_sched_barrier(0);
         rows.arrive();
-        const int all_see = s.T - s.n + p.first / a.group + 1;
-        while (step < p.s1) {   // uniform over the wavefront
-            const int next = step + NW;
-            const bool more = next < p.s1;
+        const int all_see = s.T - s.n + p.first / a.group + 1, open = min(all_see / KEYS, p.s1);
+        auto body = [&](auto masked) {
+            constexpr bool MASKED = decltype(masked)::value;
+            const int next = step + NW, key0 = step * KEYS;
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TRANSFERS) : "memory");   // K of this step; its V is newer
-            const int key0 = step * KEYS;
-            const bool all = key0 + KEYS <= all_see;
             float16v sc[1];
             half8v pb[2];
             half8v kf[D / 16];
             rows.read_keys(kf, ktile, kfrag);
             rows.scores(sc[0], kf);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the K tile has been read
-            if (more) request(next, k_src, ktile, false);
-            if (all) rows.template softmax<1, false>(sc, pb, key0, a.scale_log2e, h);
-            else rows.template softmax<1, true>(sc, pb, key0, a.scale_log2e, h);
-            if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TRANSFERS) : "memory");   // V of this step; the next K is newer
-            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            if (all) rows.template values<1, false>(pb, vtile, key0, h, vfrag);
-            else rows.template values<1, true>(pb, vtile, key0, h, vfrag);
+            request(next, k_src, ktile, k_lane);
+            rows.template softmax<1, MASKED>(sc, pb, key0, a.scale_log2e, h);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TRANSFERS) : "memory");   // V of this step; the next K is newer
+            rows.template values<1, MASKED>(pb, vtile, key0, h, vfrag);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the V tile has been read
-            if (more) request(next, v_src, vtile, true);
+            request(next, v_src, vtile, v_lane);
             step = next;
-        }
+        };
+        while (step < open) body(std::false_type{});
+        while (step < p.s1) body(std::true_type{});
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is under way into the tiles behind this
         // the states of the wavefronts meet in LDS
         const float l_run = rows.l_run + __shfl_xor(rows.l_run, 32, 64);
         __syncthreads();   // every wavefront has left its tiles
