@@ -59,7 +59,8 @@ size_t w4a16_packed_bytes(int N, int K, int G);
 size_t w4a16_workspace_bytes(int M_max, int N, int K, int G);
 
 /* Zero the ticket area at the start of a workspace.  Must be enqueued once before the first call that uses the buffer
- * and needs its tickets: w4a16_gemm and its fused forms, w4a16_decoder_layer, tree_verify_attn, tree_verify_attn_kv8, lm_head_sample.
+ * and needs its tickets: w4a16_gemm and its fused forms, w4a16_decoder_layer, tree_verify_attn, tree_verify_attn_kv8, lm_head_sample,
+ * w4a16_prompt_attn, and w8a8_gemm and w8a8_linear of the library beside this one.
  * Each of those calls leaves the tickets zero again and lm_head_topk leaves them alone (in a workspace of its stated size), so one
  * initialisation serves any number of later calls (of any kind and shape that fits).  Two
  * calls that may run concurrently must not share a workspace.  A workspace must be 256-byte aligned
