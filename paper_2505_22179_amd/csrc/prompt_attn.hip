@@ -880,16 +880,16 @@ static PromptPlan prompt_plan(int rows, int B, int max_q, int max_k, int Hq, int
     p.rows = kFewRows;
     p.cut = true;
     if (!p.few) {
-        // Whole tiles of 256 rows (a step of 64 keys takes 2.15 us), of 128, two to a compute unit (1.35 us alone, 2.15 with a neighbour), or tiles of 256 cut
-        // into equal stretches (40 us more for pieces written, read and joined): the shortest by these times, were all sequences as long as the longest.
-        // 32/8 heads: 1024 queries 38, 31 us and - ; 2048 queries -, 61 and 90; 4 x 64 queries behind 2936 keys -, 69 and 58; 4096 queries 156, 166 and -.
+        // Whole tiles of 128 rows, two and more to a compute unit (D 128: a step of 64 keys takes 1.35 us alone, 1.65 with a neighbour, a round of many 2.15), or
+        // of 256 where prompts are long and workgroups many and D is 128: 4096 queries, 32/8 heads 152 us (128 rows: 161), 16384 2131 (2219), but 16 x 1000, 16/16 heads
+        // 168 (130), 8 prompts of up to 1500, 64/8 heads 162 (153); D 64, 4096 queries 109 (101), 24 prompts of up to 700, 28/4 heads 59 (47).
+        // Few tiles behind many keys are cut into equal stretches (40 us more for pieces written, read and joined) where that is shorter, were all sequences as
+        // long as the longest: 4 x 64 queries behind 2936 keys, 32/8 heads 58 us (whole 69); 2048 queries 90 (59).
         const long long steps = (max_k + 63) / 64, part = max_q >= max_k ? 1 : 2;   // a whole prompt's rows see half of its keys on average
-        const long long high = tiles_of(256) * Hkv, low = tiles_of(128) * Hkv;
-        const long long whole = high <= 256 ? steps * 2150 : (high + 255) / 256 * steps * part * 1075;
-        const long long halves = low <= 256 ? steps * 1350 : low <= 512 ? steps * 2150 : (low + 511) / 512 * steps * part * 1075;
-        const long long cut = high * steps * part * 1075 / 256 + 40000;
-        p.cut = cut < whole && cut < halves;
-        p.rows = !p.cut && halves < whole ? 128 : 256;
+        const long long high = tiles_of(256) * Hkv, low = tiles_of(128) * Hkv, of_size = D == 128 ? 100 : 62;
+        const long long halves = steps * of_size * (low <= 256 ? 1350 : 1650) / 100, cut = high * steps * part * of_size * 1075 / 256 / 100 + 40000;
+        p.cut = low <= 512 && cut < halves;
+        p.rows = p.cut || (D == 128 && high >= 512 && (long long)rows * group >= 16384ll * B) ? 256 : 128;
     }
     const long long tiles = tiles_of(p.rows);
     if (p.cut) {   // no more workgroups than there can be work for, were every sequence as long as the longest
