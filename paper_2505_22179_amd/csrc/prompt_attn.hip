@@ -375,15 +375,24 @@ __device__ __forceinline__ uint32_t v_fragment(int lane)
     return Tile<D>::v_place(key, 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + 8 * (lane & 1);
 }
 
-__device__ __forceinline__ void store_row_quad(const PromptArgs &a, const Sequence &s, const Piece &p, int row, int D, int d, float4v val, float l)
+// where a row's output belongs, and what its sum of weighted values is to be multiplied by: a row that sees no key gets zeros; one whose scores are
+// all -inf 0 / 0
+__device__ __forceinline__ _Float16 *row_of(const PromptArgs &a, const Sequence &s, const Piece &p, int row, int D)
 {
     const int pair = p.first + row, query = pair / a.group;
-    // a row that sees no key gets zeros; one whose scores are all -inf 0 / 0
-    const float inv = s.T - s.n + query >= 0 ? 1.f / l : 0.f;
+    return a.out + ((size_t)(s.q0 + query) * a.Hq + p.kvh * a.group + (pair - query * a.group)) * D;
+}
+__device__ __forceinline__ float row_factor(const PromptArgs &a, const Sequence &s, const Piece &p, int row, float l)
+{
+    return s.T - s.n + (p.first + row) / a.group >= 0 ? 1.f / l : 0.f;
+}
+__device__ __forceinline__ void store_row_quad(const PromptArgs &a, const Sequence &s, const Piece &p, int row, int D, int d, float4v val, float l)
+{
+    const float inv = row_factor(a, s, p, row, l);
     half4v y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = (_Float16)(val[e] * inv);
-    *reinterpret_cast<half4v *>(a.out + ((size_t)(s.q0 + query) * a.Hq + p.kvh * a.group + (pair - query * a.group)) * D + d) = y;
+    *reinterpret_cast<half4v *>(row_of(a, s, p, row, D) + d) = y;
 }
 
 // Where the piece of a cut tile goes: workgroup i keeps the tile that its stretch begins in at 2 i, the one that it ends in at 2 i + 1.
@@ -717,21 +726,40 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
         for (; step < open; ++step) body(step, std::false_type{});
         for (; step < p.s1; ++step) body(step, std::true_type{});
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is under way into the buffers behind this
+        const float l = rows.l_run + __shfl_xor(rows.l_run, 32, 64);
+        if (whole) {
+            // through LDS, so that rows leave in pieces of 16 bytes next to each other
+            constexpr int OUT_ROW = ROW + 16;   // rows lie 16 bytes apart from the banks of the last
+            uint8_t *const own = lds + wave * 32 * OUT_ROW;
+            const float inv = row_factor(a, s, p, wave * 32 + c, l);
+            __syncthreads();   // every wavefront has left the last tile
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    half4v y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = (_Float16)(rows.o[dt][4 * g + e] * inv);
+                    *reinterpret_cast<half4v *>(own + c * OUT_ROW + (32 * dt + 8 * g + 4 * h) * 2) = y;
+                }
+#pragma unroll
+            for (int i = 0; i < 32 / PER; ++i) {
+                const int r = i * PER + trow;
+                if (wave * 32 + r < p.rows) *reinterpret_cast<half8v *>(row_of(a, s, p, wave * 32 + r, D) + 8 * tchunk) = read_chunk(own + r * OUT_ROW + 16 * tchunk);
+            }
+            return;
+        }
         // a piece is read by another kernel: plain stores, whose lines the L2 puts together (written through, 32 bytes at a time, 128 KB took 20 us and more)
         float *const po = a.part_o + (size_t)slot * ROWS * D, *const pm = a.part_ml + (size_t)slot * ROWS * 2;
-        const float l = rows.l_run + __shfl_xor(rows.l_run, 32, 64);
         const int row = wave * 32 + c;
         if (row < p.rows) {
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float4v val = {rows.o[dt][4 * g], rows.o[dt][4 * g + 1], rows.o[dt][4 * g + 2], rows.o[dt][4 * g + 3]};
-                    const int d = 32 * dt + 8 * g + 4 * h;
-                    if (whole) store_row_quad(a, s, p, row, D, d, val, l);
-                    else *reinterpret_cast<float4v *>(po + row * D + d) = val;
-                }
-            if (!whole && h == 0) {
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<float4v *>(po + row * D + 32 * dt + 8 * g + 4 * h) =
+                        (float4v){rows.o[dt][4 * g], rows.o[dt][4 * g + 1], rows.o[dt][4 * g + 2], rows.o[dt][4 * g + 3]};
+            if (h == 0) {
                 pm[2 * row] = rows.m_run;
                 pm[2 * row + 1] = l;
             }
