@@ -205,6 +205,13 @@ __device__ __forceinline__ half4v read_transposed(const uint8_t *p)
     return __builtin_bit_cast(half4v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)p));
 }
 __device__ __forceinline__ bool not_finite(_Float16 x) { return (__builtin_bit_cast(uint16_t, x) & 0x7C00u) == 0x7C00u; }
+// one of eight: an exponent of all ones, and no other, carries into the bit of the sign
+__device__ __forceinline__ bool not_finite(half8v x)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const u32x4 b = (__builtin_bit_cast(u32x4, x) & 0x7FFF7FFFu) + 0x04000400u;
+    return ((b[0] | b[1] | b[2] | b[3]) & 0x80008000u) != 0;
+}
 
 // Chunks of sixteen bytes lie permuted in the LDS tiles, so that fragment reads spread over the banks.
 template <int D>
@@ -662,6 +669,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
     constexpr int TRANSFERS = TILE / 1024 / NW;      // of a wavefront, K and V each
     static_assert(TRANSFERS >= 1, "");
     extern __shared__ float4v smem4[];
+    __shared__ uint32_t bad_sh[2];   // mark() of a step with such values; never cleared: one that lies there by chance costs time only
+    auto mark = [](int step) { return 0x9E3779B1u * (uint32_t)(step + 1); };
     uint8_t *const lds = reinterpret_cast<uint8_t *>(smem4);   // STAGES times K, V
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, c = lane & 31;
@@ -695,6 +704,22 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
                 quad_to_lds(vs, tile + TILE + t * 1024, v_lane[t & 1], (uint32_t)(t * PER) * stride);
             }
         };
+        // What a row does not see may be anything, and 0 times it need not be 0: a step that is masked looks its values over first, each wavefront those that it
+        // brought.  If there is one that is not finite, it joins the sums of the rows that see it and is cleared (looked for where the fragments are read, by every
+        // wavefront, it took 24 prompts of 200 tokens, 32/8 heads 41 us).
+        auto any_not_finite = [&](const uint8_t *vtile) {
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i < TRANSFERS; ++i) found |= not_finite(read_chunk(vtile + (wave * TRANSFERS + i) * 1024 + lane * 16));
+            return found;
+        };
+        auto clear_not_finite = [&](uint8_t *vtile) {
+            for (int i = 0; i < TRANSFERS; ++i) {
+                half8v *const x = reinterpret_cast<half8v *>(vtile + (wave * TRANSFERS + i) * 1024 + lane * 16);
+                for (int e = 0; e < 8; ++e)
+                    if (not_finite((*x)[e])) (*x)[e] = 0;
+            }
+        };
         Rows<D> rows;
         rows.start(a, s, p, wave * 32 + c, h);
         if (p.s0 < p.s1) {
@@ -707,10 +732,14 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
         const int all_see = s.T - s.n + p.first / a.group + 1, open = min(all_see / KEYS, p.s1);
         auto body = [&](int step, auto masked) {
             constexpr bool MASKED = decltype(masked)::value;
+            uint8_t *const ktile = stage(step), *const vtile = ktile + TILE;
             // this tile has landed (those asked for after it need not have), and the one before it has been read
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * TRANSFERS * (STAGES - 2)) : "memory");
+            if constexpr (MASKED) {
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * TRANSFERS * (STAGES - 2)) : "memory");
+                if (__any(any_not_finite(vtile))) bad_sh[step & 1] = mark(step);
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            } else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * TRANSFERS * (STAGES - 2)) : "memory");
             request(step + STAGES - 1);
-            const uint8_t *const ktile = stage(step);
             float16v sc[KT];
             half8v pb[2 * KT];
 #pragma unroll
@@ -720,7 +749,14 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
                 rows.scores(sc[kt], kf);
             }
             rows.template softmax<KT, MASKED>(sc, pb, step * KEYS, a.scale_log2e, h);
-            rows.template values<KT, MASKED>(pb, ktile + TILE, step * KEYS, h, vfrag);
+            if constexpr (MASKED)
+                if (bad_sh[step & 1] == mark(step)) {   // uniform over the workgroup
+                    rows.template add_not_finite<KT>(vtile, step * KEYS, h);
+                    __syncthreads();
+                    clear_not_finite(vtile);
+                    __syncthreads();
+                }
+            rows.template values<KT, false>(pb, vtile, step * KEYS, h, vfrag);
         };
         int step = p.s0;
         for (; step < open; ++step) body(step, std::false_type{});
