@@ -317,22 +317,13 @@ struct Rows {
     }
 
     // fragments u of the V tile: 16 keys, all D values
-    template <bool MASKED>
-    __device__ __forceinline__ static void read_values(half8v (&vf)[D / 32], bool &bad, const uint8_t *vtile, int u, uint32_t vfrag)
+    __device__ __forceinline__ static void read_values(half8v (&vf)[D / 32], const uint8_t *vtile, int u, uint32_t vfrag)
     {
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) {
             const uint8_t *const p = vtile + u * 16 * Tile<D>::ROW + (vfrag ^ (dt << 6));
             const half4v lo = read_transposed(p), hi = read_transposed(p + 8 * Tile<D>::ROW);
             vf[dt] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            if constexpr (MASKED) {   // what a row does not see may be anything: 0 times it need not be 0
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool b = not_finite(vf[dt][e]);
-                    bad |= b;
-                    vf[dt][e] = b ? (_Float16)0 : vf[dt][e];
-                }
-            }
         }
     }
     __device__ __forceinline__ void add_product(const half8v (&vf)[D / 32], half8v pb)
@@ -357,22 +348,38 @@ struct Rows {
                             for (int e = 0; e < 4; ++e) o[dt][4 * quad + e] += not_finite(x[e]) ? (float)x[e] : 0.f;
             }
     }
-    template <int KT, bool MASKED>
-    __device__ __forceinline__ void values(const half8v (&pb)[2 * KT], const uint8_t *vtile, int key0, int h, uint32_t vfrag)
+    template <int KT>
+    __device__ __forceinline__ void values(const half8v (&pb)[2 * KT], const uint8_t *vtile, uint32_t vfrag)
     {
-        bool bad = false;
         half8v vf[2][D / 32];
-        read_values<MASKED>(vf[0], bad, vtile, 0, vfrag);
+        read_values(vf[0], vtile, 0, vfrag);
 #pragma unroll
         for (int u = 0; u < 2 * KT; ++u) {
-            if (u + 1 < 2 * KT) read_values<MASKED>(vf[(u + 1) & 1], bad, vtile, u + 1, vfrag);
+            if (u + 1 < 2 * KT) read_values(vf[(u + 1) & 1], vtile, u + 1, vfrag);
             add_product(vf[u & 1], pb[u]);
         }
         settled(o[D / 32 - 1]);   // the branches behind this go round too little for the last product
-        if constexpr (MASKED)
-            if (__any(bad)) add_not_finite<KT>(vtile, key0, h);
     }
 };
+
+// values that a wavefront brought to LDS, 1 KB N times: is one of them not finite (this lane's share); and zeros in the place of those
+template <int N>
+__device__ __forceinline__ bool any_not_finite(const uint8_t *at, int lane)
+{
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) found |= not_finite(read_chunk(at + i * 1024 + lane * 16));
+    return found;
+}
+template <int N>
+__device__ __forceinline__ void clear_not_finite(uint8_t *at, int lane)
+{
+    for (int i = 0; i < N; ++i) {
+        half8v *const x = reinterpret_cast<half8v *>(at + i * 1024 + lane * 16);
+        for (int e = 0; e < 8; ++e)
+            if (not_finite((*x)[e])) (*x)[e] = 0;
+    }
+}
 
 // V: lane s of 16-lane block b points at key row 4 (b / 2) + s / 4 (and 8 further on), elements 32 dt + 16 (b % 2) + 4 (s % 4) ..
 template <int D>
@@ -707,19 +714,6 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
         // What a row does not see may be anything, and 0 times it need not be 0: a step that is masked looks its values over first, each wavefront those that it
         // brought.  If there is one that is not finite, it joins the sums of the rows that see it and is cleared (looked for where the fragments are read, by every
         // wavefront, it took 24 prompts of 200 tokens, 32/8 heads 41 us).
-        auto any_not_finite = [&](const uint8_t *vtile) {
-            bool found = false;
-#pragma unroll
-            for (int i = 0; i < TRANSFERS; ++i) found |= not_finite(read_chunk(vtile + (wave * TRANSFERS + i) * 1024 + lane * 16));
-            return found;
-        };
-        auto clear_not_finite = [&](uint8_t *vtile) {
-            for (int i = 0; i < TRANSFERS; ++i) {
-                half8v *const x = reinterpret_cast<half8v *>(vtile + (wave * TRANSFERS + i) * 1024 + lane * 16);
-                for (int e = 0; e < 8; ++e)
-                    if (not_finite((*x)[e])) (*x)[e] = 0;
-            }
-        };
         Rows<D> rows;
         rows.start(a, s, p, wave * 32 + c, h);
         if (p.s0 < p.s1) {
@@ -736,7 +730,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
             // this tile has landed (those asked for after it need not have), and the one before it has been read
             if constexpr (MASKED) {
                 asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * TRANSFERS * (STAGES - 2)) : "memory");
-                if (__any(any_not_finite(vtile))) bad_sh[step & 1] = mark(step);
+                if (__any(any_not_finite<TRANSFERS>(vtile + wave * TRANSFERS * 1024, lane))) bad_sh[step & 1] = mark(step);
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             } else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * TRANSFERS * (STAGES - 2)) : "memory");
             request(step + STAGES - 1);
@@ -753,10 +747,10 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
                 if (bad_sh[step & 1] == mark(step)) {   // uniform over the workgroup
                     rows.template add_not_finite<KT>(vtile, step * KEYS, h);
                     __syncthreads();
-                    clear_not_finite(vtile);
+                    clear_not_finite<TRANSFERS>(vtile + wave * TRANSFERS * 1024, lane);
                     __syncthreads();
                 }
-            rows.template values<KT, false>(pb, vtile, step * KEYS, h, vfrag);
+            rows.template values<KT>(pb, vtile, vfrag);
         };
         int step = p.s0;
         for (; step < open; ++step) body(step, std::false_type{});
@@ -866,7 +860,13 @@ __global__ __launch_bounds__(512) void prompt_attn_few_kernel(PromptArgs a)
             request(next, k_src, ktile, k_lane);
             rows.template softmax<1, MASKED>(sc, pb, key0, a.scale_log2e, h);
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TRANSFERS) : "memory");   // V of this step; the next K is newer
-            rows.template values<1, MASKED>(pb, vtile, key0, h, vfrag);
+            if constexpr (MASKED)
+                if (__any(any_not_finite<TRANSFERS>(vtile, lane))) {
+                    rows.template add_not_finite<1>(vtile, key0, h);
+                    clear_not_finite<TRANSFERS>(vtile, lane);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                }
+            rows.template values<1>(pb, vtile, vfrag);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the V tile has been read
             request(next, v_src, vtile, v_lane);
             step = next;
