@@ -237,3 +237,19 @@ def test_operands_that_arrive_late(M, N, K):
         if first is None:
             first = y
         assert torch.equal(y, first), call
+
+
+@pytest.mark.parametrize("pre", [B.W8A8_PLAIN, B.W8A8_RMS_NORM, B.W8A8_SILU_MUL])
+def test_rows_are_quantised_alike_however_many_they_are(pre):
+    M, K = 530, 9216
+    x = np.random.default_rng(3).standard_normal((M, K * (2 if pre == B.W8A8_SILU_MUL else 1))).astype(np.float16)
+    gamma = I.make_gamma(4, K) if pre == B.W8A8_RMS_NORM else None
+    codes, scale = quantised(x, pre, gamma, 1e-5, M, K)
+    few, few_scale = quantised(x[:32], pre, gamma, 1e-5, 32, K)
+    plain, some = plain_codes(codes, M, K), plain_codes(few, 32, K)
+    if pre != B.W8A8_RMS_NORM:   # its sum of squares is taken in another order
+        np.testing.assert_array_equal(plain[:32], some)
+        np.testing.assert_array_equal(scale[:32], few_scale)
+    exact = R.w8a8_input(x, pre, gamma, 1e-5)   # bounds as in the other tests of codes
+    near = (2.0 ** -11 + (2.0 ** -16 if pre else 0.0)) * np.abs(exact) + 2.0 ** -25
+    assert (np.abs(plain * scale[:, None].astype(np.float64) - exact) <= scale[:, None].astype(np.float64) / 2 * (1 + 1e-12) + near).all()
