@@ -4,10 +4,10 @@
 // tile of rows spans few queries and the keys it sees end almost together.  S^T = K . Q^T leaves a lane with scores of ONE pair (column
 // lane % 32), which are the operand of O^T += V^T . P^T as they stand; the softmax runs in registers, one pass over the keys.
 //
-// Lengths are known on the device only, so the work is dealt out there: the tiles of all sequences and KV heads, each as long as the keys that
-// it sees, lie end to end, and every workgroup takes an equal stretch of that line.  A tile that a border falls into is cut there, and the
-// last of its workgroups to finish joins the pieces (exchange as in tree_attn_kernel; a border cuts one tile, so the tickets of the
-// workgroups do for the tiles).
+// Lengths are known on the device only, so the work is dealt out there.  Where there are tiles enough, each workgroup takes one.  Where there are few,
+// the tiles of all sequences and KV heads, each as long as the keys that it sees, lie end to end, and every workgroup takes an equal stretch of that
+// line.  A tile that a border falls into is cut there; the pieces are joined by the last of their workgroups to finish (rows of single tokens;
+// exchange as in tree_attn_kernel; a border cuts one tile, so the tickets of the workgroups do for the tiles) or by a kernel of its own.
 #include "attn_common.h"
 
 namespace w4 {
@@ -40,9 +40,9 @@ __device__ __forceinline__ long long divide(long long a, long long b)
     return q + (left >= b) - (left < 0);
 }
 
-// What a piece costs beside its keys (places, first transfers, exchange), in keys: 6 us, in which 32 rows go through 256 keys and more, 256 rows
-// through 320.  Without it a stretch could hold dozens of short sequences: 16 of 1 .. 8192 keys, 32/8 heads, one query each, 179 us.
-constexpr int kPieceKeys = 256;
+// What a piece costs beside its keys (places, first transfers, exchange), in keys: 6 us and more, in which 32 or 256 rows go through some 300.  64 sequences of up to
+// 4096 keys, one query each, 32/8 heads: counted as 384 keys 36 us, as 256 44, 96 70; as 512 no less.
+constexpr int kPieceKeys = 384;
 
 // A sequence, and its place on the line of work.  Tile t of a KV head reaches from cost(t) to cost(t + 1): the keys that its last query sees, about,
 // and kPieceKeys, each counted `group` times: nothing is divided.
@@ -665,7 +665,10 @@ __device__ __forceinline__ void take_one(const PromptArgs &a, int lane, Work wor
     }
 }
 
-// Many rows: eight wavefronts of 32 rows each, keys through LDS in tiles of 64, one barrier per tile, four buffers: three tiles are under way.
+// Many rows: NW wavefronts of 32 rows each, keys through LDS in tiles of 64, one barrier per tile, STAGES buffers of which all but one are under way.
+// 16384 queries, 32/8 heads: 2130 us, 1030 TFLOP/s, matrix units busy 53 % of the cycles, LDS 53 %, vector units 45 %: a wavefront's products and its softmax
+// follow one another, and two wavefronts on a SIMD hide only part of one behind the other (products alone take 1460 us, the vector instructions alone
+// 1210).  Four wavefronts of 64 rows, halves of the wavefronts a phase apart, products and softmax of two tiles interleaved, priorities: 2190 to 2800.
 constexpr int kTileKeys = 64, kTileLeast = 1024;
 template <int D, int NW, int STAGES, bool CUT>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs a)
@@ -800,7 +803,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
 }
 
 // Few rows (single tokens of a batch): 32 rows, and eight wavefronts that each take every eighth step of 32 keys.  A wavefront shares no K or V tile,
-// so it brings them itself and meets the others only at the end of a piece: no barrier in the walk.
+// so it brings them itself and meets the others only at the end of a piece: no barrier in the walk.  Bound by the cache where it is long (16 x 8192 keys, 8 heads of
+// 128: 105 us, 5.1 TB/s), else by its chain: lengths, first tiles, meeting of the wavefronts, join (one of 8192 14 us, of 100 7.4).
 template <int D>
 __global__ __launch_bounds__(512) void prompt_attn_few_kernel(PromptArgs a)
 {
