@@ -47,7 +47,7 @@ size_t w8a8_workspace_bytes(int M, int N, int K);
 int w8a8_gemm(const void *codes, const float *scale, const void *packed, const float *w_scale, const void *residual, void *y, int M, int N, int K,
               void *workspace, size_t workspace_bytes, void *stream);
 
-/* w8a8_quantize into the workspace, then w8a8_gemm: the same results bit for bit. */
+/* w8a8_quantize into the workspace, then w8a8_gemm: the same results bit for bit.  x, too, may be y. */
 int w8a8_linear(const void *x, int pre, const void *gamma, float eps, const void *packed, const float *w_scale, const void *residual, void *y, int M,
                 int N, int K, void *workspace, size_t workspace_bytes, void *stream);
 

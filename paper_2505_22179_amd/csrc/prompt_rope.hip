@@ -135,6 +135,8 @@ struct Unit {
     }
 };
 
+// A workgroup per token; bound by the copy where there are many (8192 tokens, 64/8 heads of 128: 62 us in the kernel, 5.4 TB/s), by the launch where there are few
+// (16 tokens 3.6 us).
 template <int V, bool INTERLEAVED>
 __global__ __launch_bounds__(kRopeThreads) void rope_prompt_kernel(PromptRopeArgs a)
 {

@@ -656,7 +656,10 @@ int w8a8_linear(const void *x, int pre, const void *gamma, float eps, const void
     const GemmArgs a = {codes, (const uint8_t *)packed, scale, w_scale, (const _Float16 *)residual, (_Float16 *)y,
                         reinterpret_cast<float *>(codes + codes_bytes(M, K) + aligned256((size_t)M * 4)), (uint32_t *)workspace, M, N, k_blocks(K), 1,
                         (const _Float16 *)x, (const _Float16 *)gamma, eps, K};
-    if (M == 1 && K <= kFusedK) {
+    // in place the token has to be read before the first output is written
+    const uintptr_t x0 = (uintptr_t)x, y0 = (uintptr_t)y;
+    const bool apart = x0 + (size_t)K * (pre == W8A8_SILU_MUL ? 4 : 2) <= y0 || y0 + (size_t)N * 2 <= x0;
+    if (M == 1 && K <= kFusedK && apart) {
         auto *const kernel = pre == W8A8_PLAIN      ? &w8a8_stream_kernel<1, 1, W8A8_PLAIN, true>
                              : pre == W8A8_RMS_NORM ? &w8a8_stream_kernel<1, 1, W8A8_RMS_NORM, true>
                                                     : &w8a8_stream_kernel<1, 1, W8A8_SILU_MUL, true>;

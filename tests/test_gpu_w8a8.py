@@ -253,3 +253,14 @@ def test_rows_are_quantised_alike_however_many_they_are(pre):
     exact = R.w8a8_input(x, pre, gamma, 1e-5)   # bounds as in the other tests of codes
     near = (2.0 ** -11 + (2.0 ** -16 if pre else 0.0)) * np.abs(exact) + 2.0 ** -25
     assert (np.abs(plain * scale[:, None].astype(np.float64) - exact) <= scale[:, None].astype(np.float64) / 2 * (1 + 1e-12) + near).all()
+
+
+@pytest.mark.parametrize("M, K, pre", [(1, 512, B.W8A8_PLAIN), (1, 256, B.W8A8_SILU_MUL), (3, 512, B.W8A8_RMS_NORM), (70, 512, B.W8A8_PLAIN)])
+def test_input_in_place(M, K, pre):
+    lin = Linear(M + 5, M, 512, K, pre)
+    want = lin.linear()
+    buffer = torch.full((M + 1, 512), SENTINEL, dtype=torch.float16, device=DEV)
+    buffer[:M] = dev(lin.x)
+    B.w8a8_linear(buffer, pre, dev(lin.gamma), lin.eps, lin.packed(), dev(lin.t), None, buffer, M, 512, K, lin.workspace())
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(buffer[:M].cpu().numpy().view(np.uint16), want.view(np.uint16))
