@@ -213,12 +213,16 @@ __device__ __forceinline__ bool not_finite(half8v x)
     return ((b[0] | b[1] | b[2] | b[3]) & 0x80008000u) != 0;
 }
 
-// Chunks of sixteen bytes lie permuted in the LDS tiles, so that fragment reads spread over the banks.
+// Chunks of sixteen bytes lie permuted in the LDS tiles, so that fragment reads spread over the 64 banks (256 bytes, two rows of 64 values): sixteen lanes of a
+// K read take one chunk of sixteen keys, 32 of a V read four chunks of four keys.  With permutations of eight chunks and of pairs a quarter of all cycles went
+// to conflicts.
 template <int D>
 struct Tile {
     static constexpr int ROW = D * 2, CHUNKS = D / 8;
-    __device__ __forceinline__ static uint32_t k_place(int key, int chunk) { return (uint32_t)(key * ROW + ((chunk ^ (key & 7)) << 4)); }
-    __device__ __forceinline__ static uint32_t v_place(int key, int chunk) { return (uint32_t)(key * ROW + ((chunk ^ (2 * key & (CHUNKS - 1))) << 4)); }
+    __device__ __forceinline__ static int k_chunk(int key, int chunk) { return chunk ^ (D == 128 ? key & 15 : key >> 1 & 7); }
+    __device__ __forceinline__ static int v_chunk(int key, int chunk) { return chunk ^ (D == 128 ? 4 * key & 15 : 2 * key & 7); }
+    __device__ __forceinline__ static uint32_t k_place(int key, int chunk) { return (uint32_t)(key * ROW + (k_chunk(key, chunk) << 4)); }
+    __device__ __forceinline__ static uint32_t v_place(int key, int chunk) { return (uint32_t)(key * ROW + (v_chunk(key, chunk) << 4)); }
 };
 
 // 32 rows (pairs) of a wavefront, lane column c = lane % 32: queries, outputs so far and the running state of the softmax
@@ -666,9 +670,9 @@ __device__ __forceinline__ void take_one(const PromptArgs &a, int lane, Work wor
 }
 
 // Many rows: NW wavefronts of 32 rows each, keys through LDS in tiles of 64, one barrier per tile, STAGES buffers of which all but one are under way.
-// 16384 queries, 32/8 heads: 2130 us, 1030 TFLOP/s, matrix units busy 53 % of the cycles, LDS 53 %, vector units 45 %: a wavefront's products and its softmax
-// follow one another, and two wavefronts on a SIMD hide only part of one behind the other (products alone take 1460 us, the vector instructions alone
-// 1210).  Four wavefronts of 64 rows, halves of the wavefronts a phase apart, products and softmax of two tiles interleaved, priorities: 2190 to 2800.
+// 16384 queries, 32/8 heads: 2110 us, 1040 TFLOP/s at a clock that power holds at 1.8 GHz; matrix units busy 54 % of the cycles, vector units 45 %, LDS 28 %: a
+// wavefront's products and its softmax follow one another, and two wavefronts on a SIMD hide only part of one behind the other (products alone take
+// 1460 us, the vector instructions alone 1210).  Four wavefronts of 64 rows, halves of the wavefronts a phase apart, products and softmax of two tiles interleaved, priorities: 2190 to 2800.
 constexpr int kTileKeys = 64, kTileLeast = 1024;
 template <int D, int NW, int STAGES, bool CUT>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs a)
@@ -687,13 +691,12 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
     const uint32_t kfrag = Tile<D>::k_place(c, h), vfrag = v_fragment<D>(lane);
     const int trow = lane / CHUNKS, tchunk = lane % CHUNKS;
     const uint32_t stride = (uint32_t)a.Hkv * ROW;
-    static_assert(2 * PER % 8 == 0, "rows of transfers two apart lie alike");
-    uint32_t k_lane[2], v_lane[2];
+    uint32_t k_lane[TRANSFERS], v_lane[TRANSFERS];
 #pragma unroll
-    for (int odd = 0; odd < 2; ++odd) {
-        const int row = odd * PER + trow;
-        k_lane[odd] = trow * stride + ((tchunk ^ (row & 7)) << 4);
-        v_lane[odd] = trow * stride + ((tchunk ^ (2 * row & (CHUNKS - 1))) << 4);
+    for (int i = 0; i < TRANSFERS; ++i) {
+        const int row = (wave * TRANSFERS + i) * PER + trow;
+        k_lane[i] = trow * stride + (Tile<D>::k_chunk(row, tchunk) << 4);
+        v_lane[i] = trow * stride + (Tile<D>::v_chunk(row, tchunk) << 4);
     }
 
     auto work = [&](const Sequence &s, const Piece &p, bool whole, unsigned slot) {
@@ -710,8 +713,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
 #pragma unroll
             for (int i = 0; i < TRANSFERS; ++i) {
                 const int t = wave * TRANSFERS + i;
-                quad_to_lds(ks, tile + t * 1024, k_lane[t & 1], (uint32_t)(t * PER) * stride);
-                quad_to_lds(vs, tile + TILE + t * 1024, v_lane[t & 1], (uint32_t)(t * PER) * stride);
+                quad_to_lds(ks, tile + t * 1024, k_lane[i], (uint32_t)(t * PER) * stride);
+                quad_to_lds(vs, tile + TILE + t * 1024, v_lane[i], (uint32_t)(t * PER) * stride);
             }
         };
         // What a row does not see may be anything, and 0 times it need not be 0: a step that is masked looks its values over first, each wavefront those that it
@@ -827,19 +830,19 @@ __global__ __launch_bounds__(512) void prompt_attn_few_kernel(PromptArgs a)
         const uint8_t *const k_src = reinterpret_cast<const uint8_t *>(a.k) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
         const uint8_t *const v_src = reinterpret_cast<const uint8_t *>(a.v) + ((size_t)s.k0 * a.Hkv + p.kvh) * ROW;
         // what lies behind the sequence's last key or behind the piece is not read (the former is masked wherever it could count)
-        uint32_t k_lane[2], v_lane[2];
+        uint32_t k_lane[4], v_lane[4];
 #pragma unroll
-        for (int odd = 0; odd < 2; ++odd) {
-            const int row = odd * PER + trow;
-            k_lane[odd] = trow * stride + ((tchunk ^ (row & 7)) << 4);
-            v_lane[odd] = trow * stride + ((tchunk ^ (2 * row & (CHUNKS - 1))) << 4);
+        for (int i = 0; i < 4; ++i) {
+            const int row = i * PER + trow;
+            k_lane[i] = trow * stride + (Tile<D>::k_chunk(row, tchunk) << 4);
+            v_lane[i] = trow * stride + (Tile<D>::v_chunk(row, tchunk) << 4);
         }
-        auto request = [&](int step, const uint8_t *src, uint8_t *tile, const uint32_t (&at)[2]) {
+        auto request = [&](int step, const uint8_t *src, uint8_t *tile, const uint32_t (&at)[4]) {
             const long long key0 = (long long)step * KEYS;
             const uint32_t bytes = step < p.s1 ? (uint32_t)min((s.T - 1 - key0) * stride + ROW, 0x7FFFFFFFll) : 0;
             const Stretch from = stretch(src + (size_t)key0 * stride, bytes);
 #pragma unroll
-            for (int i = 0; i < TRANSFERS; ++i) quad_to_lds(from, tile + i * 1024, at[i & 1], (uint32_t)(i * PER) * stride);
+            for (int i = 0; i < TRANSFERS; ++i) quad_to_lds(from, tile + i * 1024, at[i & 3], (uint32_t)(i * PER) * stride);
         };
         Rows<D> rows;
         rows.start(a, s, p, c, h);
