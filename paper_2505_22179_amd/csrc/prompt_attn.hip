@@ -955,10 +955,13 @@ static PromptPlan prompt_plan(int rows, int B, int max_q, int max_k, int Hq, int
         // of 256 where prompts are long and workgroups many and D is 128: 4096 queries, 32/8 heads 152 us (128 rows: 161), 16384 2131 (2219), but 16 x 1000, 16/16 heads
         // 168 (130), 8 prompts of up to 1500, 64/8 heads 162 (153); D 64, 4096 queries 109 (101), 24 prompts of up to 700, 28/4 heads 59 (47).
         // Few tiles behind many keys are cut into equal stretches (40 us more for pieces written, read and joined) where that is shorter, were all sequences as
-        // long as the longest: 4 x 64 queries behind 2936 keys, 32/8 heads 58 us (whole 69); 2048 queries 90 (59).
+        // long as the longest; of several behind prefixes, which seldom are, 0.6 of that: the longest holds whole tiles up, equal stretches the sum.  32/8 heads:
+        // 4 x 64 queries behind 2936 keys 52 us (whole 69), 2048 queries 90 (54), 8 single tokens over up to 8000 keys with 1000 queries of one prompt 83 (136), 32 of them over
+        // up to 4000 with 256 behind 2744 142 (112).
         const long long steps = (max_k + 63) / 64, part = max_q >= max_k ? 1 : 2;   // a whole prompt's rows see half of its keys on average
         const long long high = tiles_of(256) * Hkv, low = tiles_of(128) * Hkv, of_size = D == 128 ? 100 : 62;
-        const long long halves = steps * of_size * (low <= 256 ? 1350 : 1650) / 100, cut = high * steps * part * of_size * 1075 / 256 / 100 + 40000;
+        const long long halves = steps * of_size * (low <= 256 ? 1350 : 1650) / 100, evenly = high * steps * part * of_size * 1075 / 256 / 100;
+        const long long cut = (B > 1 && part == 2 ? evenly * 6 / 10 : evenly) + 40000;
         p.cut = low <= 512 && cut < halves;
         p.rows = p.cut || (D == 128 && high >= 512 && (long long)rows * group >= 16384ll * B) ? 256 : 128;
     }
