@@ -999,8 +999,9 @@ static int launch_prompt(const PromptArgs &a, const PromptPlan &p, hipStream_t s
         hipLaunchKernelGGL((prompt_attn_join_kernel<D, 256, kTileKeys, kTileLeast>), dim3(256 / kJoinRows, (unsigned)p.grid), dim3(256), 0, stream, a);
         return launch_status();
     }
-    if (p.rows == 128) return launch_with_lds<D + 2>(&prompt_attn_tile_kernel<D, 4, 2, false>, 2 * stage, 256, a, p, stream);
-    return launch_with_lds<D + 3>(&prompt_attn_tile_kernel<D, 8, 4, false>, 4 * stage, 512, a, p, stream);
+    if constexpr (D == 128)
+        if (p.rows == 256) return launch_with_lds<D + 3>(&prompt_attn_tile_kernel<D, 8, 4, false>, 4 * stage, 512, a, p, stream);
+    return launch_with_lds<D + 2>(&prompt_attn_tile_kernel<D, 4, 2, false>, 2 * stage, 256, a, p, stream);
 }
 
 }  // namespace w4

@@ -265,3 +265,34 @@ def test_keys_that_arrive_late(lens, Hq, Hkv, D):
         if first is None:
             first = out
         assert torch.equal(out, first), call
+
+
+@pytest.mark.parametrize("lens, Hq, Hkv, D", [([(40, 40), (70, 70)], 8, 2, 128), ([(150, 150), (90, 200)], 14, 2, 64), ([(100, 2500), (60, 1000)], 8, 2, 128), ([(100, 2500), (60, 1000)], 14, 2, 64),
+                                              ([(3, 600), (2, 333)], 8, 2, 128), ([(2100, 2100)], 64, 8, 128)])
+def test_one_value_that_is_not_finite(lens, Hq, Hkv, D):
+    """in kernels for few rows, tiles of 128 and 256 rows, whole and cut: it reaches the rows that see it, in its place, and nothing else"""
+    b = Batch(21, lens, Hq, Hkv, D)
+    clean = b.run()
+    n, T = lens[-1]
+    key, group = T - (n + 1) // 2, Hq // Hkv   # seen by the later half of the last sequence's queries
+    b.v[b.k_start[-1] + key, 0, 3], b.v[b.k_start[-1] + key, Hkv - 1, D - 1] = np.inf, np.nan
+    got, want = b.run(), clean.copy()
+    sees = slice(b.q_start[-2] + key - (T - n), b.q_start[-1])
+    assert not np.isfinite(got[sees, :group, 3]).any() and not np.isfinite(got[sees, -group:, D - 1]).any()
+    want[sees, :group, 3], want[sees, -group:, D - 1] = got[sees, :group, 3], got[sees, -group:, D - 1]
+    np.testing.assert_array_equal(got, want)
+
+
+def test_rows_of_the_largest_tiles():
+    """prompts long and many enough for tiles of 256 rows, which begin and end inside queries of odd groups: rows of them, and the same rows asked for alone"""
+    for lens, Hq, Hkv in (([(2100, 2100)], 64, 8), ([(3500, 3700)], 40, 8)):
+        n, T = lens[0]
+        b = Batch(22, lens, Hq, Hkv, 128)
+        got = b.run()
+        assert (got[n:] == SENTINEL).all()
+        for i in (0, 1, 31, 32, 51, 52, 700, n - 33, n - 1):
+            one = Batch(22, lens, Hq, Hkv, 128)
+            one.lens, one.rows, one.q = [(1, T - n + i + 1)], 1, b.q[i:i + 1]
+            one.q_start, one.k_len = np.array([0, 1], dtype=np.int32), np.array([T - n + i + 1], dtype=np.int32)
+            ref, spread = R.prompt_attn(one.q, one.k, one.v, one.q_start, one.k_start, one.k_len, one.scale, np.zeros(one.q.shape))
+            close(got[i:i + 1], ref, spread, T, one.scale * 128 * np.abs(one.q.astype(np.float64)).max() * 6)
