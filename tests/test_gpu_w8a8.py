@@ -264,3 +264,9 @@ def test_input_in_place(M, K, pre):
     B.w8a8_linear(buffer, pre, dev(lin.gamma), lin.eps, lin.packed(), dev(lin.t), None, buffer, M, 512, K, lin.workspace())
     torch.cuda.synchronize()
     np.testing.assert_array_equal(buffer[:M].cpu().numpy().view(np.uint16), want.view(np.uint16))
+
+
+@pytest.mark.parametrize("M, N, K", [(1900, 8072, 1168), (25, 6152, 1040), (60, 6152, 528)])
+def test_linears_whose_tiles_end_outside(M, N, K):
+    """tiles of 256 x 256, and two tiles of channels to a wavefront"""
+    Linear(M, M, N, K, B.W8A8_RMS_NORM, True).check()
