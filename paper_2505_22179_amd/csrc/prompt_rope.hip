@@ -125,8 +125,8 @@ struct Unit {
     Part a, b;
     __device__ __forceinline__ void load(const _Float16 *src, int at, int gap)
     {
-        a = *reinterpret_cast<const Part *>(src + at);
-        b = *reinterpret_cast<const Part *>(src + at + gap);
+        a = __builtin_nontemporal_load(reinterpret_cast<const Part *>(src + at));
+        b = __builtin_nontemporal_load(reinterpret_cast<const Part *>(src + at + gap));
     }
     __device__ __forceinline__ void store(_Float16 *dst, int at, int gap) const
     {
@@ -135,8 +135,8 @@ struct Unit {
     }
 };
 
-// A workgroup per token; bound by the copy where there are many (8192 tokens, 64/8 heads of 128: 62 us in the kernel, 5.4 TB/s), by the launch where there are few
-// (16 tokens 3.6 us).
+// A workgroup per token, whose next head is on its way while one is turned; bound by the copy where there are many (8192 tokens of first use, 64/8 heads of 128:
+// 71.5 us, 4.8 TB/s; one head after another 74.1), by the launch where there are few (16 tokens 3.6 us).
 template <int V, bool INTERLEAVED>
 __global__ __launch_bounds__(kRopeThreads) void rope_prompt_kernel(PromptRopeArgs a)
 {
@@ -144,12 +144,18 @@ __global__ __launch_bounds__(kRopeThreads) void rope_prompt_kernel(PromptRopeArg
     const int heads_at_once = kRopeThreads / units;
     const int u = threadIdx.x % units, h0 = threadIdx.x / units;
     if (h0 >= heads_at_once) return;
-    const int p = a.pos[m], to = a.slot ? a.slot[m] : m;
-    const bool placed = p >= 0 && p < a.n_pos, stored = to >= 0 && to < a.cache_rows;
     const int heads = a.Hq + 2 * a.Hkv;
     const _Float16 *const row = a.qkv + (size_t)m * heads * a.D;
     const bool turns = u < turned;
     const int at = turns && !INTERLEAVED ? u * V : u * 2 * V, gap = turns && !INTERLEAVED ? pairs : V;   // of queries and keys
+    Unit<V> ahead;   // of the next head; the first is asked for before the position is known
+    auto load = [&](int head) {
+        const bool value = head >= a.Hq + a.Hkv;
+        ahead.load(row + (size_t)head * a.D, value ? u * 2 * V : at, value ? V : gap);
+    };
+    if (h0 < heads) load(h0);
+    const int p = a.pos[m], to = a.slot ? a.slot[m] : m;
+    const bool placed = p >= 0 && p < a.n_pos, stored = to >= 0 && to < a.cache_rows;
     float c[V], s[V];
     if (turns && placed) {
 #pragma unroll
@@ -158,8 +164,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_prompt_kernel(PromptRopeArg
     for (int head = h0; head < heads; head += heads_at_once) {
         const bool value = head >= a.Hq + a.Hkv;
         const int here = value ? u * 2 * V : at, step = value ? V : gap;
-        Unit<V> x;
-        x.load(row + (size_t)head * a.D, here, step);
+        Unit<V> x = ahead;
+        if (head + heads_at_once < heads) load(head + heads_at_once);
         if (!value) {
             if (!placed) continue;   // this row's q and k are left untouched
             if (turns) {
