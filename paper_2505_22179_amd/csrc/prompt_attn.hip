@@ -155,6 +155,29 @@ struct Line {
         }
         return false;
     }
+    // brings the sequence of tile `number` of the line to hand, right after the constructor; where the tile begins, or -1 if there are fewer
+    __device__ __forceinline__ long long find_tile(const PromptArgs &a, int number, int lane)
+    {
+        for (; base < a.B; base += 64) {
+            Sequence mine;
+            int upto_tiles;
+            const long long upto = read(a, mine, upto_tiles, lane);
+            const uint64_t hit = __ballot(upto_tiles > number && base + lane < a.B);
+            if (hit) {
+                const int src = __builtin_ctzll(hit);
+                auto take = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
+                seq = {take(mine.n), take(mine.T), take(mine.q0), take(mine.k0), take(mine.tiles), take(mine.ahead)};
+                per_head = cost<ROWS>(seq, a.group, seq.tiles);
+                to = of_lane(upto, src);
+                from = to - per_head * a.Hkv;
+                const int of_it = number - (take(upto_tiles) - seq.tiles * a.Hkv), kvh = of_it / seq.tiles;
+                return from + kvh * per_head + cost<ROWS>(seq, a.group, of_it - kvh * seq.tiles);
+            }
+            before = of_lane(upto, 63);
+            number -= __builtin_amdgcn_readlane(upto_tiles, 63);
+        }
+        return -1;
+    }
 };
 
 // One piece of work: steps s0 .. s1 - 1 of a tile.
@@ -590,12 +613,12 @@ __device__ __forceinline__ void go_through(const PromptArgs &a, int tid, float *
 }
 
 // Joins the pieces of the tiles that the tile kernel's stretches cut, kJoinRows rows to a workgroup: a tile of 256 rows is 128 KB a piece, of which one
-// workgroup alone reads 20 KB in a microsecond (4 x 64 queries behind 7936 keys, 32/8 heads: 103 us joined by the last to finish, 72 like this).
-// blockIdx.x: rows (next to each other on all XCDs: cut tiles begin at every eighth stretch, say); blockIdx.y: the stretch whose end cuts the tile
-// that begins in it.
+// workgroup alone reads 20 KB in a microsecond (4 x 64 queries behind 7936 keys, 32/8 heads: 103 us joined by the last to finish, 57 like this).
+// blockIdx.x: rows (next to each other on all XCDs); blockIdx.y: the tile.  With a workgroup per stretch instead, most of which find that no tile begins
+// there, 72 queries over 20000 keys and 50 over 18000, 16/2 heads, took 71 us, like this 61.
 constexpr int kJoinRows = 8;
 template <int D, int ROWS, int STEP, int LEAST>
-__global__ __launch_bounds__(256) void prompt_attn_join_kernel(PromptArgs a)
+__global__ __launch_bounds__(256) void prompt_attn_join_kernel(PromptArgs a, unsigned stretches)
 {
     static_assert(kMostGroups <= 256, "");
     const int tid = threadIdx.x, lane = tid & 63;
@@ -605,15 +628,14 @@ __global__ __launch_bounds__(256) void prompt_attn_join_kernel(PromptArgs a)
     Sequence mine;
     long long first_upto;
     Line<ROWS> line(a, lane, mine, first_upto);
-    const Cut<ROWS> cut(line, a.group, gridDim.y, LEAST);
-    const unsigned me = blockIdx.y;
-    const long long at = cut.border(me + 1);
-    if (me + 1 >= cut.groups || at >= line.total) return;
-    if (!line.find(a, at, lane, mine, first_upto, a.B <= 64)) return;
+    const Cut<ROWS> cut(line, a.group, stretches, LEAST);
+    const long long at = line.find_tile(a, (int)blockIdx.y, lane);
+    if (at < 0) return;
     Piece p;
     tile_of<ROWS, STEP>(a, line, at, p);
     const int row0 = blockIdx.x * kJoinRows;
-    if (p.begin >= at || p.begin < cut.border(me) || p.steps == 0 || row0 >= p.rows) return;   // not cut here, or not first here
+    const unsigned me = (unsigned)__builtin_amdgcn_readfirstlane((int)divide(p.begin, cut.length));   // the stretch that it begins in
+    if (p.end <= cut.border(me + 1) || p.steps == 0 || row0 >= p.rows) return;   // not cut
     const auto found = cut.look(p, me, tid, lane, pieces_sh);
     __syncthreads();
     const uint32_t pieces = cut.template finish<4>(found, tid, lane, pieces_sh, slots);
@@ -929,7 +951,7 @@ constexpr int kFewRows = 32;
 
 struct PromptPlan {
     bool few, cut;
-    int rows, grid;   // of a tile; workgroups
+    int rows, grid, tiles;   // of a tile; workgroups; tiles at most
     size_t o_bytes, ml_bytes;
 };
 
@@ -956,7 +978,7 @@ static PromptPlan prompt_plan(int rows, int B, int max_q, int max_k, int Hq, int
         // 168 (130), 8 prompts of up to 1500, 64/8 heads 162 (153); D 64, 4096 queries 109 (101), 24 prompts of up to 700, 28/4 heads 59 (47).
         // Few tiles behind many keys are cut into equal stretches (40 us more for pieces written, read and joined) where that is shorter, were all sequences as
         // long as the longest; of several behind prefixes, which seldom are, 0.6 of that: the longest holds whole tiles up, equal stretches the sum.  32/8 heads:
-        // 4 x 64 queries behind 2936 keys 52 us (whole 69), 2048 queries 90 (54), 8 single tokens over up to 8000 keys with 1000 queries of one prompt 83 (136), 32 of them over
+        // 4 x 64 queries behind 2936 keys 46 us (whole 69), 2048 queries 90 (54), 8 single tokens over up to 8000 keys with 1000 queries of one prompt 83 (136), 32 of them over
         // up to 4000 with 256 behind 2744 142 (112).
         const long long steps = (max_k + 63) / 64, part = max_q >= max_k ? 1 : 2;   // a whole prompt's rows see half of its keys on average
         const long long high = tiles_of(256) * Hkv, low = tiles_of(128) * Hkv, of_size = D == 128 ? 100 : 62;
@@ -967,12 +989,14 @@ static PromptPlan prompt_plan(int rows, int B, int max_q, int max_k, int Hq, int
     }
     const long long tiles = tiles_of(p.rows);
     if (p.cut) {   // no more workgroups than there can be work for, were every sequence as long as the longest
+        p.tiles = (int)min(tiles * Hkv, 65535ll);
         p.grid = (int)min(tiles * Hkv * (((long long)max_k + 255) / 256), (long long)kMostGroups);
         p.o_bytes = (size_t)p.grid * 2 * p.rows * D * 4;
         p.ml_bytes = (size_t)p.grid * 2 * p.rows * 8;
     } else {       // whole tiles, as take_one() deals them out
         p.grid = (int)(8 % Hkv == 0 ? (tiles + 8 / Hkv - 1) / (8 / Hkv) * 8 : tiles * Hkv);
         p.o_bytes = p.ml_bytes = 0;
+        p.tiles = 0;
     }
     return p;
 }
@@ -996,7 +1020,7 @@ static int launch_prompt(const PromptArgs &a, const PromptPlan &p, hipStream_t s
     if (p.cut) {
         const int rc = launch_with_lds<D + 1>(&prompt_attn_tile_kernel<D, 8, 4, true>, 4 * stage, 512, a, p, stream);
         if (rc != W4A16_OK) return rc;
-        hipLaunchKernelGGL((prompt_attn_join_kernel<D, 256, kTileKeys, kTileLeast>), dim3(256 / kJoinRows, (unsigned)p.grid), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((prompt_attn_join_kernel<D, 256, kTileKeys, kTileLeast>), dim3(256 / kJoinRows, (unsigned)p.tiles), dim3(256), 0, stream, a, (unsigned)p.grid);
         return launch_status();
     }
     if constexpr (D == 128)
