@@ -118,12 +118,11 @@ struct Line {
         }
         return min(upto + before, kLongestLine);
     }
-    __device__ __forceinline__ Line(const PromptArgs &a, int lane, Sequence &mine, long long &upto)
+    __device__ __forceinline__ Line(const PromptArgs &a, int lane, Sequence &mine, long long &upto, int &upto_tiles)
     {
         total = from = to = per_head = before = 0;
         tiles = 0;
         for (base = 0; base < a.B; base += 64) {
-            int upto_tiles;
             upto = read(a, mine, upto_tiles, lane);
             before = of_lane(upto, min(63, a.B - base - 1));
             tiles = min(tiles + __builtin_amdgcn_readlane(upto_tiles, min(63, a.B - base - 1)), kMostTiles);
@@ -155,13 +154,13 @@ struct Line {
         }
         return false;
     }
-    // brings the sequence of tile `number` of the line to hand, right after the constructor; where the tile begins, or -1 if there are fewer
-    __device__ __forceinline__ long long find_tile(const PromptArgs &a, int number, int lane)
+    // brings the sequence of tile `number` of the line to hand, right after the constructor (mine and the like as for find()); where the tile begins, or
+    // -1 if there are fewer
+    __device__ __forceinline__ long long find_tile(const PromptArgs &a, int number, int lane, Sequence mine, long long upto, int upto_tiles, bool known)
     {
         for (; base < a.B; base += 64) {
-            Sequence mine;
-            int upto_tiles;
-            const long long upto = read(a, mine, upto_tiles, lane);
+            if (!known) upto = read(a, mine, upto_tiles, lane);
+            known = false;
             const uint64_t hit = __ballot(upto_tiles > number && base + lane < a.B);
             if (hit) {
                 const int src = __builtin_ctzll(hit);
@@ -572,7 +571,8 @@ __device__ __forceinline__ void go_through(const PromptArgs &a, int tid, float *
     __shared__ uint16_t slots[kMostGroups];
     Sequence mine;
     long long first_upto;
-    Line<ROWS> line(a, lane, mine, first_upto);
+    int upto_tiles;
+    Line<ROWS> line(a, lane, mine, first_upto, upto_tiles);
     const Cut<ROWS> cut(line, a.group, gridDim.x, LEAST);
     if (blockIdx.x >= cut.groups) return;
     const unsigned me = stretch_number(blockIdx.x, cut.groups);
@@ -627,9 +627,10 @@ __global__ __launch_bounds__(256) void prompt_attn_join_kernel(PromptArgs a, uns
     __shared__ __attribute__((aligned(16))) float shared[256 * 6];
     Sequence mine;
     long long first_upto;
-    Line<ROWS> line(a, lane, mine, first_upto);
+    int upto_tiles;
+    Line<ROWS> line(a, lane, mine, first_upto, upto_tiles);
     const Cut<ROWS> cut(line, a.group, stretches, LEAST);
-    const long long at = line.find_tile(a, (int)blockIdx.y, lane);
+    const long long at = line.find_tile(a, (int)blockIdx.y, lane, mine, first_upto, upto_tiles, a.B <= 64);
     if (at < 0) return;
     Piece p;
     tile_of<ROWS, STEP>(a, line, at, p);
