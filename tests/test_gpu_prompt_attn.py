@@ -296,3 +296,11 @@ def test_rows_of_the_largest_tiles():
             one.q_start, one.k_len = np.array([0, 1], dtype=np.int32), np.array([T - n + i + 1], dtype=np.int32)
             ref, spread = R.prompt_attn(one.q, one.k, one.v, one.q_start, one.k_start, one.k_len, one.scale, np.zeros(one.q.shape))
             close(got[i:i + 1], ref, spread, T, one.scale * 128 * np.abs(one.q.astype(np.float64)).max() * 6)
+
+
+@pytest.mark.parametrize("where", [0, 40, 69])
+def test_a_cut_tile_among_many_sequences(where):
+    """more sequences than a wavefront reads at a time, one of them long enough to be cut, empty ones between"""
+    lens = [(i % 3, 1 + 7 * i % 150) for i in range(70)]
+    lens[where] = (100, 9000)
+    Batch(23 + where, lens, 8, 2, 128).check()
