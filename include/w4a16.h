@@ -372,7 +372,7 @@ size_t w4a16_prompt_attn_workspace_bytes(int rows, int B, int max_q, int max_k, 
  *                  their roundings do
  * A row that sees no key (more queries than keys) gets zeros.  Softmax and sums in fp32; probabilities are rounded to fp16 for the product with the values.
  * A row whose visible scores are all -inf, or among them a NaN or +inf, is NaN; one that sees a value that is not finite is not finite there.  D 64 or 128,
- * Hq % Hkv == 0, Hq / Hkv <= 64, Hkv <= 1024, B <= 4096, rows <= 2^23, rows * Hq <= 2^29, a finite scale > 0.  `workspace` as for tree_verify_attn. */
+ * Hq % Hkv == 0, Hq / Hkv <= 64, Hkv <= 1024, B <= 4096, rows <= 2^23, rows * Hq <= 2^29, 0 < scale <= 2^60.  `workspace` as for tree_verify_attn. */
 int w4a16_prompt_attn(const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start, const int32_t *k_len, void *out, int B,
                       int rows, int k_rows, int max_q, int max_k, int Hq, int Hkv, int D, float scale, void *workspace, size_t workspace_bytes,
                       void *stream);

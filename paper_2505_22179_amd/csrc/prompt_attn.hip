@@ -19,6 +19,9 @@ typedef __attribute__((address_space(3))) half4v lds_half4v;
 
 constexpr int kMostSequences = 4096;
 constexpr int kMostTiles = 1 << 20;   // that are counted; more than workgroups anyhow
+constexpr float kLag = 8.f;
+constexpr float kFar = 0x1p20f;   // scaled scores from here on: half a last place is 2^-4 here
+constexpr float kMostScale = 0x1p60f;   // |q . k| of 128 fp16 products is below 2^39, a scaled score above kLowest
 constexpr int kMostGroups = 256;   // workgroups of a call: one per compute unit, a ticket each
 
 struct PromptArgs {
@@ -253,6 +256,7 @@ struct Rows {
     half8v qf[D / 16];
     float16v o[D / 32];
     float m_run, l_run;   // l_run: this lane's share (its keys) of the row's sum
+    float lag;            // how far a score may exceed m_run before that moves
     int pos;              // the row sees keys 0 .. pos
 
     __device__ __forceinline__ void start(const PromptArgs &a, const Sequence &s, const Piece &p, int row, int h)
@@ -263,6 +267,7 @@ struct Rows {
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) qf[j] = *reinterpret_cast<const half8v *>(src + 16 * j);
         m_run = kLowest;
+        lag = kLag;
         l_run = 0.f;
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
@@ -290,9 +295,9 @@ struct Rows {
         for (int j = 0; j < D / 16; ++j) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[j], qf[j], s, 0, 0, 0);
     }
 
-    // their probabilities, as operands of the product with the values, and the running sum; returns the factor that the outputs are still to be scaled by
+    // their probabilities, as operands of the product with the values, and the running sum; scales the outputs where their reference moves
     template <int KT>
-    __device__ __forceinline__ float probabilities(float16v (&s)[KT], half8v (&pb)[2 * KT], float scale_log2e)
+    __device__ __forceinline__ void probabilities(float16v (&s)[KT], half8v (&pb)[2 * KT], float scale_log2e)
     {
         float m[2] = {max_of_two(s[0][0], s[0][1]), max_of_two(s[0][2], s[0][3])};
 #pragma unroll
@@ -302,27 +307,44 @@ struct Rows {
         // The scale is positive (checked by the host): the largest raw score is the largest scaled one.  The maximum that the exponentials are taken
         // from moves only where it has grown by 8 (a factor of 2^8, in fp16 probabilities of up to 256): the outputs are seldom scaled, and any
         // reference that is not far below the largest score serves as well.
-        const float m_seen = half_wave_max(max_of_two(m[0], m[1])) * scale_log2e;
-        const float m_larger = max_of_two(m_run, m_seen), m_new = m_seen <= m_run + 8.f ? m_run : m_larger, alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-        m_run = m_new;
-        const float less = -m_new;
+        // The largest score's product with the scale is rounded in the maximum and not in the multiply-add below: half a last place of the maximum, which from
+        // 2^27 on is more than a probability in fp16 has room for.  Far from zero the scores are scaled, and so rounded alike, beforehand: such a row
+        // comes by here in every step.
+        const float m_seen = half_wave_max(max_of_two(m[0], m[1])) * scale_log2e, grown = m_seen - m_run;
+        float factor = scale_log2e;
+        if (__any(grown > lag)) {
+            const float m_new = grown > kLag ? m_seen : m_run, alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
+            const bool far = __builtin_fabsf(m_new) >= kFar;
+            lag = far ? -__builtin_inff() : kLag;
+            if (__any(far)) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[kt][i] *= scale_log2e;
+                factor = 1.f;
+            }
+        }
+        const float less = -m_run;
         float sum[2] = {};
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], scale_log2e, less));
-                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i + 1], scale_log2e, less));
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], factor, less));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i + 1], factor, less));
                 const half2v both = __builtin_convertvector((float2v){p0, p1}, half2v);
                 sum[(i >> 1) & 1] = __builtin_amdgcn_fdot2(both, (half2v){1, 1}, sum[(i >> 1) & 1], false);   // of what multiplies the values; one instruction for two
                 pb[2 * kt + (i >> 3)][i & 7] = both[0];
                 pb[2 * kt + (i >> 3)][(i & 7) + 1] = both[1];
             }
-        l_run = l_run * alpha + (sum[0] + sum[1]);
-        return alpha;
+        l_run += sum[0] + sum[1];
     }
 
-    // the same with the mask, and the outputs scaled
+    // the same with the mask
     template <int KT, bool MASKED>
     __device__ __forceinline__ void softmax(float16v (&s)[KT], half8v (&pb)[2 * KT], int key0, float scale_log2e, int h)
     {
@@ -335,11 +357,7 @@ struct Rows {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[kt][i] = 32 * kt + 8 * (i >> 2) + (i & 3) <= room ? s[kt][i] : -__builtin_inff();
         }
-        const float alpha = probabilities<KT>(s, pb, scale_log2e);
-        if (__any(alpha != 1.f)) {
-#pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
-        }
+        probabilities<KT>(s, pb, scale_log2e);
     }
 
     // fragments u of the V tile: 16 keys, all D values
@@ -1048,6 +1066,7 @@ int w4a16_prompt_attn(const void *q, const void *k, const void *v, const int32_t
     const int rc = check_prompt_sizes(rows, B, max_q, max_k, Hq, Hkv, D);
     if (rc != W4A16_OK) return rc;
     if (k_rows < 1 || !(scale > 0.f) || !(scale < __builtin_inff())) return W4A16_EINVAL;
+    if (scale > kMostScale) return W4A16_EUNSUP;
     if (!q || !k || !v || !q_start || !out || (k_start == nullptr) != (k_len == nullptr)) return W4A16_ENULL;
     if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) ||
         ((reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(k_start) | reinterpret_cast<uintptr_t>(k_len)) & 3u))

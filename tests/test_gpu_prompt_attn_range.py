@@ -1,0 +1,46 @@
+"""GPU: attention of packed sequences where scores leave the range that fp16 probabilities and fp32 exponents have room for, in every kernel."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_22179_amd import binding as B
+from tests.test_gpu_prompt_attn import Batch
+
+pytestmark = pytest.mark.gpu
+# few rows; tiles of 128 rows; tiles of 128 rows that are cut into ranges of keys (they have 256); whole tiles of 256 rows
+KERNELS = [([(1, 4000), (1, 33)], 8, 2, 128), ([(2, 900), (1, 60)], 8, 2, 64), ([(200, 200), (40, 90)], 8, 2, 128), ([(150, 200)], 14, 2, 64), ([(100, 9000)], 8, 2, 128),
+           ([(100, 9000)], 14, 2, 64), ([(2100, 2100)], 64, 8, 128)]
+
+
+def rows_of(b):
+    """(row, query head, first key row, keys seen) of some forty rows of the batch, the first and last of each sequence among them"""
+    for (n, T), q0, k0 in zip(b.lens, b.q_start, b.k_start):
+        for i in sorted({int(x) for x in np.linspace(0, n - 1, 14)}):
+            for head in {0, b.Hq // 2 + 1, b.Hq - 1}:
+                yield q0 + i, head, k0, T - n + i + 1
+
+
+@pytest.mark.parametrize("lens, Hq, Hkv, D", KERNELS)
+@pytest.mark.parametrize("std, scale", [(300.0, None), (4000.0, None), (15000.0, None), (1.2, 1e10), (1.2, 2.0 ** 60)])
+def test_scores_far_from_zero(lens, Hq, Hkv, D, std, scale):
+    """finite queries and keys whose largest score, of up to 2^30 and 2^66, takes everything: outputs lie among the values of the keys that may be the
+    largest.  A score is off by 128 roundings of fp32 at the most, 2^-17 of its products' magnitudes; 30 below the largest, a key weighs less than 2^-43"""
+    b = Batch(31, lens, Hq, Hkv, D)
+    rng = np.random.default_rng(int(std))
+    b.q, b.k = (np.clip(rng.standard_normal(x.shape) * std, -60000, 60000).astype(np.float16) for x in (b.q, b.k))
+    b.scale = scale or b.scale
+    got = b.run().astype(np.float64)
+    q, k, v = (x.astype(np.float64) for x in (b.q, b.k, b.v))
+    for row, head, k0, seen in rows_of(b):
+        kh, vh = k[k0:k0 + seen, head // (Hq // Hkv)], v[k0:k0 + seen, head // (Hq // Hkv)]
+        s, size = kh @ q[row, head], np.abs(kh) @ np.abs(q[row, head])
+        may_be = vh[s >= s.max() - 2.0 ** -16 * size.max() - 30 / b.scale]
+        near = 2.0 ** -10 * np.abs(may_be).max(0) + 2.0 ** -20
+        assert (got[row, head] >= may_be.min(0) - near).all() and (got[row, head] <= may_be.max(0) + near).all(), (row, head)
+
+
+@pytest.mark.parametrize("lens, Hq, Hkv, D", KERNELS[:6])
+def test_the_smallest_scale_weighs_all_keys_alike(lens, Hq, Hkv, D):
+    b = Batch(32, lens, Hq, Hkv, D)
+    b.scale = 1e-38
+    b.check()
