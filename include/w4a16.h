@@ -370,7 +370,8 @@ size_t w4a16_prompt_attn_workspace_bytes(int rows, int B, int max_q, int max_k, 
  *             (on the device, 4-byte aligned; a sequence whose rows do not lie in [0, rows) and [0, k_rows) is left out)
  *   max_q, max_k   most queries and keys of a sequence, by which work is divided: results do not depend on their being right,
  *                  their roundings do
- * A row that sees no key (more queries than keys) gets zeros.  Softmax and sums in fp32; probabilities are rounded to fp16 for the product with the values.
+ * A row that sees no key (more queries than keys) gets zeros.  Softmax and sums in fp32; probabilities are rounded to fp16 for the product with the values,
+ * and one below 2^-32 of the row's largest may count as 0.
  * A row whose visible scores are all -inf, or among them a NaN or +inf, is NaN; one that sees a value that is not finite is not finite there.  D 64 or 128,
  * Hq % Hkv == 0, Hq / Hkv <= 64, Hkv <= 1024, B <= 4096, rows <= 2^23, rows * Hq <= 2^29, 0 < scale <= 2^60.  `workspace` as for tree_verify_attn. */
 int w4a16_prompt_attn(const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start, const int32_t *k_len, void *out, int B,

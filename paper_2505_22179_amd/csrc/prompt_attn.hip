@@ -19,7 +19,7 @@ typedef __attribute__((address_space(3))) half4v lds_half4v;
 
 constexpr int kMostSequences = 4096;
 constexpr int kMostTiles = 1 << 20;   // that are counted; more than workgroups anyhow
-constexpr float kLag = 8.f;
+constexpr float kLag = 8.f, kRaise = 7.f;   // probabilities reach 2^(kLag + kRaise), and 2^(1/8) times that (see kFar): fp16 ends below 2^16
 constexpr float kFar = 0x1p20f;   // scaled scores from here on: half a last place is 2^-4 here
 constexpr float kMostScale = 0x1p60f;   // |q . k| of 128 fp16 products is below 2^39, a scaled score above kLowest
 constexpr int kMostGroups = 256;   // workgroups of a call: one per compute unit, a ticket each
@@ -305,15 +305,18 @@ struct Rows {
 #pragma unroll
             for (int i = kt ? 0 : 4; i < 16; i += 2) m[(i >> 1) & 1] = max_of_three(m[(i >> 1) & 1], s[kt][i], s[kt][i + 1]);
         // The scale is positive (checked by the host): the largest raw score is the largest scaled one.  The maximum that the exponentials are taken
-        // from moves only where it has grown by 8 (a factor of 2^8, in fp16 probabilities of up to 256): the outputs are seldom scaled, and any
-        // reference that is not far below the largest score serves as well.
+        // from moves only where it has grown by kLag: the outputs are seldom scaled, and any reference that is not far below the largest score serves as well.
+        // It is lowered by kRaise, so that fp16 probabilities use the range that it leaves above: up to 2^15 now, and weights down to 2^-32 of the largest count
+        // (2^-25 without it: behind a key 26 binary orders above all others 9000 keys kept 15 % of their weight or none).  The products' operands are fp16
+        // because the matrix instruction with fp32 has a sixteenth of the rate; rounding each probability to 11 bits leaves an output within 2^-11 of its
+        // weighted magnitudes, as its own rounding does.
         // The largest score's product with the scale is rounded in the maximum and not in the multiply-add below: half a last place of the maximum, which from
         // 2^27 on is more than a probability in fp16 has room for.  Far from zero the scores are scaled, and so rounded alike, beforehand: such a row
-        // comes by here in every step.
+        // comes by here in every step, and its maximum does not lag, because kRaise, too, is rounded there.
         const float m_seen = half_wave_max(max_of_two(m[0], m[1])) * scale_log2e, grown = m_seen - m_run;
         float factor = scale_log2e;
         if (__any(grown > lag)) {
-            const float m_new = grown > kLag ? m_seen : m_run, alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            const float m_new = grown > fmaxf(lag, 0.f) ? m_seen : m_run, alpha = __builtin_amdgcn_exp2f(m_run - m_new);
             m_run = m_new;
             l_run *= alpha;
 #pragma unroll
@@ -328,7 +331,7 @@ struct Rows {
                 factor = 1.f;
             }
         }
-        const float less = -m_run;
+        const float less = kRaise - m_run;
         float sum[2] = {};
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)

@@ -44,3 +44,33 @@ def test_the_smallest_scale_weighs_all_keys_alike(lens, Hq, Hkv, D):
     b = Batch(32, lens, Hq, Hkv, D)
     b.scale = 1e-38
     b.check()
+
+
+@pytest.mark.parametrize("lens, Hq, Hkv, D", KERNELS)
+@pytest.mark.parametrize("orders", [12, 20, 26, 30])
+def test_keys_far_above_the_others(lens, Hq, Hkv, D, orders):
+    """keys `orders` binary orders above all others, whose values are 0, in every range that one wavefront or workgroup walks: what the others weigh
+    makes up the output.  A probability p (the row's largest 1) is rounded by 2^-11 p, or below fp16's normal range, 2^-14 where the largest is 2^7 at least,
+    by 2^-25 of 2^-7; fp32 adds 2^-20 and 2^-22 of the largest score"""
+    b = Batch(33, lens, Hq, Hkv, D)
+    rng = np.random.default_rng(orders)
+    b.scale = 1.0
+    b.q = (rng.standard_normal(b.q.shape) * 0.03).astype(np.float16)
+    b.q[..., 0] = 1.0
+    b.k = (rng.standard_normal(b.k.shape) * 0.5).astype(np.float16)
+    b.k[..., 0] = 0
+    b.v = (rng.uniform(512, 1536, b.v.shape)).astype(np.float16)
+    for k0, (n, T) in zip(b.k_start, b.lens):
+        high = np.arange(k0, k0 + T, 32 if n < 5 else 500)
+        b.k[high, :, 0], b.v[high] = orders * np.log(2), 0
+    got = b.run().astype(np.float64)
+    q, k, v = (x.astype(np.float64) for x in (b.q, b.k, b.v))
+    for row, head, k0, seen in rows_of(b):
+        kh, vh = k[k0:k0 + seen, head // (Hq // Hkv)], v[k0:k0 + seen, head // (Hq // Hkv)]
+        s = kh @ q[row, head]
+        p = np.exp(s - s.max())
+        want = p @ vh / p.sum()
+        off = np.maximum((2.0 ** -11 + 2.0 ** -20 + 2.0 ** -22 * np.abs(s).max()) * p, 2.0 ** -32)
+        bound = (off @ vh + off.sum() * want) / p.sum() + 2.0 ** -11 * want + 2.0 ** -25
+        err = np.abs(got[row, head] - want)
+        assert (err <= bound).all(), (row, head, (err / bound).max(), want[:3], got[row, head, :3])
