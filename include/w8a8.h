@@ -1,8 +1,8 @@
 /*
  * libw8a8 -- C ABI of the MI355X (gfx950) W8A8 linear layer: int8 weights with a scale for each output channel, activations
  * quantised to int8 with a scale for each token (paper section 2.2, "W8A8"), for any number of tokens: plain decoding, a draft's
- * verification and whole prompts.  A library of its own beside libw4a16, whose conventions, return codes (include/w4a16.h), workspaces
- * and w4a16_workspace_init it shares.
+ * verification and whole prompts.  A library of its own beside libw4a16, whose conventions, return codes (include/w4a16.h) and workspaces
+ * it shares; it exports w4a16_workspace_init and w4a16_strerror too, so that a program of W8A8 linears needs no other.
  *
  * Layout of codes, weights and activations alike: tiles of 16 rows (channels or tokens) by 64 values of k, 1 KB each, in the order in
  * which the 16x16x64 matrix instruction takes its operands; rows are padded to a multiple of 16, k to a multiple of 128:

@@ -132,6 +132,9 @@ def load_w8a8() -> ctypes.CDLL:
     L = ctypes.CDLL(LIB_W8A8_PATH)
     vp, i, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
     L.w8a8_packed_bytes.restype = L.w8a8_workspace_bytes.restype = sz
+    L.w4a16_workspace_init.argtypes = [vp, sz, vp]
+    L.w4a16_strerror.restype = ctypes.c_char_p
+    L.w4a16_strerror.argtypes = [i]
     L.w8a8_packed_bytes.argtypes = [i, i]
     L.w8a8_workspace_bytes.argtypes = [i, i, i]
     L.w8a8_pack.argtypes = L.w8a8_unpack.argtypes = [vp, vp, i, i, vp]

@@ -2,6 +2,7 @@
 // path) and the bit-exact dequantisation test export.  See layout.h for the packed layout and
 // include/w4a16.h for the contracts.
 #include "internal.h"
+#include "shared_entries.inc"
 #include <hip/hip_fp16.h>
 #include <string.h>
 
@@ -153,12 +154,6 @@ __global__ __launch_bounds__(256) void symmetric_check_kernel(const uint8_t *__r
     if (!all8) *flag = 0;
 }
 
-__global__ void fill_zero_kernel(uint32_t *p, size_t words)
-{
-    size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i < words) p[i] = 0u;
-}
-
 // plain streaming read of `n16` 16-byte words: the bandwidth ceiling the GEMM is compared with.
 // Workgroup b reads the contiguous 32 KB chunk b with all of its loads in flight at once, the
 // fastest of the patterns tried on this GPU (strided grids and larger chunks were slower).
@@ -193,20 +188,6 @@ using namespace w4;
 extern "C" {
 
 int w4a16_version(void) { return 100; }
-
-const char *w4a16_strerror(int code)
-{
-    switch (code) {
-    case W4A16_OK: return "ok";
-    case W4A16_EINVAL: return "invalid shape or argument";
-    case W4A16_ENULL: return "null pointer";
-    case W4A16_EALIGN: return "pointer not 16-byte aligned";
-    case W4A16_EUNSUP: return "unsupported configuration";
-    case W4A16_EWORKSPACE: return "workspace missing or too small";
-    case W4A16_EHIP: return "HIP runtime error";
-    default: return "unknown error code";
-    }
-}
 
 static int *param_slot(const char *name)
 {
@@ -247,17 +228,6 @@ size_t w4a16_packed_bytes(int N, int K, int G)
 {
     if (check_weight_shape(N, K, G) != W4A16_OK) return 0;
     return (size_t)(pad_cols(N) / kBlockCols) * (size_t)(K / kGroup) * (size_t)kRecordBytes;
-}
-
-int w4a16_workspace_init(void *workspace, size_t workspace_bytes, void *stream)
-{
-    if (!workspace) return W4A16_ENULL;
-    if (workspace_misaligned(workspace)) return W4A16_EALIGN;
-    if (workspace_bytes < kTicketBytes) return W4A16_EWORKSPACE;
-    size_t words = kTicketBytes / 4;
-    hipLaunchKernelGGL(fill_zero_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0,
-                       (hipStream_t)stream, (uint32_t *)workspace, words);
-    return launch_status();
 }
 
 int w4a16_weight_is_symmetric(const void *packed, int N, int K, int G, int32_t *flag, void *stream)

@@ -1,6 +1,7 @@
 // W8A8 linear: quantisation of tokens, the product of int8 codes, packing.  Contracts in include/w8a8.h.
 #include "../internal.h"
 #include "../devscope.h"
+#include "../shared_entries.inc"
 #include "../../../include/w8a8.h"
 
 namespace w4 {
