@@ -504,6 +504,11 @@ int tree_verify_attn_plan_describe(int M, int P, int Hq, int Hkv, int D, size_t 
  * format and sizes. */
 int tree_verify_attn_kv8_plan_describe(int M, int P, int Hq, int Hkv, int D, int format, int *out);
 
+/* How w4a16_prompt_attn deals out a call of these sizes, so that a test can show which of its kernels it has compared with the oracle.  out receives
+ * 3 ints: [0] 0 = few rows, 1 = whole tiles, 2 = tiles that are cut where a workgroup's equal stretch of the work ends, [1] rows (query and
+ * head) of a tile, [2] workgroups.  Host only: touches no GPU.  Errors as w4a16_prompt_attn's size checks. */
+int w4a16_prompt_attn_plan_describe(int rows, int B, int max_q, int max_k, int Hq, int Hkv, int D, int *out);
+
 /* The logits kernel lm_head_topk would run with the current knobs.  out receives 3 ints: [0] 1 if the wavefronts of a
  * workgroup share x through LDS, 0 if each fetches its own, [1] wavefronts per workgroup, [2] vocabulary tiles per
  * wavefront.  16 wavefronts mean the kernel that keeps x in LDS: four of them share each of the workgroup's four tiles,

@@ -51,6 +51,12 @@ int w8a8_gemm(const void *codes, const float *scale, const void *packed, const f
 int w8a8_linear(const void *x, int pre, const void *gamma, float eps, const void *packed, const float *w_scale, const void *residual, void *y, int M,
                 int N, int K, void *workspace, size_t workspace_bytes, void *stream);
 
+/* How w8a8_gemm, and w8a8_linear behind its quantisation, would run a product, so that a test can show which kernels it has compared with the
+ * oracle.  out receives 4 ints: [0] 0 = weights streamed for few tokens, 1 = tiles, [1] tokens and [2] channels of a workgroup's tile, [3] workgroups
+ * that share a tile's walk along k.  (w8a8_linear has a kernel of its own for one token of K up to 4096.)  Host only: touches no GPU.  Errors as
+ * w8a8_gemm's size checks. */
+int w8a8_gemm_plan_describe(int M, int N, int K, int *out);
+
 #ifdef __cplusplus
 }
 #endif

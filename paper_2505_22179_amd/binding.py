@@ -21,9 +21,10 @@ EXPORTS = (
     "lm_head_packed_bytes", "lm_head_pack", "w4a16_decoder_layer", "w4a16_plan_describe", "w4a16_gemm_static", "w4a16_weight_is_symmetric",
     "tree_verify_attn_plan_describe", "lm_head_plan_describe", "rope_append_qk_norm", "rope_append_kv8", "w4a16_kv8_read", "tree_accept_kv8",
     "tree_verify_attn_kv8", "tree_verify_attn_kv8_workspace_bytes", "tree_verify_attn_kv8_plan_describe", "lm_head_sample", "lm_head_sample_workspace_bytes",
-    "rope_table", "rope_prompt", "w4a16_prompt_attn", "w4a16_prompt_attn_workspace_bytes",
+    "rope_table", "rope_prompt", "w4a16_prompt_attn", "w4a16_prompt_attn_workspace_bytes", "w4a16_prompt_attn_plan_describe",
 )
-EXPORTS_W8A8 = ("w8a8_packed_bytes", "w8a8_pack", "w8a8_unpack", "w8a8_quantize", "w8a8_workspace_bytes", "w8a8_gemm", "w8a8_linear")   # of include/w8a8.h
+EXPORTS_W8A8 = ("w8a8_packed_bytes", "w8a8_pack", "w8a8_unpack", "w8a8_quantize", "w8a8_workspace_bytes", "w8a8_gemm", "w8a8_linear",
+                "w8a8_gemm_plan_describe")   # of include/w8a8.h
 
 EPI_NONE, EPI_RESIDUAL, EPI_SILU_MUL = 0, 1, 2
 SYMMETRIC = 0x100   # OR-ed into an epilogue code: every zero-point of the weight is 8
@@ -118,6 +119,7 @@ def load() -> ctypes.CDLL:
     L.rope_prompt.argtypes = [vp, vp, vp, vp, i, i, i, vp, i, vp, vp, vp, i, i, i, i, vp]
     L.w4a16_prompt_attn_workspace_bytes.restype = sz
     L.w4a16_prompt_attn_workspace_bytes.argtypes = [i] * 7
+    L.w4a16_prompt_attn_plan_describe.argtypes = [i] * 7 + [ctypes.POINTER(ctypes.c_int)]
     L.w4a16_prompt_attn.argtypes = [vp] * 7 + [i] * 8 + [ctypes.c_float, vp, sz, vp]
     _lib = L
     return L
@@ -140,6 +142,7 @@ def load_w8a8() -> ctypes.CDLL:
     L.w8a8_pack.argtypes = L.w8a8_unpack.argtypes = [vp, vp, i, i, vp]
     L.w8a8_quantize.argtypes = [vp, i, vp, ctypes.c_float, vp, vp, i, i, vp]
     L.w8a8_gemm.argtypes = [vp] * 6 + [i, i, i, vp, sz, vp]
+    L.w8a8_gemm_plan_describe.argtypes = [i, i, i, ctypes.POINTER(ctypes.c_int)]
     L.w8a8_linear.argtypes = [vp, i, vp, ctypes.c_float, vp, vp, vp, vp, i, i, i, vp, sz, vp]
     _lib_w8a8 = L
     return L
@@ -468,6 +471,13 @@ def w4a16_prompt_attn_workspace_bytes(rows: int, B: int, max_q: int, max_k: int,
     return load().w4a16_prompt_attn_workspace_bytes(rows, B, max_q, max_k, Hq, Hkv, D)
 
 
+def w4a16_prompt_attn_plan_describe(rows: int, B: int, max_q: int, max_k: int, Hq: int, Hkv: int, D: int) -> tuple:
+    """(0 few rows, 1 whole tiles or 2 cut tiles; rows of a tile; workgroups); host only."""
+    out = (ctypes.c_int * 3)()
+    _check(load().w4a16_prompt_attn_plan_describe(rows, B, max_q, max_k, Hq, Hkv, D, out), "w4a16_prompt_attn_plan_describe")
+    return tuple(out)
+
+
 def w4a16_prompt_attn(q, k, v, q_start, k_start, k_len, out, B: int, rows: int, k_rows: int, max_q: int, max_k: int, Hq: int, Hkv: int, D: int,
                       scale: float, workspace) -> None:
     _init_cuda()
@@ -486,6 +496,13 @@ def w8a8_packed_bytes(rows: int, K: int) -> int:
 
 def w8a8_workspace_bytes(M: int, N: int, K: int) -> int:
     return load_w8a8().w8a8_workspace_bytes(M, N, K)
+
+
+def w8a8_gemm_plan_describe(M: int, N: int, K: int) -> tuple:
+    """(0 streamed weights or 1 tiles; tokens and channels of a workgroup's tile; workgroups that share its walk along k); host only."""
+    out = (ctypes.c_int * 4)()
+    _check(load_w8a8().w8a8_gemm_plan_describe(M, N, K, out), "w8a8_gemm_plan_describe")
+    return tuple(out)
 
 
 def w8a8_pack(w, packed, rows: int, K: int) -> None:

@@ -1063,6 +1063,18 @@ size_t w4a16_prompt_attn_workspace_bytes(int rows, int B, int max_q, int max_k, 
     return kTicketBytes + p.o_bytes + p.ml_bytes;
 }
 
+int w4a16_prompt_attn_plan_describe(int rows, int B, int max_q, int max_k, int Hq, int Hkv, int D, int *out)
+{
+    if (!out) return W4A16_ENULL;
+    const int rc = check_prompt_sizes(rows, B, max_q, max_k, Hq, Hkv, D);
+    if (rc != W4A16_OK) return rc;
+    const PromptPlan p = prompt_plan(rows, B, max_q, max_k, Hq, Hkv, D);
+    out[0] = p.few ? 0 : p.cut ? 2 : 1;
+    out[1] = p.rows;
+    out[2] = p.grid;
+    return W4A16_OK;
+}
+
 int w4a16_prompt_attn(const void *q, const void *k, const void *v, const int32_t *q_start, const int32_t *k_start, const int32_t *k_len, void *out, int B,
                       int rows, int k_rows, int max_q, int max_k, int Hq, int Hkv, int D, float scale, void *workspace, size_t workspace_bytes, void *stream)
 {

@@ -624,6 +624,19 @@ size_t w8a8_workspace_bytes(int M, int N, int K)
     return kTicketBytes + codes_bytes(M, K) + aligned256((size_t)M * 4) + most_partials(M);
 }
 
+int w8a8_gemm_plan_describe(int M, int N, int K, int *out)
+{
+    if (!out) return W4A16_ENULL;
+    const int rc = check_gemm_shape(M, N, K);
+    if (rc != W4A16_OK) return rc;
+    const GemmPlan p = gemm_plan(M, N, K);
+    out[0] = p.kind != kStream;
+    out[1] = p.rows;
+    out[2] = p.cols;
+    out[3] = p.splits;
+    return W4A16_OK;
+}
+
 int w8a8_gemm(const void *codes, const float *scale, const void *packed, const float *w_scale, const void *residual, void *y, int M, int N, int K,
               void *workspace, size_t workspace_bytes, void *stream)
 {
