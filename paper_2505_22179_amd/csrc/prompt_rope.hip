@@ -54,7 +54,8 @@ __device__ __forceinline__ void cos_sin(double a, double &c, double &s)
 
 // A workgroup takes kTablePositions positions and works out the frequencies once (into LDS), with the turn from one of a thread's positions to its next.
 // A thread keeps V pairs, evaluates cos and sin at its first position and turns them on from there in fp64 (four instructions an entry instead of
-// some forty; 128 turns in a row are off by 2^-45 at the most).  What bounds it are the writes: 131072 positions, 64 pairs, 12.6 us, 5.3 TB/s (every
+// some forty).  A turn is off by 2^-51 (its own roundings, cos and sin) and half a last place of its angle, at_once f; kTablePositions / at_once of
+// them in a row by 2^-44 + 2^-46 f at the most, f up to 8 (a factor of 1/8), beside the rounding of the first angle.  What bounds it are the writes: 131072 positions, 64 pairs, 12.6 us, 5.3 TB/s (every
 // entry evaluated by itself 16.5).
 template <int V>
 __global__ __launch_bounds__(kTableThreads) void rope_table_kernel(TableArgs a)
