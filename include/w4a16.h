@@ -367,7 +367,8 @@ size_t w4a16_prompt_attn_workspace_bytes(int rows, int B, int max_q, int max_k, 
  *   q, out    fp16 [rows, Hq, D];  rows that no sequence names are left untouched
  *   k, v      fp16 [k_rows, Hkv, D]; rows that a sequence does not see may hold anything
  *   q_start   int32 [B + 1], ascending;  k_start, k_len int32 [B], both or neither: without them the keys lie as the queries do
- *             (on the device, 4-byte aligned; a sequence whose rows do not lie in [0, rows) and [0, k_rows) is left out)
+ *             (on the device, 4-byte aligned; a sequence whose rows do not lie in [0, rows) and [0, k_rows) is left out).
+ *             Any order; prompts are begun from the last one on, so a call of uneven ones is shortest with the longest last
  *   max_q, max_k   most queries and keys of a sequence, by which work is divided: results do not depend on their being right,
  *                  their roundings do
  * A row that sees no key (more queries than keys) gets zeros.  Softmax and sums in fp32; probabilities are rounded to fp16 for the product with the values,

@@ -668,7 +668,8 @@ __global__ __launch_bounds__(256) void prompt_attn_join_kernel(PromptArgs a, uns
 
 // Many tiles: one per workgroup, whole.  They are numbered from the last of the last sequence down, so that the tiles that see most keys of a sequence are
 // the first to be dealt out, and an XCD keeps to its own KV heads or to its share of a head's tiles: workgroups that start together read the same keys,
-// which come from memory once for all of them (16384 queries, 32/8 heads: 2449 us, in equal stretches 3000).
+// which come from memory once for all of them (16384 queries, 32/8 heads: 2449 us, in equal stretches 3000).  The order of sequences stays the caller's: a prompt
+// of 2000 in front of 30 of 200, 32/8 heads, begins last, 94 us, and behind them first, 84.
 template <int D, int ROWS, int STEP, typename Work>
 __device__ __forceinline__ void take_one(const PromptArgs &a, int lane, Work work)
 {
@@ -714,7 +715,7 @@ __device__ __forceinline__ void take_one(const PromptArgs &a, int lane, Work wor
 }
 
 // Many rows: NW wavefronts of 32 rows each, keys through LDS in tiles of 64, one barrier per tile, STAGES buffers of which all but one are under way.
-// 16384 queries, 32/8 heads: 2110 us, 1040 TFLOP/s at a clock that power holds at 1.8 GHz; matrix units busy 54 % of the cycles, vector units 45 %, LDS 28 %: a
+// 16384 queries, 32/8 heads: 2015 to 2115 us from card to card, 1.04 to 1.09 PFLOP/s at a clock that power holds at 1.8 GHz; matrix units busy 54 % of the cycles, vector units 47 %, LDS 28 %: a
 // wavefront's products and its softmax follow one another, and two wavefronts on a SIMD hide only part of one behind the other (products alone take
 // 1460 us, the vector instructions alone 1210).  Four wavefronts of 64 rows, halves of the wavefronts a phase apart, products and softmax of two tiles interleaved, priorities: 2190 to 2800.
 constexpr int kTileKeys = 64, kTileLeast = 1024;
@@ -851,7 +852,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attn_tile_kernel(PromptArgs
 
 // Few rows (single tokens of a batch): 32 rows, and eight wavefronts that each take every eighth step of 32 keys.  A wavefront shares no K or V tile,
 // so it brings them itself and meets the others only at the end of a piece: no barrier in the walk.  Bound by the cache where it is long (16 x 8192 keys, 8 heads of
-// 128: 105 us, 5.1 TB/s), else by its chain: lengths, first tiles, meeting of the wavefronts, join (one of 8192 14 us, of 100 7.4).
+// 128: 105 us, 5.1 TB/s), else by its chain: lengths, first tiles, meeting of the wavefronts, join (one of 8192 14 us, of 100 7.4; of first use 17.7 and 8).  More than 64 sequences cost every workgroup
+// one trip to memory more for the lengths of each 64 (64 of 512 keys 33 us, 65 40, 256 116, 4096 1650, 5.3 TB/s).
 template <int D>
 __global__ __launch_bounds__(512) void prompt_attn_few_kernel(PromptArgs a)
 {
@@ -996,12 +998,14 @@ static PromptPlan prompt_plan(int rows, int B, int max_q, int max_k, int Hq, int
     p.cut = true;
     if (!p.few) {
         // Whole tiles of 128 rows, two and more to a compute unit (D 128: a step of 64 keys takes 1.35 us alone, 1.65 with a neighbour, a round of many 2.15), or
-        // of 256 where prompts are long and workgroups many and D is 128: 4096 queries, 32/8 heads 152 us (128 rows: 161), 16384 2131 (2219), but 16 x 1000, 16/16 heads
-        // 168 (130), 8 prompts of up to 1500, 64/8 heads 162 (153); D 64, 4096 queries 109 (101), 24 prompts of up to 700, 28/4 heads 59 (47).
+        // of 256 where prompts are long and workgroups many and D is 128: 4096 queries, 32/8 heads 152 us (128 rows: 158), 16384 2095 (2121), but 16 x 1000, 16/16 heads
+        // 135 (123), 8 prompts of up to 1500, 64/8 heads 155 (149); D 64, 4096 queries 103 (94), 24 prompts of 700, 28/4 heads 114 (92), of up to 700 26 (20).
         // Few tiles behind many keys are cut into equal stretches (40 us more for pieces written, read and joined) where that is shorter, were all sequences as
         // long as the longest; of several behind prefixes, which seldom are, 0.6 of that: the longest holds whole tiles up, equal stretches the sum.  32/8 heads:
-        // 4 x 64 queries behind 2936 keys 46 us (whole 69), 2048 queries 90 (54), 8 single tokens over up to 8000 keys with 1000 queries of one prompt 83 (136), 32 of them over
-        // up to 4000 with 256 behind 2744 142 (112).
+        // 4 x 64 queries behind 2936 keys 48 us (whole 78), 2048 queries 89 (61), 8 single tokens over up to 8000 keys with a prompt of 1000 72 (205), 16 of them over up to
+        // 4000 with a prompt of 512 67 to 80 (101 to 105).  The host does not see how uneven lengths are, so the choice is wrong where they are not what the factor takes
+        // them for: 16 tokens over 4000 each with that prompt 118 cut, as they are, 108 whole; 8 x 100 behind up to 4000 104 whole, as they are, 76 cut (behind 2000 each 60
+        // and 68), 32 tokens over up to 4000 with 256 queries behind 2744 121 whole, as they are, 103 cut.
         const long long steps = (max_k + 63) / 64, part = max_q >= max_k ? 1 : 2;   // a whole prompt's rows see half of its keys on average
         const long long high = tiles_of(256) * Hkv, low = tiles_of(128) * Hkv, of_size = D == 128 ? 100 : 62;
         const long long halves = steps * of_size * (low <= 256 ? 1350 : 1650) / 100, evenly = high * steps * part * of_size * 1075 / 256 / 100;

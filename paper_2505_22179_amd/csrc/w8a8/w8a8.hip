@@ -84,6 +84,8 @@ __device__ __forceinline__ u32x4 codes_of(const half8 (&v)[2], float s, float in
 }
 
 // One token by the first T threads of a workgroup; a thread keeps PER chunks of sixteen values in registers: one pass over the input.
+// 8192 tokens of 4096 as they are 23 us, behind a norm 30, of which the copy rate allows 20: vector units 75 % busy and two barriers a token.  777 gated ones of
+// 14336 17, of which 11: `up` is asked for eight values at a time, behind the gate that it multiplies, a trip to memory each.
 // store(chunk, codes) receives the chunks, those of the padding too (zeros).  Returns the scale (in the first T threads).  Two barriers, for all threads.
 template <int PRE, int T, int PER, typename Store>
 __device__ __forceinline__ float quantize_row(const _Float16 *__restrict__ row, const _Float16 *__restrict__ gamma, float eps, int K, int padded,
