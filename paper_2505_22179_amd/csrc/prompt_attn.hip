@@ -311,34 +311,34 @@ struct Rows {
         // because the matrix instruction with fp32 has a sixteenth of the rate; rounding each probability to 11 bits leaves an output within 2^-11 of its
         // weighted magnitudes, as its own rounding does.
         // The largest score's product with the scale is rounded in the maximum and not in the multiply-add below: half a last place of the maximum, which from
-        // 2^27 on is more than a probability in fp16 has room for.  Far from zero the scores are scaled, and so rounded alike, beforehand: such a row
-        // comes by here in every step, and its maximum does not lag, because kRaise, too, is rounded there.
+        // 2^27 on is more than a probability in fp16 has room for.  Far from zero a row's scores are scaled, and so rounded alike, beforehand and their distance from the
+        // maximum takes their place (over the scale, so that the multiply-add is the same for all rows): such a row comes by here in every step.
         const float m_seen = half_wave_max(max_of_two(m[0], m[1])) * scale_log2e, grown = m_seen - m_run;
-        float factor = scale_log2e;
+        float less = kRaise - m_run;
         if (__any(grown > lag)) {
-            const float m_new = grown > fmaxf(lag, 0.f) ? m_seen : m_run, alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            const float m_new = grown > kLag ? m_seen : m_run, alpha = __builtin_amdgcn_exp2f(m_run - m_new);
             m_run = m_new;
             l_run *= alpha;
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
-            const bool far = __builtin_fabsf(m_new) >= kFar;
+            const bool far = __builtin_fabsf(m_new) >= kFar && __builtin_fabsf(m_new) < -kLowest;   // neither a row that has seen nothing nor an infinite one
             lag = far ? -__builtin_inff() : kLag;
+            less = far ? kRaise : kRaise - m_new;
             if (__any(far)) {
+                const float over = 1.f / scale_log2e;
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[kt][i] *= scale_log2e;
-                factor = 1.f;
+                    for (int i = 0; i < 16; ++i) s[kt][i] = far ? (keep_f32(s[kt][i] * scale_log2e) - m_new) * over : s[kt][i];
             }
         }
-        const float less = kRaise - m_run;
         float sum[2] = {};
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], factor, less));
-                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i + 1], factor, less));
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], scale_log2e, less));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i + 1], scale_log2e, less));
                 const half2v both = __builtin_convertvector((float2v){p0, p1}, half2v);
                 sum[(i >> 1) & 1] = __builtin_amdgcn_fdot2(both, (half2v){1, 1}, sum[(i >> 1) & 1], false);   // of what multiplies the values; one instruction for two
                 pb[2 * kt + (i >> 3)][i & 7] = both[0];
@@ -715,7 +715,7 @@ __device__ __forceinline__ void take_one(const PromptArgs &a, int lane, Work wor
 }
 
 // Many rows: NW wavefronts of 32 rows each, keys through LDS in tiles of 64, one barrier per tile, STAGES buffers of which all but one are under way.
-// 16384 queries, 32/8 heads: 2015 to 2115 us from card to card, 1.04 to 1.09 PFLOP/s at a clock that power holds at 1.8 GHz; matrix units busy 54 % of the cycles, vector units 47 %, LDS 28 %: a
+// 16384 queries, 32/8 heads: 2015 to 2180 us from card to card, 1.01 to 1.09 PFLOP/s at a clock that power holds at 1.8 GHz; matrix units busy 54 % of the cycles, vector units 47 %, LDS 28 %: a
 // wavefront's products and its softmax follow one another, and two wavefronts on a SIMD hide only part of one behind the other (products alone take
 // 1460 us, the vector instructions alone 1210).  Four wavefronts of 64 rows, halves of the wavefronts a phase apart, products and softmax of two tiles interleaved, priorities: 2190 to 2800.
 constexpr int kTileKeys = 64, kTileLeast = 1024;

@@ -74,3 +74,23 @@ def test_keys_far_above_the_others(lens, Hq, Hkv, D, orders):
         bound = (off @ vh + off.sum() * want) / p.sum() + 2.0 ** -11 * want + 2.0 ** -25
         err = np.abs(got[row, head] - want)
         assert (err <= bound).all(), (row, head, (err / bound).max(), want[:3], got[row, head, :3])
+
+
+@pytest.mark.parametrize("lens, Hq, Hkv, D", KERNELS)
+@pytest.mark.parametrize("what", ["a query far from zero", "an infinite key"])
+def test_rows_far_from_zero_leave_the_others_bits_alone(lens, Hq, Hkv, D, what):
+    """the rows of a wavefront share its branches, not their arithmetic"""
+    b = Batch(34, lens, Hq, Hkv, D)
+    b.q, b.k = (b.q * np.float16(0.03)).astype(np.float16), (b.k * np.float16(30)).astype(np.float16)
+    want = b.run()
+    n, T = lens[0]
+    others = np.ones((b.rows, Hq), dtype=bool)
+    if what == "an infinite key":   # seen by the first sequence's last row alone
+        b.k[b.k_start[0] + T - 1, :, 0] = np.inf
+        others[n - 1] = False
+    else:                           # one head of it
+        b.q[n - 1, 1] = (b.q[n - 1, 1].astype(np.float32) * 1e6).clip(-60000, 60000).astype(np.float16)
+        others[n - 1, 1] = False
+    got = b.run()
+    np.testing.assert_array_equal(got[others].view(np.uint16), want[others].view(np.uint16))
+    assert (got[~others].view(np.uint16) != want[~others].view(np.uint16)).any()
