@@ -715,7 +715,7 @@ __device__ __forceinline__ void take_one(const PromptArgs &a, int lane, Work wor
 }
 
 // Many rows: NW wavefronts of 32 rows each, keys through LDS in tiles of 64, one barrier per tile, STAGES buffers of which all but one are under way.
-// 16384 queries, 32/8 heads: 2015 to 2180 us from card to card, 1.01 to 1.09 PFLOP/s at a clock that power holds at 1.8 GHz; matrix units busy 54 % of the cycles, vector units 47 %, LDS 28 %: a
+// 16384 queries, 32/8 heads: 2015 to 2180 us from card to card, 1.01 to 1.09 PFLOP/s at a clock that power holds at 1.8 GHz; matrix units busy 54 % of the cycles, vector units 46 %, LDS 28 %: a
 // wavefront's products and its softmax follow one another, and two wavefronts on a SIMD hide only part of one behind the other (products alone take
 // 1460 us, the vector instructions alone 1210).  Four wavefronts of 64 rows, halves of the wavefronts a phase apart, products and softmax of two tiles interleaved, priorities: 2190 to 2800.
 constexpr int kTileKeys = 64, kTileLeast = 1024;
